@@ -1633,6 +1633,23 @@ bool make_tmap_bf16(CUtensorMap* tm, const void* ptr, uint64_t rows, uint64_t co
     return r == CUDA_SUCCESS;
 }
 
+bool make_tmap_16bit(CUtensorMap* tm, const void* ptr, bool f16, int rank, const uint64_t* dims, const uint64_t* strides,
+                     const uint32_t* box) {
+    EncodeTiledFn enc = get_encode();
+    if (!enc || rank < 2 || rank > 4) return false;
+    cuuint64_t d[4], s[3];
+    cuuint32_t b[4], e[4];
+    for (int i = 0; i < rank; ++i) {
+        d[i] = dims[i];
+        b[i] = box[i];
+        e[i] = 1;
+        if (i + 1 < rank) s[i] = strides[i];
+    }
+    return enc(tm, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(ptr), d,
+               s, b, e, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 cudaError_t gemm_init_attrs() { return chain_init_attrs(); }
 
 // One projection = a chain of one phase.

@@ -191,6 +191,10 @@ inline size_t gemm_partial_floats(const GemmPlan& p) {
     return static_cast<size_t>(p.grid) * static_cast<size_t>(p.slots) * static_cast<size_t>(p.ntile) * 128;
 }
 bool make_tmap_bf16(CUtensorMap* tm, const void* ptr, uint64_t rows, uint64_t cols, uint32_t box_rows);
+// The same for any shape: rank 2 to 4, innermost dimension first, strides (bytes) of dimensions 1 up, box of 64
+// values innermost.
+bool make_tmap_16bit(CUtensorMap* tm, const void* ptr, bool f16, int rank, const uint64_t* dims, const uint64_t* strides,
+                     const uint32_t* box);
 cudaError_t gemm_launch(int epi, const GemmPlan& p, const CUtensorMap& tmW, const CUtensorMap& tmX,
                         const EpiArgs& ep, const Scratch& scr, int* status, cudaStream_t st,
                         const int* gate = nullptr);

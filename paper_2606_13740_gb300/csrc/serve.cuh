@@ -40,9 +40,26 @@ struct ServeWork {
     int rows;            // new tokens covered
     int pad;
     long long total;     // steps of all units
-    int pad2[6];
+    int shape[5];        // what the list was made for (serve_same_shape)
+    int pad2;
 };
 static_assert(sizeof(ServeWork) == 64, "the arrays behind it are 16-byte aligned");
+
+// Whether a work list was made for this config (calls with another one find its arrays elsewhere).
+__host__ __device__ inline void serve_key(const ServeShape& s, int* key) {
+    key[0] = s.Hkv;
+    key[1] = s.G;
+    key[2] = s.page;
+    key[3] = s.max_tiles;
+    key[4] = s.max_blocks;
+}
+__device__ inline bool serve_same_shape(const ServeShape& s, const ServeWork& w) {
+    int key[5];
+    serve_key(s, key);
+    bool same = true;
+    for (int i = 0; i < 5; ++i) same = same && key[i] == w.shape[i];
+    return same;
+}
 
 struct ServeArrays {
     ServeWork* head;

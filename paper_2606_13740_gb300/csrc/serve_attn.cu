@@ -1,105 +1,695 @@
 // Attention of a serving step's rows over the shared prefix and each request's own pages
-// (include/dllm_serve.h, dllm_serve_attention): one warp a (row, query head), 32 keys at a time, a lane
-// a key for the scores and hd / 32 features a lane for the values.
+// (include/dllm_serve.h, dllm_serve_attention) on the 5th-generation tensor cores.
+//
+// A tile is 128 query rows of one K/V head: tile_tokens tokens of the packed batch, whatever requests they
+// belong to, with the head's G query heads side by side.  So the prefix's keys and values are loaded once
+// for all the requests in the tile.  After the prefix the tile goes through its requests' own blocks of 64
+// keys, one request after another: only that request's rows are live then, and the tensor cores leave the
+// others' lanes of O as they are (disable-output-lane), so that one request's values, NaN included, never
+// reach another's rows.  The plan has cut all tiles' steps into equal runs, one a CTA (serve.cuh); a unit
+// (tile, K/V head) that a CTA holds whole is written out, the parts of the others go to a workspace and
+// k_serve_join joins them in order.  Per step j:
+//   S_j = Q K_j^T         tcgen05.mma, Q and K_j in shared memory (K-major), S_j in tensor memory
+//   P_j = exp2(S_j - m)   one thread a query row; P_j (16 bit) written back over S_j
+//   O  += P_j V_j         tcgen05.mma, P_j from tensor memory, V_j in shared memory (MN-major)
+// The running maximum m moves only when a block's maximum exceeds it by more than 8 (log2 units); only then
+// are O and the row's sum rescaled, so P stays below 2^8.  P is rounded to the cache's type, as the tensor
+// cores take it; the sum is of the unrounded values.  Warps 0-3: softmax and output (a thread a row); warp 4:
+// TMA loads, a box a page and 64 features; warp 5: MMA issue.
+// Keys past a request's end score -inf, and their values, which may be anything, are set to 0 in shared memory.
 #include "serve.cuh"
 
 namespace dllm {
 
 namespace {
 
+constexpr int kThreads = 192;
+constexpr int kHalfQ = kServeRows * 128;    // bytes of 64 features of the Q tile
+constexpr int kHalfKV = kServeBlock * 128;  // and of a K or V block
+constexpr float kLn2 = 0.6931471805599453f;
+
+template <int HD>
+constexpr int kStages = HD == 128 ? 2 : 4;  // K/V blocks in flight, two CTAs an SM
+template <int HD>
+constexpr int kSmem = 1024 + HD / 64 * (kHalfQ + 2 * kStages<HD> * kHalfKV);
+
+struct Maps {
+    CUtensorMap q;  // [rows][Hkv][G][hd], box: 64 features, the group, one head, tile_tokens rows
+    CUtensorMap k;  // [n_pages][Hkv * page][hd], box: 64 features of up to 64 places of a page
+    CUtensorMap v;
+};
+
+__device__ __forceinline__ uint64_t sw128(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+    d |= static_cast<uint64_t>((lbo >> 4) & 0x3FFFu) << 16;
+    d |= static_cast<uint64_t>((sbo >> 4) & 0x3FFFu) << 32;
+    d |= static_cast<uint64_t>(1u) << 46;  // descriptor version for tcgen05
+    d |= static_cast<uint64_t>(2u) << 61;  // 128-byte swizzle
+    return d;
+}
+// D += A B with A from tensor memory, B from shared memory; the lanes of D whose bit in off is set keep
+// their value.
+__device__ __forceinline__ void umma_tmem_a_masked(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint4 off) {
+    asm volatile(
+        "{\n .reg .pred p;\n setp.eq.b32 p, 0, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%4, %5, %6, %7}, p;\n}\n" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(off.x), "r"(off.y), "r"(off.z), "r"(off.w)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_32u(uint32_t taddr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, "
+        "%14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tma_3d(void* dst, const CUtensorMap* tm, int x, int y, int z, uint64_t* bar, uint64_t pol) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
+        " [%0], [%1, {%3, %4, %5}], [%2], %6;" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(tm)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "l"(pol)
+        : "memory");
+}
+__device__ __forceinline__ void tma_4d(void* dst, const CUtensorMap* tm, int x, int y, int z, int w, uint64_t* bar,
+                                       uint64_t pol) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
+        " [%0], [%1, {%3, %4, %5, %6}], [%2], %7;" ::"r"(smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(tm)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w), "l"(pol)
+        : "memory");
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n"
+        " fma.rn.f32x2 d, a, b, c;\n mov.b64 {%0, %1}, d;\n}\n"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n"
+        " add.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}\n"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+// 2^x by the special function unit; below 2^-126: 0
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// bits lo .. hi - 1 (any ints)
+__device__ __forceinline__ uint32_t bit_run(int lo, int hi) {
+    lo = min(max(lo, 0), 32);
+    hi = min(max(hi, lo), 32);
+    const uint32_t up = hi == 32 ? 0xffffffffu : (1u << hi) - 1u;
+    return lo == 32 ? 0u : up & ~((1u << lo) - 1u);
+}
+
+// One CTA's run of steps, unit by unit: the same walk in every role.
+struct Walk {
+    const ServeArrays& w;
+    int Hkv, tile, hk, step, left;
+    int n, own0;          // steps of the current segment; the tile's first own block (-1: none)
+    long long first, next;  // the tile's place in the sums
+    __device__ Walk(const ServeArrays& w_, int Hkv_, int cta) : w(w_), Hkv(Hkv_) {
+        const int4 d = __ldg(w.cta + cta);
+        tile = d.x;
+        hk = d.y;
+        step = d.z;
+        left = d.w;
+        if (left > 0) {
+            first = w.tile_cum[tile];
+            next = w.tile_cum[tile + 1];
+            own0 = w.tile_first[tile];
+            n = min(left, steps() - step);
+        }
+    }
+    __device__ int steps() const { return static_cast<int>(next - first); }
+    __device__ bool whole() const { return step == 0 && n == steps(); }
+    // to the next segment; false: that was the last
+    __device__ bool advance() {
+        left -= n;
+        if (left <= 0) return false;
+        step = 0;
+        if (++hk == Hkv) {
+            hk = 0;
+            ++tile;
+            first = next;
+            next = w.tile_cum[tile + 1];
+            own0 = w.tile_first[tile];
+        }
+        n = min(left, steps());
+        return n > 0;
+    }
+};
+
 template <int HD, typename T>
-__global__ void __launch_bounds__(128) k_serve_attn(ServeShape s, dllm_serve_tables t, ServeAttnArgs a) {
-    constexpr int kF = HD / 32;  // features of a lane
-    __shared__ float sq[4][HD];
+__global__ void __launch_bounds__(kThreads, 2)
+    k_serve_attn(const __grid_constant__ Maps maps, const __grid_constant__ ServeShape s,
+                 const __grid_constant__ dllm_serve_tables t, const __grid_constant__ ServeAttnArgs a) {
+    constexpr int NB = kStages<HD>, kParts = HD / 64;
+    constexpr int kQ = kParts * kHalfQ, kKV = kParts * kHalfKV;
     ServeArrays w;
     serve_arrays(s, t.work, &w);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long wid = static_cast<long long>(blockIdx.x) * 4 + warp;
-    const int row = static_cast<int>(wid / s.H), h = static_cast<int>(wid % s.H), hk = h / s.G;
-    if (row >= a.rows) return;
-    T* out = static_cast<T*>(a.out) + (static_cast<size_t>(row) * s.H + h) * HD;
-    const T* q = static_cast<const T*>(a.q) + row * a.ldq + h * HD;
-    for (int i = lane; i < HD; i += 32) sq[warp][i] = static_cast<float>(q[i]) * a.scale;
-    __syncwarp();
-    const int req = row < w.head->rows ? t.req[row] : -1;
-    float m = -INFINITY, l = 0.0f, o[kF] = {};
-    const T* kc = static_cast<const T*>(a.kc);
-    const T* vc = static_cast<const T*>(a.vc);
-    auto span = [&](const int* pages, int n_list, int n) {
-        for (int k0 = 0; k0 < n; k0 += 32) {
-            const int k = k0 + lane;
-            long long at = -1;
-            float z = -INFINITY;
-            if (k < n) {
-                const int idx = k >> s.page_log2, p = idx < n_list ? pages[idx] : -1;
-                z = 0.0f;
-                if (p >= 0 && p < s.n_pages) {
-                    at = p * s.page_stride + (static_cast<long long>(hk) * s.page + (k & (s.page - 1))) * HD;
-                    for (int c = 0; c < HD; c += 8) {
-                        const uint4 u = *reinterpret_cast<const uint4*>(kc + at + c);
-                        const uint32_t x[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float2 f = Half2<T>::unpack(x[i]);
-                            z += f.x * sq[warp][c + 2 * i] + f.y * sq[warp][c + 2 * i + 1];
-                        }
+    const int cta = blockIdx.x;
+    if (cta >= w.head->ctas) return;
+    if (!serve_same_shape(s, *w.head)) {  // a plan of another config
+        if (threadIdx.x == 0) atomicOr(t.status, DLLM_SERVE_STATE);
+        return;
+    }
+
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t *sQ = smem, *sK = sQ + kQ, *sV = sK + NB * kKV;
+    __shared__ uint64_t qfull, qempty, drain, kfull[NB], vfull[NB], kempty[NB], vempty[NB], sfull[2], pfull[2], pvdone[2];
+    __shared__ uint32_t tslot;
+    __shared__ int s_abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int prefix_blocks = w.head->prefix_blocks, prefix_len = w.head->prefix_len;
+
+    if (threadIdx.x == 0) {
+        mbar_init(&qfull, 1);
+        mbar_init(&qempty, 1);
+        mbar_init(&drain, 1);
+        for (int i = 0; i < NB; ++i) {
+            mbar_init(&kfull[i], 1);
+            mbar_init(&vfull[i], 1);
+            mbar_init(&kempty[i], 1);
+            mbar_init(&vempty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sfull[i], 1);
+            mbar_init(&pfull[i], 128);
+            mbar_init(&pvdone[i], 1);
+        }
+        s_abort = 0;
+        mbar_fence_init();
+    }
+    if (warp == 4) {
+        tmem_alloc(&tslot, 256);  // O: columns 0 .. HD - 1; S and P: 128 .. 191, 192 .. 255
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tslot;
+    pdl_launch_dependents();
+
+    // The load and MMA warps run their loops whole, the outcomes of their waits voted, and one elected lane
+    // issues.  Barrier phases count the steps j of the whole run, across its segments.
+    auto wait_all = [&](uint64_t* bar, uint32_t parity) {
+        return __all_sync(0xffffffffu, mbar_wait(bar, parity, &s_abort, t.status)) != 0;
+    };
+    Walk at(w, s.Hkv, cta);
+    if (warp == 4) {
+        // ------------------------------------------------ loads
+        const bool leader = elect_one();
+        if (leader) {
+            tma_prefetch_desc(&maps.q);
+            tma_prefetch_desc(&maps.k);
+            tma_prefetch_desc(&maps.v);
+        }
+        const uint64_t once = policy_evict_first();
+        uint64_t often;
+        asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(often));
+        const int lg = s.page_log2, page = s.page;
+        const int n_prefix = min(a.n_prefix, (prefix_len + page - 1) >> lg);
+        if (static_cast<long long>(a.n_prefix) * page < prefix_len && cta == 0 && leader) atomicOr(t.status, DLLM_SERVE_PREFIX);
+        const uint32_t q_bytes = static_cast<uint32_t>(kParts * 128 * s.G * s.tile_tokens);
+        // pages of a segment's step (-1: none, the copy fills in zeros): up to four, or one and the place in it
+        auto pages_of = [&](int step) {
+            int4 p = make_int4(-1, -1, -1, -1);
+            if (step < prefix_blocks) {
+                const int i = step * kServeBlock >> lg;
+                if (page >= kServeBlock) {
+                    if (i < n_prefix) p.x = __ldg(a.prefix_pages + i);
+                    p.y = step * kServeBlock & (page - 1);
+                } else {
+                    if (i < n_prefix) p.x = __ldg(a.prefix_pages + i);
+                    if (i + 1 < n_prefix) p.y = __ldg(a.prefix_pages + i + 1);
+                    if (page == 16) {
+                        if (i + 2 < n_prefix) p.z = __ldg(a.prefix_pages + i + 2);
+                        if (i + 3 < n_prefix) p.w = __ldg(a.prefix_pages + i + 3);
                     }
                 }
+            } else if (at.own0 >= 0) {
+                p = __ldg(w.pages + at.own0 + step - prefix_blocks);
+            } else {
+                p.y = 0;
             }
-            float mx = z;
+            return p;
+        };
+        int j = 0, seg = 0, kiss = 0, viss = 0, qiss = 0;
+        bool ok = true;
+        do {
+            if (at.left <= 0) break;
+            if (seg > 0 && !wait_all(&qempty, static_cast<uint32_t>((seg - 1) & 1))) break;
+            if (leader) {
+                mbar_arrive_expect_tx(&qfull, q_bytes);
 #pragma unroll
-            for (int d = 16; d; d /= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-            mx = fmaxf(mx, m);
-            const float ref = mx == -INFINITY ? 0.0f : mx, al = expf(m - ref), p = expf(z - ref);
-            float sum = p;
+                for (int p = 0; p < kParts; ++p)
+                    tma_4d(sQ + p * kHalfQ, &maps.q, 64 * p, 0, at.hk, at.tile * s.tile_tokens, &qfull, once);
+            }
+            qiss = ++seg;
+            int4 cur, nxt = make_int4(-1, 0, -1, -1);
+            if (lane < at.n) nxt = pages_of(at.step + lane);
+            for (int i = 0; i < at.n && ok; ++i, ++j) {
+                if ((i & 31) == 0) {
+                    cur = nxt;
+                    if (i + 32 + lane < at.n) nxt = pages_of(at.step + i + 32 + lane);
+                }
+                int p[4] = {__shfl_sync(0xffffffffu, cur.x, i & 31), __shfl_sync(0xffffffffu, cur.y, i & 31), 0, 0};
+                if (page == 16) {
+                    p[2] = __shfl_sync(0xffffffffu, cur.z, i & 31);
+                    p[3] = __shfl_sync(0xffffffffu, cur.w, i & 31);
+                }
+                const int st = j % NB;
+                const uint32_t par = static_cast<uint32_t>((j / NB - 1) & 1);
+                const uint64_t pol = at.step + i < prefix_blocks ? often : once;
+                auto load = [&](uint8_t* dst, const CUtensorMap* tm, uint64_t* bar) {
+                    mbar_arrive_expect_tx(bar, kKV);
 #pragma unroll
-            for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-            l = l * al + sum;
-            m = mx;
+                    for (int h = 0; h < kParts; ++h) {
+                        if (page >= kServeBlock) {
+                            tma_3d(dst + h * kHalfKV, tm, 64 * h, at.hk * page + p[1], p[0], bar, pol);
+                        } else {
 #pragma unroll
-            for (int i = 0; i < kF; ++i) o[i] *= al;
-            for (int j = 0; j < min(32, n - k0); ++j) {
-                const long long aj = __shfl_sync(0xffffffffu, at, j);
-                const float pj = __shfl_sync(0xffffffffu, p, j);
-                if (aj < 0) continue;
+                            for (int k = 0; k < 4; ++k)
+                                if (k < kServeBlock >> lg)
+                                    tma_3d(dst + h * kHalfKV + k * page * 128, tm, 64 * h, at.hk * page, p[k], bar, pol);
+                        }
+                    }
+                };
+                if (j >= NB && !wait_all(&kempty[st], par)) {
+                    ok = false;
+                    break;
+                }
+                if (leader) load(sK + st * kKV, &maps.k, &kfull[st]);
+                kiss = j + 1;
+                if (j >= NB && !wait_all(&vempty[st], par)) {
+                    ok = false;
+                    break;
+                }
+                if (leader) load(sV + st * kKV, &maps.v, &vfull[st]);
+                viss = j + 1;
+            }
+        } while (ok && at.advance());
+        if (leader && *const_cast<volatile int*>(&s_abort)) {
+            // the copies in flight land before the shared memory is released (one deadline for all)
+            const long long t0 = spin_clock();
+            auto land = [&](uint64_t* bar, int phase) {
+                while (!mbar_try_wait(bar, static_cast<uint32_t>(phase & 1)) && spin_clock() - t0 < kWaitLimitCycles) {
+                }
+            };
+            if (qiss) land(&qfull, qiss - 1);
+            for (int k = max(0, kiss - NB); k < kiss; ++k) land(&kfull[k % NB], k / NB);
+            for (int k = max(0, viss - NB); k < viss; ++k) land(&vfull[k % NB], k / NB);
+        }
+    } else if (warp == 5) {
+        // ------------------------------------------------ MMA issue
+        const bool leader = elect_one();
+        const uint32_t t_o = __shfl_sync(0xffffffffu, tmem, 0), t_s = t_o + 128;
+        constexpr uint32_t kType = std::is_same<T, __half>::value ? 0u : (1u << 7) | (1u << 10);
+        constexpr uint32_t kShape = (1u << 4) | kType | (static_cast<uint32_t>(kServeRows >> 4) << 24);
+        constexpr uint32_t id_s = kShape | (static_cast<uint32_t>(kServeBlock >> 3) << 17);
+        constexpr uint32_t id_o = kShape | (static_cast<uint32_t>(HD >> 3) << 17) | (1u << 16);  // V is MN-major
+        const uint64_t qd = sw128(smem_u32(sQ), 16, 1024), kd = sw128(smem_u32(sK), 16, 1024);
+        const uint64_t vd = sw128(smem_u32(sV), kHalfKV, 1024);
+        auto issue_s = [&](int j, bool last) {
+            const int st = j % NB, sb = j % 2;
+            if (!wait_all(&kfull[st], static_cast<uint32_t>((j / NB) & 1))) return false;
+            // S_j goes where P_{j-2} was: its P V must be done
+            if (j >= 2 && !wait_all(&pvdone[sb], static_cast<uint32_t>(((j - 2) / 2) & 1))) return false;
+            tc_fence_after();
+            if (leader) {
+                const uint64_t kds = kd + static_cast<uint64_t>(st * (kKV >> 4));
 #pragma unroll
-                for (int i = 0; i < kF; ++i) o[i] += pj * static_cast<float>(vc[aj + lane * kF + i]);
+                for (int k = 0; k < HD / 16; ++k)
+                    umma_bf16(t_s + static_cast<uint32_t>(sb * 64),
+                              qd + static_cast<uint64_t>(((k >> 2) * kHalfQ + (k & 3) * 32) >> 4),
+                              kds + static_cast<uint64_t>(((k >> 2) * kHalfKV + (k & 3) * 32) >> 4), id_s, k > 0 ? 1u : 0u);
+                umma_commit(&sfull[sb]);
+                umma_commit(&kempty[st]);
+                if (last) umma_commit(&qempty);  // the segment's last use of Q
+            }
+            __syncwarp();
+            return true;
+        };
+        int j = 0, seg = 0;
+        bool ok = true;
+        do {
+            if (at.left <= 0) break;
+            ok = wait_all(&qfull, static_cast<uint32_t>(seg++ & 1)) && issue_s(j, at.n == 1);
+            // first and last + 1 live lane of a step
+            const int tok0 = at.tile * s.tile_tokens;
+            auto live_of = [&](int step) {
+                int2 r = make_int2(0, kServeRows);
+                if (step >= prefix_blocks && at.own0 >= 0) {
+                    const int4 f = __ldg(w.info + at.own0 + step - prefix_blocks);
+                    r.x = max(f.x - tok0, 0) * s.G;
+                    r.y = min(f.y - tok0, s.tile_tokens) * s.G;
+                }
+                return r;
+            };
+            int2 cur, nxt = make_int2(0, 0);
+            if (lane < at.n) nxt = live_of(at.step + lane);
+            for (int i = 0; i < at.n && ok; ++i, ++j) {
+                if ((i & 31) == 0) {
+                    cur = nxt;
+                    if (i + 32 + lane < at.n) nxt = live_of(at.step + i + 32 + lane);
+                }
+                const int lo = __shfl_sync(0xffffffffu, cur.x, i & 31), hi = __shfl_sync(0xffffffffu, cur.y, i & 31);
+                if (i + 1 < at.n && !issue_s(j + 1, i + 2 == at.n)) {
+                    ok = false;
+                    break;
+                }
+                const int st = j % NB, sb = j % 2;
+                ok = wait_all(&vfull[st], static_cast<uint32_t>((j / NB) & 1)) &&
+                     wait_all(&pfull[sb], static_cast<uint32_t>((j / 2) & 1));
+                if (!ok) break;
+                tc_fence_after();
+                if (leader) {
+                    const uint64_t vds = vd + static_cast<uint64_t>(st * (kKV >> 4));
+                    const uint4 off = make_uint4(~bit_run(lo, hi), ~bit_run(lo - 32, hi - 32), ~bit_run(lo - 64, hi - 64),
+                                                 ~bit_run(lo - 96, hi - 96));
+#pragma unroll
+                    for (int k = 0; k < kServeBlock / 16; ++k)
+                        umma_tmem_a_masked(t_o, t_s + static_cast<uint32_t>(sb * 64 + k * 8),
+                                           vds + static_cast<uint64_t>((k * 2048) >> 4), id_o, off);
+                    umma_commit(&pvdone[sb]);
+                    umma_commit(&vempty[st]);
+                }
+                __syncwarp();
+            }
+        } while (ok && at.advance());
+        // every MMA is done before the CTA gives back tensor memory and shared memory
+        if (leader) {
+            umma_commit(&drain);
+            const long long t0 = spin_clock();
+            while (!mbar_try_wait(&drain, 0) && spin_clock() - t0 < kWaitLimitCycles) {
             }
         }
-    };
-    if (req >= 0) {
-        span(a.prefix_pages, a.n_prefix, w.head->prefix_len);
-        const int q_len = t.row_start[req + 1] - t.row_start[req];
-        int n = t.n_keys[req];
-        if (n > 0 && w.head->causal) n += row - t.row_start[req] + 1 - q_len;
-        span(t.table + static_cast<size_t>(req) * s.max_pages, s.max_pages, n);
-    }
-    const float il = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+        __syncwarp();
+    } else {
+        // ------------------------------------------------ softmax, output
+        const int r = threadIdx.x;  // row of the tile = lane of tensor memory
+        const int tok_off = r / s.G, g = r - tok_off * s.G;
+        const uint32_t lane_off = static_cast<uint32_t>(warp * 32) << 16;
+        const uint32_t t_o = tmem + lane_off, t_s = tmem + 128 + lane_off;
+        const float sl2 = a.scale * 1.4426950408889634f;
+        const int rows = min(w.head->rows, a.rows), causal = w.head->causal;
+        auto wait = [&](uint64_t* bar, uint32_t parity) {
+            return __all_sync(0xffffffffu, mbar_wait(bar, parity, &s_abort, t.status)) != 0;
+        };
+        int j = 0;
+        bool ok = true;
+        do {
+            if (at.left <= 0) break;
+            const int tok = at.tile * s.tile_tokens + tok_off;
+            const bool there = tok_off < s.tile_tokens && tok < rows;
+            float m = -INFINITY, l = 0.0f;
+            {
+                uint32_t zero[32];
 #pragma unroll
-    for (int i = 0; i < kF; i += 2)
-        *reinterpret_cast<uint32_t*>(out + lane * kF + i) = Half2<T>::pack(o[i] * il, o[i + 1] * il);
-    if (a.lse && lane == 0) a.lse[static_cast<size_t>(row) * s.H + h] = m + logf(l);
+                for (int i = 0; i < 32; ++i) zero[i] = 0u;
+#pragma unroll
+                for (int c = 0; c < HD; c += 32) tmem_st_32u(t_o + static_cast<uint32_t>(c), zero);
+            }
+            int4 f = make_int4(0, 0, 0, 0), fn = f;
+            auto info_of = [&](int step) {
+                return step >= prefix_blocks && at.own0 >= 0 ? __ldg(w.info + at.own0 + step - prefix_blocks) : make_int4(0, 0, 0, 0);
+            };
+            fn = info_of(at.step);
+            for (int i = 0; i < at.n; ++i, ++j) {
+                const int step = at.step + i, sb = j % 2;
+                f = fn;
+                if (i + 1 < at.n) fn = info_of(step + 1);
+                // keys of the block that there are, and that this row sees
+                int valid, seen;
+                bool live = there;
+                if (step < prefix_blocks) {
+                    valid = min(kServeBlock, prefix_len - step * kServeBlock);
+                    seen = there ? valid : 0;
+                } else {
+                    valid = min(kServeBlock, f.w + f.y - f.x - f.z);
+                    live = there && tok >= f.x && tok < f.y;
+                    seen = !live ? 0 : causal ? min(valid, f.w + tok - f.x + 1 - f.z) : valid;
+                }
+                ok = wait(&sfull[sb], static_cast<uint32_t>((j / 2) & 1));
+                if (!ok) break;
+                if (__any_sync(0xffffffffu, seen > 0)) {
+                    tc_fence_after();
+                    const uint32_t ts = t_s + static_cast<uint32_t>(sb * 64);
+                    float v[64];
+                    tmem_ld_32x64(ts, v);
+                    if (__any_sync(0xffffffffu, seen < kServeBlock)) {
+#pragma unroll
+                        for (int k = 0; k < 64; ++k)
+                            if (k >= seen) v[k] = -INFINITY;
+                    }
+                    float mx;
+                    {
+                        float mi[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+                        for (int k = 4; k < 64; k += 8) {
+#pragma unroll
+                            for (int u = 0; u < 4; ++u)
+                                mi[u] = k + 4 < 64 ? fmaxf(fmaxf(mi[u], v[k + u]), v[k + 4 + u]) : fmaxf(mi[u], v[k + u]);
+                        }
+                        mx = fmaxf(fmaxf(mi[0], mi[1]), fmaxf(mi[2], mi[3])) * sl2;
+                    }
+                    const bool up = mx > m + 8.0f;  // (m = -inf: the row's first keys)
+                    if (__any_sync(0xffffffffu, up && m != -INFINITY)) {
+                        ok = wait(&pvdone[(j - 1) % 2], static_cast<uint32_t>(((j - 1) / 2) & 1));
+                        if (!ok) break;
+                        tc_fence_after();
+                        const float al = up && m != -INFINITY ? ex2(m - mx) : 1.0f;
+                        float o[32];
+#pragma unroll 1
+                        for (int c = 0; c < HD; c += 32) {
+                            tmem_ld_32x32(t_o + static_cast<uint32_t>(c), o);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) o[k] *= al;
+                            tmem_st_32x32(t_o + static_cast<uint32_t>(c), o);
+                        }
+                        l *= al;
+                    }
+                    if (up) m = mx;
+                    const float ref = m == -INFINITY ? 0.0f : -m;
+                    uint32_t pk[32];
+                    float2 ls[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+                    const float2 sl = make_float2(sl2, sl2), nm = make_float2(ref, ref);
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        float2 e = fma2(make_float2(v[2 * k], v[2 * k + 1]), sl, nm);
+                        e.x = ex2(e.x);
+                        e.y = ex2(e.y);
+                        ls[k & 1] = add2(ls[k & 1], e);
+                        pk[k] = Half2<T>::pack(e.x, e.y);
+                    }
+                    l += (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
+                    tmem_st_32u(ts, pk);
+                } else if (__any_sync(0xffffffffu, live)) {
+                    // rows of the block's request, all before its keys: nothing, but their lanes do take part
+                    uint32_t zero[32];
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) zero[k] = 0u;
+                    tc_fence_after();
+                    tmem_st_32u(t_s + static_cast<uint32_t>(sb * 64), zero);
+                }
+                if (valid < kServeBlock) {
+                    // the values of keys that are not there
+                    const int st = j % NB;
+                    ok = wait(&vfull[st], static_cast<uint32_t>((j / NB) & 1));
+                    if (!ok) break;
+                    uint4* v4 = reinterpret_cast<uint4*>(sV + st * kKV);
+                    for (int k = max(valid, 0) * 8 + r; k < kServeBlock * 8; k += 128) {
+#pragma unroll
+                        for (int h = 0; h < kParts; ++h) v4[h * (kHalfKV / 16) + k] = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async_smem();
+                }
+                tc_fence_before();
+                mbar_arrive(&pfull[sb]);
+            }
+            if (!ok) break;
+            // O after the segment's last P V
+            ok = wait(&pvdone[(j - 1) % 2], static_cast<uint32_t>(((j - 1) / 2) & 1));
+            if (!ok) break;
+            tc_fence_after();
+            const bool whole = at.whole();
+            const float il = l != 0.0f ? 1.0f / l : 0.0f;
+            const size_t row_head = static_cast<size_t>(tok) * s.H + at.hk * s.G + g;
+            T* op = static_cast<T*>(a.out) + row_head * HD;
+            const size_t slot = 2 * static_cast<size_t>(cta) + (at.step == 0 ? 1 : 0);  // an end of the run: its first or last unit
+            float* pp = t.partials + (slot * kServeRows + r) * HD;
+#pragma unroll 1
+            for (int c = 0; c < HD; c += 32) {
+                float o[32];
+                tmem_ld_32x32(t_o + static_cast<uint32_t>(c), o);
+                if (whole && there) {
+                    uint4* dst = reinterpret_cast<uint4*>(op + c);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        uint4 x;
+                        x.x = Half2<T>::pack(o[8 * k] * il, o[8 * k + 1] * il);
+                        x.y = Half2<T>::pack(o[8 * k + 2] * il, o[8 * k + 3] * il);
+                        x.z = Half2<T>::pack(o[8 * k + 4] * il, o[8 * k + 5] * il);
+                        x.w = Half2<T>::pack(o[8 * k + 6] * il, o[8 * k + 7] * il);
+                        dst[k] = x;
+                    }
+                } else if (!whole && l != 0.0f) {
+                    float4* dst = reinterpret_cast<float4*>(pp + c);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) dst[k] = make_float4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                }
+            }
+            if (whole) {
+                if (there && a.lse) a.lse[row_head] = (m + log2f(l)) * kLn2;
+            } else {
+                float2* ml = reinterpret_cast<float2*>(t.partials + static_cast<size_t>(2 * kServeCtas) * kServeRows * HD);
+                ml[slot * kServeRows + r] = make_float2(m, l);
+            }
+            tc_fence_before();
+        } while (at.advance());
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 4) tmem_dealloc(tmem, 256);
+}
+
+// Joins the parts of units that several CTAs share, in the order of their keys: a warp a (row, query head).
+// Rows that are padding get zeros.
+template <int HD, typename T>
+__global__ void __launch_bounds__(256) k_serve_join(const __grid_constant__ ServeShape s,
+                                                    const __grid_constant__ dllm_serve_tables t,
+                                                    const __grid_constant__ ServeAttnArgs a) {
+    constexpr int kF = HD / 32;
+    ServeArrays w;
+    serve_arrays(s, t.work, &w);
+    const int lane = threadIdx.x & 31;
+    const long long id = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+    const int n = static_cast<int>(id / s.H), h = static_cast<int>(id - static_cast<long long>(n) * s.H);
+    if (n >= a.rows) {
+        pdl_wait();
+        return;
+    }
+    T* out = static_cast<T*>(a.out) + static_cast<size_t>(id) * HD + lane * kF;
+    float acc[kF] = {}, M = -INFINITY, L = 0.0f;
+    if (n < w.head->rows && serve_same_shape(s, *w.head)) {
+        const int tile = n / s.tile_tokens, hk = h / s.G, ctas = w.head->ctas;
+        const long long total = w.head->total, c0 = w.tile_cum[tile], steps = w.tile_cum[tile + 1] - c0;
+        const long long x0 = c0 * s.Hkv + hk * steps, x1 = x0 + steps;
+        // the CTA that holds step x: the last whose run begins at or before it
+        const int first = static_cast<int>(((x0 + 1) * ctas - 1) / total), last = static_cast<int>((x1 * ctas - 1) / total);
+        pdl_wait();
+        if (first == last) return;  // written by its CTA
+        const int r = (n - tile * s.tile_tokens) * s.G + h - hk * s.G;
+        const float2* ml = reinterpret_cast<const float2*>(t.partials + static_cast<size_t>(2 * kServeCtas) * kServeRows * HD);
+        auto slot = [&](int c) { return 2 * static_cast<size_t>(c) + (c == first ? 1 : 0); };
+        for (int b = first; b <= last; b += 32) {
+            float2 x = make_float2(-INFINITY, 0.0f);
+            if (b + lane <= last) x = ml[slot(b + lane) * kServeRows + r];
+            float mb = x.x;
+#pragma unroll
+            for (int d = 16; d; d /= 2) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, d));
+            mb = fmaxf(mb, M);
+            const float ref = mb == -INFINITY ? 0.0f : mb;
+            const float al = M == -INFINITY ? 0.0f : exp2f(M - ref), wt = x.y == 0.0f ? 0.0f : exp2f(x.x - ref);
+            float lb = wt * x.y;
+#pragma unroll
+            for (int d = 16; d; d /= 2) lb += __shfl_xor_sync(0xffffffffu, lb, d);
+            L = L * al + lb;
+            M = mb;
+#pragma unroll
+            for (int i = 0; i < kF; ++i) acc[i] *= al;
+            uint32_t some = __ballot_sync(0xffffffffu, x.y != 0.0f);
+            while (some) {
+                const int k = __ffs(some) - 1;
+                some &= some - 1;
+                const float wk = __shfl_sync(0xffffffffu, wt, k);
+                const float* p = t.partials + (slot(b + k) * kServeRows + r) * HD + lane * kF;
+                if constexpr (kF == 4) {
+                    const float4 v = *reinterpret_cast<const float4*>(p);
+                    acc[0] += wk * v.x;
+                    acc[1] += wk * v.y;
+                    acc[2] += wk * v.z;
+                    acc[3] += wk * v.w;
+                } else {
+                    const float2 v = *reinterpret_cast<const float2*>(p);
+                    acc[0] += wk * v.x;
+                    acc[1] += wk * v.y;
+                }
+            }
+        }
+    } else {
+        pdl_wait();
+    }
+    const float il = L != 0.0f ? 1.0f / L : 0.0f;
+    if constexpr (kF == 4) {
+        uint2 x;
+        x.x = Half2<T>::pack(acc[0] * il, acc[1] * il);
+        x.y = Half2<T>::pack(acc[2] * il, acc[3] * il);
+        *reinterpret_cast<uint2*>(out) = x;
+    } else {
+        *reinterpret_cast<uint32_t*>(out) = Half2<T>::pack(acc[0] * il, acc[1] * il);
+    }
+    if (a.lse && lane == 0) a.lse[id] = (M + log2f(L)) * kLn2;
 }
 
 template <int HD, typename T>
-cudaError_t go(const ServeShape& s, const dllm_serve_tables& t, const ServeAttnArgs& a, cudaStream_t st) {
-    const long long ctas = (static_cast<long long>(a.rows) * s.H + 3) / 4;
-    k_serve_attn<HD, T><<<static_cast<unsigned>(ctas), 128, 0, st>>>(s, t, a);
-    return cudaGetLastError();
+cudaError_t go(const ServeShape& s, const dllm_serve_tables& t, const ServeAttnArgs& a, int sms, cudaStream_t st) {
+    constexpr bool f16 = std::is_same<T, __half>::value;
+    Maps maps;
+    const uint64_t e = 2, page_rows = static_cast<uint64_t>(s.Hkv) * s.page;
+    const uint64_t qdims[4] = {HD, static_cast<uint64_t>(s.G), static_cast<uint64_t>(s.Hkv), static_cast<uint64_t>(a.rows)};
+    const uint64_t qstr[3] = {HD * e, s.G * HD * e, a.ldq * e};
+    const uint32_t qbox[4] = {64, static_cast<uint32_t>(s.G), 1, static_cast<uint32_t>(s.tile_tokens)};
+    const uint64_t kdims[3] = {HD, page_rows, static_cast<uint64_t>(s.n_pages)};
+    const uint64_t kstr[2] = {HD * e, s.page_stride * e};
+    const uint32_t kbox[3] = {64, static_cast<uint32_t>(s.page < kServeBlock ? s.page : kServeBlock), 1};
+    if (!make_tmap_16bit(&maps.q, a.q, f16, 4, qdims, qstr, qbox) || !make_tmap_16bit(&maps.k, a.kc, f16, 3, kdims, kstr, kbox) ||
+        !make_tmap_16bit(&maps.v, a.vc, f16, 3, kdims, kstr, kbox))
+        return cudaErrorInvalidValue;
+    cudaError_t err = cudaFuncSetAttribute(reinterpret_cast<const void*>(k_serve_attn<HD, T>),
+                                           cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<HD>);
+    if (err != cudaSuccess) return err;
+    const int ctas = 2 * sms < kServeCtas ? 2 * sms : kServeCtas;
+    k_serve_attn<HD, T><<<ctas, kThreads, kSmem<HD>, st>>>(maps, s, t, a);
+    err = cudaGetLastError();
+    if (err != cudaSuccess) return err;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>((static_cast<long long>(a.rows) * s.H + 7) / 8));
+    cfg.blockDim = dim3(256);
+    cfg.stream = st;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, k_serve_join<HD, T>, s, t, a);
 }
 
 }  // namespace
 
 size_t serve_partial_bytes(const ServeShape& s) {
-    return 0;
+    return static_cast<size_t>(2 * kServeCtas) * kServeRows * (s.hd * sizeof(float) + sizeof(float2));
 }
 
 cudaError_t launch_serve_attention(const ServeShape& s, const dllm_serve_tables& t, const ServeAttnArgs& a, int sms,
                                    cudaStream_t st) {
-    (void)sms;
     if (s.dtype == DLLM_BF16)
-        return s.hd == 128 ? go<128, __nv_bfloat16>(s, t, a, st) : go<64, __nv_bfloat16>(s, t, a, st);
-    return s.hd == 128 ? go<128, __half>(s, t, a, st) : go<64, __half>(s, t, a, st);
+        return s.hd == 128 ? go<128, __nv_bfloat16>(s, t, a, sms, st) : go<64, __nv_bfloat16>(s, t, a, sms, st);
+    return s.hd == 128 ? go<128, __half>(s, t, a, sms, st) : go<64, __half>(s, t, a, sms, st);
 }
 
 }  // namespace dllm

@@ -233,6 +233,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
             w.head->tiles = tiles;
             w.head->rows = rows;
             w.head->total = total;
+            serve_key(a.s, w.head->shape);
             t.status[1] = s_refused;
             t.status[2] = taken;
             t.status[3] = given;
