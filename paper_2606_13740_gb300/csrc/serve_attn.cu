@@ -14,8 +14,10 @@
 //   O  += P_j V_j         tcgen05.mma, P_j from tensor memory, V_j in shared memory (MN-major)
 // The running maximum m moves only when a block's maximum exceeds it by more than 8 (log2 units); only then
 // are O and the row's sum rescaled, so P stays below 2^8.  P is rounded to the cache's type, as the tensor
-// cores take it; the sum is of the unrounded values.  Warps 0-3: softmax and output (a thread a row); warp 4:
-// TMA loads, a box a page and 64 features; warp 5: MMA issue.
+// cores take it; the sum is of the unrounded values.  Warps 0-3: softmax and output (a thread a row); warps 4
+// and 7: TMA loads of Q and K, and of V, a box a page and 64 features; warps 5 and 6: the MMAs of S and of
+// P V.  (With one warp for the loads and one for the MMAs each spent 2000 cycles a step on them, twice what
+// the tensor cores and the softmax take.)
 // Keys past a request's end score -inf, and their values, which may be anything, are set to 0 in shared memory.
 #include "serve.cuh"
 
@@ -23,7 +25,7 @@ namespace dllm {
 
 namespace {
 
-constexpr int kThreads = 192;
+constexpr int kThreads = 256;
 constexpr int kHalfQ = kServeRows * 128;    // bytes of 64 features of the Q tile
 constexpr int kHalfKV = kServeBlock * 128;  // and of a K or V block
 constexpr float kLn2 = 0.6931471805599453f;
@@ -169,7 +171,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *sQ = smem, *sK = sQ + kQ, *sV = sK + NB * kKV;
-    __shared__ uint64_t qfull, qempty, drain, kfull[NB], vfull[NB], kempty[NB], vempty[NB], sfull[2], pfull[2], pvdone[2];
+    __shared__ uint64_t qfull, qempty, drain[2], kfull[NB], vfull[NB], kempty[NB], vempty[NB], sfull[2], pfull[2], pvdone[2];
     __shared__ uint32_t tslot;
     __shared__ int s_abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -178,7 +180,8 @@ __global__ void __launch_bounds__(kThreads, 2)
     if (threadIdx.x == 0) {
         mbar_init(&qfull, 1);
         mbar_init(&qempty, 1);
-        mbar_init(&drain, 1);
+        mbar_init(&drain[0], 1);
+        mbar_init(&drain[1], 1);
         for (int i = 0; i < NB; ++i) {
             mbar_init(&kfull[i], 1);
             mbar_init(&vfull[i], 1);
@@ -197,6 +200,12 @@ __global__ void __launch_bounds__(kThreads, 2)
         tmem_alloc(&tslot, 256);  // O: columns 0 .. HD - 1; S and P: 128 .. 191, 192 .. 255
         tmem_relinquish();
     }
+    // rows past the tile's tokens (groups that do not divide 128) stay zero: ordinary scores, never read
+    for (int i = s.G * s.tile_tokens * 8 + static_cast<int>(threadIdx.x); i < kServeRows * 8; i += kThreads) {
+#pragma unroll
+        for (int h = 0; h < kParts; ++h) reinterpret_cast<uint4*>(sQ + h * kHalfQ)[i] = make_uint4(0, 0, 0, 0);
+    }
+    fence_proxy_async_smem();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -209,33 +218,32 @@ __global__ void __launch_bounds__(kThreads, 2)
         return __all_sync(0xffffffffu, mbar_wait(bar, parity, &s_abort, t.status)) != 0;
     };
     Walk at(w, s.Hkv, cta);
-    if (warp == 4) {
+    if (warp == 4 || warp == 7) {
         // ------------------------------------------------ loads
-        const bool leader = elect_one();
+        const bool leader = elect_one(), is_k = warp == 4;
+        const CUtensorMap* tm = is_k ? &maps.k : &maps.v;
         if (leader) {
-            tma_prefetch_desc(&maps.q);
-            tma_prefetch_desc(&maps.k);
-            tma_prefetch_desc(&maps.v);
+            if (is_k) tma_prefetch_desc(&maps.q);
+            tma_prefetch_desc(tm);
         }
-        const uint64_t once = policy_evict_first();
-        uint64_t often;
-        asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(often));
-        const int lg = s.page_log2, page = s.page;
+        const uint64_t once = policy_evict_first(), often = policy_evict_last();
+        const int lg = s.page_log2, page = s.page, boxes = page < kServeBlock ? kServeBlock >> lg : 1;
         const int n_prefix = min(a.n_prefix, (prefix_len + page - 1) >> lg);
-        if (static_cast<long long>(a.n_prefix) * page < prefix_len && cta == 0 && leader) atomicOr(t.status, DLLM_SERVE_PREFIX);
-        const uint32_t q_bytes = static_cast<uint32_t>(kParts * 128 * s.G * s.tile_tokens);
+        if (static_cast<long long>(a.n_prefix) * page < prefix_len && cta == 0 && is_k && leader)
+            atomicOr(t.status, DLLM_SERVE_PREFIX);
+        uint8_t* ring = is_k ? sK : sV;
+        uint64_t *full = is_k ? kfull : vfull, *empty = is_k ? kempty : vempty;
         // pages of a segment's step (-1: none, the copy fills in zeros): up to four, or one and the place in it
         auto pages_of = [&](int step) {
             int4 p = make_int4(-1, -1, -1, -1);
             if (step < prefix_blocks) {
                 const int i = step * kServeBlock >> lg;
+                if (i < n_prefix) p.x = __ldg(a.prefix_pages + i);
                 if (page >= kServeBlock) {
-                    if (i < n_prefix) p.x = __ldg(a.prefix_pages + i);
                     p.y = step * kServeBlock & (page - 1);
                 } else {
-                    if (i < n_prefix) p.x = __ldg(a.prefix_pages + i);
                     if (i + 1 < n_prefix) p.y = __ldg(a.prefix_pages + i + 1);
-                    if (page == 16) {
+                    if (boxes == 4) {
                         if (i + 2 < n_prefix) p.z = __ldg(a.prefix_pages + i + 2);
                         if (i + 3 < n_prefix) p.w = __ldg(a.prefix_pages + i + 3);
                     }
@@ -247,59 +255,55 @@ __global__ void __launch_bounds__(kThreads, 2)
             }
             return p;
         };
-        int j = 0, seg = 0, kiss = 0, viss = 0, qiss = 0;
+        int j = 0, seg = 0;
         bool ok = true;
         do {
             if (at.left <= 0) break;
-            if (seg > 0 && !wait_all(&qempty, static_cast<uint32_t>((seg - 1) & 1))) break;
-            if (leader) {
-                mbar_arrive_expect_tx(&qfull, q_bytes);
+            if (is_k) {
+                if (seg > 0 && !wait_all(&qempty, static_cast<uint32_t>((seg - 1) & 1))) break;
+                if (leader) {
+                    mbar_arrive_expect_tx(&qfull, static_cast<uint32_t>(kParts * 128 * s.G * s.tile_tokens));
 #pragma unroll
-                for (int p = 0; p < kParts; ++p)
-                    tma_4d(sQ + p * kHalfQ, &maps.q, 64 * p, 0, at.hk, at.tile * s.tile_tokens, &qfull, once);
+                    for (int p = 0; p < kParts; ++p)
+                        tma_4d(sQ + p * kHalfQ, &maps.q, 64 * p, 0, at.hk, at.tile * s.tile_tokens, &qfull, once);
+                }
+                ++seg;
             }
-            qiss = ++seg;
             int4 cur, nxt = make_int4(-1, 0, -1, -1);
             if (lane < at.n) nxt = pages_of(at.step + lane);
-            for (int i = 0; i < at.n && ok; ++i, ++j) {
+            for (int i = 0; i < at.n; ++i) {
                 if ((i & 31) == 0) {
                     cur = nxt;
                     if (i + 32 + lane < at.n) nxt = pages_of(at.step + i + 32 + lane);
                 }
-                int p[4] = {__shfl_sync(0xffffffffu, cur.x, i & 31), __shfl_sync(0xffffffffu, cur.y, i & 31), 0, 0};
-                if (page == 16) {
-                    p[2] = __shfl_sync(0xffffffffu, cur.z, i & 31);
-                    p[3] = __shfl_sync(0xffffffffu, cur.w, i & 31);
-                }
+                const int p0 = __shfl_sync(0xffffffffu, cur.x, i & 31), p1 = __shfl_sync(0xffffffffu, cur.y, i & 31);
+                const int p2 = __shfl_sync(0xffffffffu, cur.z, i & 31), p3 = __shfl_sync(0xffffffffu, cur.w, i & 31);
                 const int st = j % NB;
-                const uint32_t par = static_cast<uint32_t>((j / NB - 1) & 1);
-                const uint64_t pol = at.step + i < prefix_blocks ? often : once;
-                auto load = [&](uint8_t* dst, const CUtensorMap* tm, uint64_t* bar) {
-                    mbar_arrive_expect_tx(bar, kKV);
+                if (j >= NB && !wait_all(&empty[st], static_cast<uint32_t>((j / NB - 1) & 1))) {
+                    ok = false;
+                    break;
+                }
+                if (leader) {
+                    const uint64_t pol = at.step + i < prefix_blocks ? often : once;
+                    uint8_t* dst = ring + st * kKV;
+                    const int y = at.hk * page;
+                    mbar_arrive_expect_tx(&full[st], kKV);
 #pragma unroll
                     for (int h = 0; h < kParts; ++h) {
-                        if (page >= kServeBlock) {
-                            tma_3d(dst + h * kHalfKV, tm, 64 * h, at.hk * page + p[1], p[0], bar, pol);
+                        uint8_t* d = dst + h * kHalfKV;
+                        if (boxes == 1) {
+                            tma_3d(d, tm, 64 * h, y + p1, p0, &full[st], pol);
                         } else {
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                if (k < kServeBlock >> lg)
-                                    tma_3d(dst + h * kHalfKV + k * page * 128, tm, 64 * h, at.hk * page, p[k], bar, pol);
+                            tma_3d(d, tm, 64 * h, y, p0, &full[st], pol);
+                            tma_3d(d + page * 128, tm, 64 * h, y, p1, &full[st], pol);
+                            if (boxes == 4) {
+                                tma_3d(d + page * 256, tm, 64 * h, y, p2, &full[st], pol);
+                                tma_3d(d + page * 384, tm, 64 * h, y, p3, &full[st], pol);
+                            }
                         }
                     }
-                };
-                if (j >= NB && !wait_all(&kempty[st], par)) {
-                    ok = false;
-                    break;
                 }
-                if (leader) load(sK + st * kKV, &maps.k, &kfull[st]);
-                kiss = j + 1;
-                if (j >= NB && !wait_all(&vempty[st], par)) {
-                    ok = false;
-                    break;
-                }
-                if (leader) load(sV + st * kKV, &maps.v, &vfull[st]);
-                viss = j + 1;
+                ++j;
             }
         } while (ok && at.advance());
         if (leader && *const_cast<volatile int*>(&s_abort)) {
@@ -309,92 +313,94 @@ __global__ void __launch_bounds__(kThreads, 2)
                 while (!mbar_try_wait(bar, static_cast<uint32_t>(phase & 1)) && spin_clock() - t0 < kWaitLimitCycles) {
                 }
             };
-            if (qiss) land(&qfull, qiss - 1);
-            for (int k = max(0, kiss - NB); k < kiss; ++k) land(&kfull[k % NB], k / NB);
-            for (int k = max(0, viss - NB); k < viss; ++k) land(&vfull[k % NB], k / NB);
+            if (seg) land(&qfull, seg - 1);
+            for (int k = max(0, j - NB); k < j; ++k) land(&full[k % NB], k / NB);
         }
-    } else if (warp == 5) {
+    } else if (warp >= 5) {
         // ------------------------------------------------ MMA issue
         const bool leader = elect_one();
         const uint32_t t_o = __shfl_sync(0xffffffffu, tmem, 0), t_s = t_o + 128;
         constexpr uint32_t kType = std::is_same<T, __half>::value ? 0u : (1u << 7) | (1u << 10);
         constexpr uint32_t kShape = (1u << 4) | kType | (static_cast<uint32_t>(kServeRows >> 4) << 24);
-        constexpr uint32_t id_s = kShape | (static_cast<uint32_t>(kServeBlock >> 3) << 17);
-        constexpr uint32_t id_o = kShape | (static_cast<uint32_t>(HD >> 3) << 17) | (1u << 16);  // V is MN-major
-        const uint64_t qd = sw128(smem_u32(sQ), 16, 1024), kd = sw128(smem_u32(sK), 16, 1024);
-        const uint64_t vd = sw128(smem_u32(sV), kHalfKV, 1024);
-        auto issue_s = [&](int j, bool last) {
-            const int st = j % NB, sb = j % 2;
-            if (!wait_all(&kfull[st], static_cast<uint32_t>((j / NB) & 1))) return false;
-            // S_j goes where P_{j-2} was: its P V must be done
-            if (j >= 2 && !wait_all(&pvdone[sb], static_cast<uint32_t>(((j - 2) / 2) & 1))) return false;
-            tc_fence_after();
-            if (leader) {
-                const uint64_t kds = kd + static_cast<uint64_t>(st * (kKV >> 4));
-#pragma unroll
-                for (int k = 0; k < HD / 16; ++k)
-                    umma_bf16(t_s + static_cast<uint32_t>(sb * 64),
-                              qd + static_cast<uint64_t>(((k >> 2) * kHalfQ + (k & 3) * 32) >> 4),
-                              kds + static_cast<uint64_t>(((k >> 2) * kHalfKV + (k & 3) * 32) >> 4), id_s, k > 0 ? 1u : 0u);
-                umma_commit(&sfull[sb]);
-                umma_commit(&kempty[st]);
-                if (last) umma_commit(&qempty);  // the segment's last use of Q
-            }
-            __syncwarp();
-            return true;
-        };
-        int j = 0, seg = 0;
+        int j = 0;
         bool ok = true;
-        do {
-            if (at.left <= 0) break;
-            ok = wait_all(&qfull, static_cast<uint32_t>(seg++ & 1)) && issue_s(j, at.n == 1);
-            // first and last + 1 live lane of a step
-            const int tok0 = at.tile * s.tile_tokens;
-            auto live_of = [&](int step) {
-                int2 r = make_int2(0, kServeRows);
-                if (step >= prefix_blocks && at.own0 >= 0) {
-                    const int4 f = __ldg(w.info + at.own0 + step - prefix_blocks);
-                    r.x = max(f.x - tok0, 0) * s.G;
-                    r.y = min(f.y - tok0, s.tile_tokens) * s.G;
+        if (warp == 5) {
+            constexpr uint32_t id_s = kShape | (static_cast<uint32_t>(kServeBlock >> 3) << 17);
+            const uint64_t qd = sw128(smem_u32(sQ), 16, 1024), kd = sw128(smem_u32(sK), 16, 1024);
+            int seg = 0;
+            do {
+                if (at.left <= 0) break;
+                ok = wait_all(&qfull, static_cast<uint32_t>(seg++ & 1));
+                for (int i = 0; i < at.n && ok; ++i, ++j) {
+                    const int st = j % NB, sb = j % 2;
+                    ok = wait_all(&kfull[st], static_cast<uint32_t>((j / NB) & 1));
+                    // S_j goes where P_{j-2} was: its P V must be done
+                    if (ok && j >= 2) ok = wait_all(&pvdone[sb], static_cast<uint32_t>(((j - 2) / 2) & 1));
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (leader) {
+                        const uint64_t kds = kd + static_cast<uint64_t>(st * (kKV >> 4));
+#pragma unroll
+                        for (int k = 0; k < HD / 16; ++k)
+                            umma_bf16(t_s + static_cast<uint32_t>(sb * 64),
+                                      qd + static_cast<uint64_t>(((k >> 2) * kHalfQ + (k & 3) * 32) >> 4),
+                                      kds + static_cast<uint64_t>(((k >> 2) * kHalfKV + (k & 3) * 32) >> 4), id_s, k > 0 ? 1u : 0u);
+                        umma_commit(&sfull[sb]);
+                        umma_commit(&kempty[st]);
+                        if (i + 1 == at.n) umma_commit(&qempty);  // the segment's last use of Q
+                    }
+                    __syncwarp();
                 }
-                return r;
-            };
-            int2 cur, nxt = make_int2(0, 0);
-            if (lane < at.n) nxt = live_of(at.step + lane);
-            for (int i = 0; i < at.n && ok; ++i, ++j) {
-                if ((i & 31) == 0) {
-                    cur = nxt;
-                    if (i + 32 + lane < at.n) nxt = live_of(at.step + i + 32 + lane);
-                }
-                const int lo = __shfl_sync(0xffffffffu, cur.x, i & 31), hi = __shfl_sync(0xffffffffu, cur.y, i & 31);
-                if (i + 1 < at.n && !issue_s(j + 1, i + 2 == at.n)) {
-                    ok = false;
-                    break;
-                }
-                const int st = j % NB, sb = j % 2;
-                ok = wait_all(&vfull[st], static_cast<uint32_t>((j / NB) & 1)) &&
-                     wait_all(&pfull[sb], static_cast<uint32_t>((j / 2) & 1));
-                if (!ok) break;
-                tc_fence_after();
-                if (leader) {
-                    const uint64_t vds = vd + static_cast<uint64_t>(st * (kKV >> 4));
+            } while (ok && at.advance());
+        } else {
+            constexpr uint32_t id_o = kShape | (static_cast<uint32_t>(HD >> 3) << 17) | (1u << 16);  // V is MN-major
+            const uint64_t vd = sw128(smem_u32(sV), kHalfKV, 1024);
+            do {
+                if (at.left <= 0) break;
+                // first and last + 1 live lane of a step
+                const int tok0 = at.tile * s.tile_tokens;
+                auto live_of = [&](int step) {
+                    int2 r = make_int2(0, kServeRows);
+                    if (step >= prefix_blocks && at.own0 >= 0) {
+                        const int4 f = __ldg(w.info + at.own0 + step - prefix_blocks);
+                        r.x = max(f.x - tok0, 0) * s.G;
+                        r.y = min(f.y - tok0, s.tile_tokens) * s.G;
+                    }
+                    return r;
+                };
+                int2 cur, nxt = make_int2(0, 0);
+                if (lane < at.n) nxt = live_of(at.step + lane);
+                for (int i = 0; i < at.n; ++i, ++j) {
+                    if ((i & 31) == 0) {
+                        cur = nxt;
+                        if (i + 32 + lane < at.n) nxt = live_of(at.step + i + 32 + lane);
+                    }
+                    const int lo = __shfl_sync(0xffffffffu, cur.x, i & 31), hi = __shfl_sync(0xffffffffu, cur.y, i & 31);
                     const uint4 off = make_uint4(~bit_run(lo, hi), ~bit_run(lo - 32, hi - 32), ~bit_run(lo - 64, hi - 64),
                                                  ~bit_run(lo - 96, hi - 96));
+                    const int st = j % NB, sb = j % 2;
+                    ok = wait_all(&vfull[st], static_cast<uint32_t>((j / NB) & 1)) &&
+                         wait_all(&pfull[sb], static_cast<uint32_t>((j / 2) & 1));
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (leader) {
+                        const uint64_t vds = vd + static_cast<uint64_t>(st * (kKV >> 4));
 #pragma unroll
-                    for (int k = 0; k < kServeBlock / 16; ++k)
-                        umma_tmem_a_masked(t_o, t_s + static_cast<uint32_t>(sb * 64 + k * 8),
-                                           vds + static_cast<uint64_t>((k * 2048) >> 4), id_o, off);
-                    umma_commit(&pvdone[sb]);
-                    umma_commit(&vempty[st]);
+                        for (int k = 0; k < kServeBlock / 16; ++k)
+                            umma_tmem_a_masked(t_o, t_s + static_cast<uint32_t>(sb * 64 + k * 8),
+                                               vds + static_cast<uint64_t>((k * 2048) >> 4), id_o, off);
+                        umma_commit(&pvdone[sb]);
+                        umma_commit(&vempty[st]);
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
-            }
-        } while (ok && at.advance());
+            } while (ok && at.advance());
+        }
         // every MMA is done before the CTA gives back tensor memory and shared memory
         if (leader) {
-            umma_commit(&drain);
+            umma_commit(&drain[warp - 5]);
             const long long t0 = spin_clock();
-            while (!mbar_try_wait(&drain, 0) && spin_clock() - t0 < kWaitLimitCycles) {
+            while (!mbar_try_wait(&drain[warp - 5], 0) && spin_clock() - t0 < kWaitLimitCycles) {
             }
         }
         __syncwarp();
@@ -432,25 +438,25 @@ __global__ void __launch_bounds__(kThreads, 2)
                 const int step = at.step + i, sb = j % 2;
                 f = fn;
                 if (i + 1 < at.n) fn = info_of(step + 1);
-                // keys of the block that there are, and that this row sees
+                // keys of the block that there are, and that this row sees.  A row that is not live (of another
+                // request) computes on, unmasked, and keeps its m and l: its lane of O is not written.
                 int valid, seen;
-                bool live = there;
+                bool live = true;
                 if (step < prefix_blocks) {
-                    valid = min(kServeBlock, prefix_len - step * kServeBlock);
-                    seen = there ? valid : 0;
+                    valid = seen = min(kServeBlock, prefix_len - step * kServeBlock);
                 } else {
                     valid = min(kServeBlock, f.w + f.y - f.x - f.z);
                     live = there && tok >= f.x && tok < f.y;
-                    seen = !live ? 0 : causal ? min(valid, f.w + tok - f.x + 1 - f.z) : valid;
+                    seen = causal ? min(valid, f.w + tok - f.x + 1 - f.z) : valid;
                 }
                 ok = wait(&sfull[sb], static_cast<uint32_t>((j / 2) & 1));
                 if (!ok) break;
-                if (__any_sync(0xffffffffu, seen > 0)) {
+                if (__any_sync(0xffffffffu, live && seen > 0)) {
                     tc_fence_after();
                     const uint32_t ts = t_s + static_cast<uint32_t>(sb * 64);
                     float v[64];
                     tmem_ld_32x64(ts, v);
-                    if (__any_sync(0xffffffffu, seen < kServeBlock)) {
+                    if (__any_sync(0xffffffffu, live && seen < kServeBlock)) {
 #pragma unroll
                         for (int k = 0; k < 64; ++k)
                             if (k >= seen) v[k] = -INFINITY;
@@ -466,7 +472,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                         }
                         mx = fmaxf(fmaxf(mi[0], mi[1]), fmaxf(mi[2], mi[3])) * sl2;
                     }
-                    const bool up = mx > m + 8.0f;  // (m = -inf: the row's first keys)
+                    const bool up = live && mx > m + 8.0f;  // (m = -inf: the row's first keys)
                     if (__any_sync(0xffffffffu, up && m != -INFINITY)) {
                         ok = wait(&pvdone[(j - 1) % 2], static_cast<uint32_t>(((j - 1) / 2) & 1));
                         if (!ok) break;
@@ -495,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                         ls[k & 1] = add2(ls[k & 1], e);
                         pk[k] = Half2<T>::pack(e.x, e.y);
                     }
-                    l += (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
+                    if (live) l += (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
                     tmem_st_32u(ts, pk);
                 } else if (__any_sync(0xffffffffu, live)) {
                     // rows of the block's request, all before its keys: nothing, but their lanes do take part
