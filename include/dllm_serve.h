@@ -128,7 +128,7 @@ int dllm_serve_qk_norm_rope(const dllm_serve_config* cfg, const dllm_serve_table
  * prefix_len prefix positions (pages prefix_pages dev int32 [n_prefix], in
  * order, of the same pool) and the own keys that the row sees.  Query head h
  * reads K/V head h / (n_heads / n_kv_heads).  q row r at r * ldq, out
- * [rows][n_heads * head_dim]; lse dev fp32 [rows][n_heads], nullable: the
+ * [rows][n_heads * head_dim], 32-byte aligned; lse dev fp32 [rows][n_heads], nullable: the
  * natural logarithm of the row's softmax sum.  A row that sees no key, and
  * padding, gives zeros (lse -inf).  Keys and values past a request's n_keys,
  * or past the prefix, may hold anything, infinities and NaN included.

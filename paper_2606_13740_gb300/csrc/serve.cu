@@ -175,6 +175,7 @@ int dllm_serve_attention(const dllm_serve_config* cfg, const dllm_serve_tables* 
         return fail(DLLM_EINVAL, "serve attention: ldq must be a multiple of 8, and no less than a row");
     for (const void* p : {q, kc, vc, static_cast<const void*>(out)})
         if (!aligned(p, 16)) return fail(DLLM_EINVAL, "serve attention: buffers must be 16-byte aligned");
+    if (!aligned(out, 32)) return fail(DLLM_EINVAL, "serve attention: out must be 32-byte aligned");
     if (rows == 0) return DLLM_OK;
     const int sms = sm_count();
     if (sms <= 0) return fail(DLLM_ECUDA, "no CUDA device");

@@ -103,7 +103,7 @@ def test_calls_refuse_bad_arguments(L):
         return L.dllm_serve_attention(cp, tp, q, ldq, kc, vc, pages, n, scale, out, None, rows, None)
 
     for bad in (dict(q=None), dict(ldq=248), dict(ldq=260), dict(kc=None), dict(vc=P + 2), dict(pages=None), dict(n=-1),
-                dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")), dict(scale=float("nan")), dict(out=None),
+                dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")), dict(scale=float("nan")), dict(out=None), dict(out=P + 16),
                 dict(rows=65), dict(rows=-1)):
         assert attn(**bad) == -1, bad
     # no rows: nothing to do, and no GPU needed for it
