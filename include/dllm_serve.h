@@ -112,7 +112,8 @@ int dllm_serve_plan(const dllm_serve_config* cfg, const dllm_serve_tables* t, co
                     const int32_t* q_len, int batch, int rows, int prefix_len, int causal, void* stream);
 
 /* Queries and keys of rows 0 .. rows - 1: RMSNorm of each head,
- * y = x * rsqrt(mean(x^2) + eps) * gain (gain dev fp32 [head_dim], null: ones),
+ * y = x * rsqrt(mean(x^2) + eps) * gain (gain dev fp32 [head_dim], 16-byte
+ * aligned, null: ones),
  * then rotate-half RoPE: features j and j + head_dim / 2 turned by
  * pos[row] * theta[j] (theta dev fp32 [head_dim / 2]).  q, k, v dev of in_dtype
  * (the config's dtype, or DLLM_F32): row r at r * ldq, r * ldk, r * ldv

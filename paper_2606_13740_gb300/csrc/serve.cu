@@ -152,6 +152,8 @@ int dllm_serve_qk_norm_rope(const dllm_serve_config* cfg, const dllm_serve_table
         return fail(DLLM_EINVAL, "qk_norm_rope: strides must be multiples of 8, and no less than a row");
     for (const void* p : {q, k, v, static_cast<const void*>(q_out), static_cast<const void*>(kc), static_cast<const void*>(vc)})
         if (!aligned(p, 16)) return fail(DLLM_EINVAL, "qk_norm_rope: buffers must be 16-byte aligned");
+    if (!aligned(q_gain, 16) || !aligned(k_gain, 16) || !aligned(theta, 4))
+        return fail(DLLM_EINVAL, "qk_norm_rope: gains must be 16-byte aligned");
     if (q_out == q && (in_dtype != s.dtype || ldq != ld_out))
         return fail(DLLM_EINVAL, "qk_norm_rope: in place, q_out has q's type and stride");
     if (rows == 0) return DLLM_OK;

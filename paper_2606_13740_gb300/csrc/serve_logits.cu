@@ -16,7 +16,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kChunk = 8192;  // ids of a stretch: 32 KB of words, five CTAs an SM beside them
+constexpr int kChunk = 8192;  // ids of a stretch, at most: 32 KB of words
+constexpr int kGroup = 128;   // ids that a warp takes side by side, 4 a lane
+constexpr int kGroups = 4;    // of these in flight together
 constexpr int kCountBits = 20;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -25,11 +27,41 @@ struct Part {
     int arg, pad;
 };
 
-// Stretches of a row: chunks, each cut among the `split` warps that share a row.
+// How a call is cut: stretches of `chunk` ids, `rows_cta` rows a CTA, `split` warps a row and stretch.
 struct Cut {
-    int chunks, rows_cta, split;
+    int chunk, chunks, rows_cta, split;
 };
-__host__ __device__ inline int cut_parts(const Cut& c) { return c.chunks * c.split; }
+
+__device__ __forceinline__ float2 sub2(float2 a, float b) {
+    float2 d;
+    asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %4};\n"
+        " sub.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}\n"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n"
+        " add.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}\n"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float b) {
+    float2 d;
+    asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %4};\n"
+        " mul.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}\n"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b));
+    return d;
+}
+// 2^x by the special function unit; below 2^-126: 0 (nothing beside the largest, 1)
+__device__ __forceinline__ float ex2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 
 template <typename T>
 struct Io;
@@ -75,9 +107,9 @@ __device__ __forceinline__ float exp_below(float a, float m) { return a == -INFI
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) k_logits(const __grid_constant__ dllm_serve_logits_args a, Cut cut,
                                                      Part* __restrict__ part, float* __restrict__ zcur) {
-    __shared__ __align__(16) uint32_t word[kChunk];
+    extern __shared__ __align__(16) uint32_t word[];  // [cut.chunk]
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int v0 = blockIdx.y * kChunk, v1 = min(a.vocab, v0 + kChunk), n = v1 - v0;
+    const int v0 = blockIdx.y * cut.chunk, v1 = min(a.vocab, v0 + cut.chunk), n = v1 - v0;
     const int row0 = blockIdx.x * cut.rows_cta, row1 = min(a.rows, row0 + cut.rows_cta);
     const int words = (a.vocab + 31) / 32;
 
@@ -94,17 +126,31 @@ __global__ void __launch_bounds__(kThreads) k_logits(const __grid_constant__ dll
             if (a.bias_ids) {
                 const int len = a.bias_len ? min(max(__ldg(a.bias_len + req), 0), a.bias_ld) : a.bias_ld;
                 for (int i = tid; i < len; i += kThreads) {
-                    const int v = __ldg(a.bias_ids + static_cast<size_t>(req) * a.bias_ld + i) - v0;
-                    if (v >= 0 && v < n) atomicMax(&word[v], static_cast<uint32_t>(i + 1) << kCountBits);
+                    const unsigned v = static_cast<unsigned>(__ldg(a.bias_ids + static_cast<size_t>(req) * a.bias_ld + i) - v0);
+                    if (v < static_cast<unsigned>(n)) atomicMax(&word[v], static_cast<uint32_t>(i + 1) << kCountBits);
                 }
                 __syncthreads();
             }
             if (a.hist) {
                 const int len = a.hist_len ? min(max(__ldg(a.hist_len + req), 0), a.hist_ld) : a.hist_ld;
                 const int* h = a.hist + static_cast<size_t>(req) * a.hist_ld;
-                for (int i = tid; i < len; i += kThreads) {
-                    const int v = __ldg(h + i) - v0;
-                    if (v >= 0 && v < n) atomicAdd(&word[v], 1u);
+                auto count = [&](int id) {
+                    const unsigned v = static_cast<unsigned>(id - v0);
+                    if (v < static_cast<unsigned>(n)) atomicAdd(&word[v], 1u);
+                };
+                // whole 16-byte pieces, and what is before and behind them
+                const int lead = min(len, static_cast<int>((16 - reinterpret_cast<uintptr_t>(h) % 16) % 16 / 4));
+                const int4* h4 = reinterpret_cast<const int4*>(h + lead);
+                const int n4 = (len - lead) / 4;
+                if (tid < lead) count(__ldg(h + tid));
+                if (tid < len - lead - 4 * n4) count(__ldg(h + lead + 4 * n4 + tid));
+#pragma unroll 2
+                for (int i = tid; i < n4; i += kThreads) {
+                    const int4 x = __ldg(h4 + i);
+                    count(x.x);
+                    count(x.y);
+                    count(x.z);
+                    count(x.w);
                 }
             }
             __syncthreads();
@@ -114,91 +160,130 @@ __global__ void __launch_bounds__(kThreads) k_logits(const __grid_constant__ dll
         const float pres = asks && a.pres ? __ldg(a.pres + req) : 0.0f;
         const float* bias = a.bias_ids && asks ? a.bias + static_cast<size_t>(req) * a.bias_ld : nullptr;
 
-        // warp jobs: (row, share of the stretch), shares of whole groups of 128 ids
+        // warp jobs: (row, share of the stretch), shares of whole groups
         for (int job = warp; job < (r1 - r0) * cut.split; job += kWarps) {
-            const int row = r0 + job / cut.split, share = job % cut.split;
-            const int g0 = (n + 127) / 128 * share / cut.split * 128, g1 = min(n, (n + 127) / 128 * (share + 1) / cut.split * 128);
+            const int row = r0 + job / cut.split, share = job % cut.split, groups = (n + kGroup - 1) / kGroup;
+            const int g0 = groups * share / cut.split * kGroup, g1 = min(n, groups * (share + 1) / cut.split * kGroup);
             const T* src = static_cast<const T*>(a.logits) + static_cast<size_t>(row) * a.ld + v0;
             T* dst = a.out ? static_cast<T*>(a.out) + static_cast<size_t>(row) * a.ld_out + v0 : nullptr;
             const int g = a.grammar ? __ldg(a.grammar_row + row) : -1;
             const uint32_t* allow = g >= 0 && g < a.n_grammar ? a.grammar + static_cast<size_t>(g) * words + v0 / 32 : nullptr;
-            const int cur = a.cur ? __ldg(a.cur + row) - v0 : -1;
-            const int mask = a.mask_id - v0;
-            float m = -INFINITY, s = 0.0f;
+            const int cur = a.cur ? __ldg(a.cur + row) - v0 : -1, mask = a.mask_id < 0 ? -1 : a.mask_id - v0;
+            float m = -INFINITY;
+            float2 s[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
             int arg = kChunk;
-            for (int i0 = g0 + 4 * lane; i0 < g1; i0 += 128) {
-                float z[4];
-                const bool whole = VEC && i0 + 4 <= n;
+            for (int base = g0; base < g1; base += kGroup * kGroups) {
+                const int i0 = base + 4 * lane;
+                float z[kGroups][4];
+                // (a warp's groups lie whole in the stretch but for the vocabulary's end)
+                const bool whole = VEC && base + kGroup * kGroups <= g1;
                 if (whole) {
-                    Io<T>::get4(src + i0, z);
+#pragma unroll
+                    for (int u = 0; u < kGroups; ++u) Io<T>::get4(src + i0 + u * kGroup, z[u]);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) z[i] = i0 + i < n ? Io<T>::get(src + i0 + i) : -INFINITY;
+                    for (int u = 0; u < kGroups; ++u)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            z[u][i] = i0 + u * kGroup + i < g1 ? Io<T>::get(src + i0 + u * kGroup + i) : -INFINITY;
                 }
                 if (asks) {
-                    const uint4 u = *reinterpret_cast<const uint4*>(word + i0);
-                    if (u.x | u.y | u.z | u.w) {
-                        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t c = w[i] & ((1u << kCountBits) - 1), k = w[i] >> kCountBits;
-                            if (c) {
-                                const float f = z[i] > 0.0f ? __fdiv_rn(z[i], rep) : __fmul_rn(z[i], rep);
-                                z[i] = __fsub_rn(f, __fadd_rn(__fmul_rn(freq, static_cast<float>(c)), pres));
+                    for (int u = 0; u < kGroups; ++u) {
+                        if (!whole && i0 + u * kGroup >= g1) break;
+                        const uint4 x = *reinterpret_cast<const uint4*>(word + i0 + u * kGroup);
+                        if (x.x | x.y | x.z | x.w) {
+                            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t c = w[i] & ((1u << kCountBits) - 1), k = w[i] >> kCountBits;
+                                if (c) {
+                                    const float f = z[u][i] > 0.0f ? __fdiv_rn(z[u][i], rep) : __fmul_rn(z[u][i], rep);
+                                    z[u][i] = __fsub_rn(f, __fadd_rn(__fmul_rn(freq, static_cast<float>(c)), pres));
+                                }
+                                if (k) z[u][i] = __fadd_rn(z[u][i], __ldg(bias + k - 1));
                             }
-                            if (k) z[i] = __fadd_rn(z[i], __ldg(bias + k - 1));
                         }
                     }
                 }
                 if (allow) {
-                    const uint32_t ok = __ldg(allow + (i0 >> 5)) >> (i0 & 31);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (!((ok >> i) & 1u)) z[i] = -INFINITY;
+                    for (int u = 0; u < kGroups; ++u) {
+                        if (!whole && i0 + u * kGroup >= g1) break;
+                        const uint32_t ok = __ldg(allow + ((i0 + u * kGroup) >> 5)) >> (i0 & 31);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (!((ok >> i) & 1u)) z[u][i] = -INFINITY;
+                    }
                 }
                 if (dst) {
                     if (whole) {
-                        Io<T>::put4(dst + i0, z);
+#pragma unroll
+                        for (int u = 0; u < kGroups; ++u) Io<T>::put4(dst + i0 + u * kGroup, z[u]);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (i0 + i < n) Io<T>::put(dst + i0 + i, z[i]);
+                        for (int u = 0; u < kGroups; ++u)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (i0 + u * kGroup + i < g1) Io<T>::put(dst + i0 + u * kGroup + i, z[u][i]);
                     }
                 }
-                if (static_cast<unsigned>(cur - i0) < 4u) {
+                // the current id's logit, and the mask id out of the decision
+                if (static_cast<unsigned>(cur - base) < kGroup * kGroups && cur < g1) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (cur == i0 + i) zcur[row] = z[i];
-                }
-                if (static_cast<unsigned>(mask - i0) < 4u) {
+                    for (int u = 0; u < kGroups; ++u)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (mask == i0 + i) z[i] = -INFINITY;
+                        for (int i = 0; i < 4; ++i)
+                            if (cur == i0 + u * kGroup + i) zcur[row] = z[u][i];
                 }
-                const float mx = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
+                if (static_cast<unsigned>(mask - base) < kGroup * kGroups) {
+#pragma unroll
+                    for (int u = 0; u < kGroups; ++u)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (mask == i0 + u * kGroup + i) z[u][i] = -INFINITY;
+                }
+                float mx = -INFINITY;
+#pragma unroll
+                for (int u = 0; u < kGroups; ++u) mx = fmaxf(mx, fmaxf(fmaxf(z[u][0], z[u][1]), fmaxf(z[u][2], z[u][3])));
                 if (mx > m) {  // rare after the first groups
-                    s *= exp_below(m, mx);
+                    const float al = exp_below(m, mx);
+                    s[0] = make_float2((s[0].x + s[0].y + s[1].x + s[1].y) * al, 0.0f);
+                    s[1] = make_float2(0.0f, 0.0f);
                     m = mx;
-                    arg = i0 + (z[0] == mx ? 0 : z[1] == mx ? 1 : z[2] == mx ? 2 : 3);
+#pragma unroll
+                    for (int u = kGroups - 1; u >= 0; --u)
+#pragma unroll
+                        for (int i = 3; i >= 0; --i)
+                            if (z[u][i] == mx) arg = i0 + u * kGroup + i;
                 }
                 // (the difference first: z and m may be the type's lowest value, whose product overflows)
                 const float ref = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s += exp2f((z[i] - ref) * kLog2e);
+                for (int u = 0; u < kGroups; ++u) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float2 e = mul2(sub2(make_float2(z[u][2 * i], z[u][2 * i + 1]), ref), kLog2e);
+                        e.x = ex2(e.x);
+                        e.y = ex2(e.y);
+                        s[i] = add2(s[i], e);
+                    }
+                }
             }
+            float sum = (s[0].x + s[0].y) + (s[1].x + s[1].y);
             // the warp's lanes: largest z, of equal ones the lowest id
 #pragma unroll
             for (int d = 16; d; d /= 2) {
-                const float om = __shfl_xor_sync(0xffffffffu, m, d), os = __shfl_xor_sync(0xffffffffu, s, d);
+                const float om = __shfl_xor_sync(0xffffffffu, m, d), os = __shfl_xor_sync(0xffffffffu, sum, d);
                 const int oa = __shfl_xor_sync(0xffffffffu, arg, d);
                 const float mx = fmaxf(m, om);
-                s = s * (m == mx ? 1.0f : exp_below(m, mx)) + os * (om == mx ? 1.0f : exp_below(om, mx));
+                sum = sum * (m == mx ? 1.0f : exp_below(m, mx)) + os * (om == mx ? 1.0f : exp_below(om, mx));
                 arg = om > m ? oa : om < m ? arg : min(arg, oa);
                 m = mx;
             }
             if (lane == 0)
                 part[(static_cast<size_t>(row) * cut.chunks + blockIdx.y) * cut.split + share] =
-                    Part{m, s, arg < kChunk ? v0 + arg : -1, 0};
+                    Part{m, sum, arg < kChunk ? v0 + arg : -1, 0};
         }
         __syncthreads();
         r0 = r1;
@@ -240,13 +325,22 @@ __global__ void __launch_bounds__(128) k_merge(const __grid_constant__ dllm_serv
     }
 }
 
-Cut logits_cut(int rows, int n_req) {
+// Rows of a request share its words and the reading of its lists; CTAs enough to fill the GPU come first.
+// (512 rows of 126464 ids in 32-row CTAs of 8192 ids, 256 of them: 274 us.)
+Cut logits_cut(int rows, int vocab, int n_req, int sms) {
     Cut c;
-    c.chunks = 0;
-    // rows of a request share its words; single rows share a CTA's warps instead
-    const int per = rows / (n_req > 0 ? n_req : rows);
+    const int per = n_req > 0 ? rows / n_req : 1;
     c.rows_cta = per < 1 ? 1 : per > 32 ? 32 : per;
-    c.split = c.rows_cta >= kWarps ? 1 : (kWarps + c.rows_cta - 1) / c.rows_cta;
+    c.chunk = kChunk;
+    auto ctas = [&] {
+        return static_cast<long long>((rows + c.rows_cta - 1) / c.rows_cta) * ((vocab + c.chunk - 1) / c.chunk);
+    };
+    while (c.rows_cta > kWarps && ctas() < 6ll * sms) c.rows_cta = (c.rows_cta + 1) / 2;
+    while (c.chunk > 2048 && ctas() < sms) c.chunk /= 2;
+    c.chunks = (vocab + c.chunk - 1) / c.chunk;
+    const int most = c.chunk / (kGroup * kGroups);
+    c.split = (kWarps + c.rows_cta - 1) / c.rows_cta;
+    if (c.split > most) c.split = most;
     return c;
 }
 
@@ -255,8 +349,8 @@ cudaError_t go(const dllm_serve_logits_args& a, const Cut& c, Part* part, float*
     const dim3 grid((a.rows + c.rows_cta - 1) / c.rows_cta, c.chunks);
     const bool vec = reinterpret_cast<uintptr_t>(a.logits) % (4 * sizeof(T)) == 0 && a.ld % 4 == 0 &&
                      reinterpret_cast<uintptr_t>(a.out) % (4 * sizeof(T)) == 0 && (!a.out || a.ld_out % 4 == 0);
-    if (vec) k_logits<T, true><<<grid, kThreads, 0, st>>>(a, c, part, zcur);
-    else k_logits<T, false><<<grid, kThreads, 0, st>>>(a, c, part, zcur);
+    if (vec) k_logits<T, true><<<grid, kThreads, c.chunk * 4, st>>>(a, c, part, zcur);
+    else k_logits<T, false><<<grid, kThreads, c.chunk * 4, st>>>(a, c, part, zcur);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess || !(a.x0 || a.conf || a.tokconf)) return e;
     cudaLaunchConfig_t cfg{};
@@ -268,20 +362,19 @@ cudaError_t go(const dllm_serve_logits_args& a, const Cut& c, Part* part, float*
     at.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_merge, a, cut_parts(c), static_cast<const Part*>(part), static_cast<const float*>(zcur));
+    return cudaLaunchKernelEx(&cfg, k_merge, a, c.chunks * c.split, static_cast<const Part*>(part), static_cast<const float*>(zcur));
 }
 
 }  // namespace
 
 size_t serve_logits_bytes(int rows, int vocab) {
-    const size_t chunks = (static_cast<size_t>(vocab) + kChunk - 1) / kChunk;
-    return serve_round(static_cast<size_t>(rows) * chunks * kWarps * sizeof(Part)) + serve_round(static_cast<size_t>(rows) * 4);
+    // the most parts that a cut makes of a row: eight of each 8192 ids, or one of each 512
+    const size_t parts = static_cast<size_t>((vocab + kChunk - 1) / kChunk) * kWarps * 2;
+    return serve_round(static_cast<size_t>(rows) * 4) + serve_round(static_cast<size_t>(rows) * parts * sizeof(Part));
 }
 
 cudaError_t launch_serve_logits(const dllm_serve_logits_args& a, int sms, cudaStream_t st) {
-    (void)sms;
-    Cut c = logits_cut(a.rows, a.n_req);
-    c.chunks = (a.vocab + kChunk - 1) / kChunk;
+    const Cut c = logits_cut(a.rows, a.vocab, a.hist || a.bias_ids ? a.n_req : 0, sms);
     float* zcur = static_cast<float*>(a.ws);
     Part* part = reinterpret_cast<Part*>(static_cast<char*>(a.ws) + serve_round(static_cast<size_t>(a.rows) * 4));
     return a.dtype == DLLM_F32    ? go<float>(a, c, part, zcur, st)

@@ -3,10 +3,12 @@
 //
 // A head of hd features is held by hd / 16 lanes, each with the 8 features from 8 l on and the 8 from
 // hd / 2 + 8 l on: the rotation's partners are in one thread, loads and stores are 16 bytes a lane, and the
-// mean of squares takes two or three shuffles.  A warp takes heads of one row, so that the row's hd / 2
-// angles are made once a warp (one or two a lane) and travel by shuffles.  The angle is position x theta in
-// 64 bits, reduced to a part of a turn before it is rounded to 32 bits: the rotation is as exact at position
-// 10^6 as at 1.  Bound: memory, each value once in and once out.
+// mean of squares takes two or three shuffles.  A warp takes heads of one row, the next ones loading while
+// it works on a pass, and makes the row's hd / 2 angles once, one or two a lane, shared through shared memory.
+// An angle is position x theta as an integer: theta / 2 pi in units of 2^-64 of a turn, so that the product's
+// whole turns fall off its top and the rotation is as exact at position 10^6 as at 1.  (In 64-bit floating
+// point, of which the SM does two operations a cycle, the angles of 1201 rows took a fifth of the call.)
+// Bound: memory, each value once in and once out.
 #include "serve.cuh"
 
 namespace dllm {
@@ -15,27 +17,56 @@ namespace {
 
 constexpr int kWarpsPerCta = 8;
 
+// 8 values as they lie in memory, and as floats
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, float* v) {
-    const uint4 u = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+struct Raw8 {
+    uint4 u;
+    __device__ __forceinline__ void load(const T* p) { u = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void get(float* v) const {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = Half2<T>::unpack(w[i]);
-        v[2 * i] = f.x;
-        v[2 * i + 1] = f.y;
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = Half2<T>::unpack(w[i]);
+            v[2 * i] = f.x;
+            v[2 * i + 1] = f.y;
+        }
     }
-}
+};
 template <>
-__device__ __forceinline__ void load8<float>(const float* p, float* v) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const float4 f = reinterpret_cast<const float4*>(p)[i];
-        v[4 * i] = f.x;
-        v[4 * i + 1] = f.y;
-        v[4 * i + 2] = f.z;
-        v[4 * i + 3] = f.w;
+struct Raw8<float> {
+    float4 f[2];
+    __device__ __forceinline__ void load(const float* p) {
+        f[0] = reinterpret_cast<const float4*>(p)[0];
+        f[1] = reinterpret_cast<const float4*>(p)[1];
     }
+    __device__ __forceinline__ void get(float* v) const {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            v[4 * i] = f[i].x;
+            v[4 * i + 1] = f[i].y;
+            v[4 * i + 2] = f[i].z;
+            v[4 * i + 3] = f[i].w;
+        }
+    }
+};
+__device__ __forceinline__ void get8(const float* p, float* v) {  // 16-byte aligned
+    const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+// theta / 2 pi in units of 2^-64 of a turn, whole turns dropped: theta is a whole number below 2^24 times a
+// power of two, the number's product with the first 64 bits of 1 / 2 pi is exact, and what the bits behind
+// them would add is below 2^-40 / 2^23 of a turn a position (theta <= 1).
+__device__ __forceinline__ unsigned long long turns_of(float theta) {
+    const uint32_t u = __float_as_uint(theta);
+    const int e = static_cast<int>((u >> 23) & 255u);
+    const unsigned long long mant = (u & 0x7fffffu) | (e ? 0x800000u : 0u), per = 0x28be60db9391054aull;
+    const unsigned long long lo = mant * per, hi = __umul64hi(mant, per);
+    const int sh = 150 - max(e, 1);  // theta = mant 2^-sh
+    unsigned long long t;
+    if (sh <= 0) t = sh > -64 ? lo << -sh : 0;
+    else if (sh < 64) t = (hi << (64 - sh)) | (lo >> sh);
+    else t = sh < 128 ? hi >> (sh - 64) : 0;
+    return u >> 31 ? 0ull - t : t;
 }
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const float* v) {
@@ -65,48 +96,40 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) k_serve_norm(ServeShape s, 
         slot = -1;
     }
 
-    // cos and sin of pairs lane, lane + 32; then those of pairs 8 l .. 8 l + 7
-    float cs[8], sn[8];
+    __shared__ float4 angles[kWarpsPerCta][2][HD / 8];  // cosines, sines
     {
-        float c[HD / 64], d[HD / 64];
+        float* c = reinterpret_cast<float*>(angles[threadIdx.x >> 5][0]);
+        float* d = reinterpret_cast<float*>(angles[threadIdx.x >> 5][1]);
 #pragma unroll
-        for (int i = 0; i < HD / 64; ++i) {
-            const double turns = static_cast<double>(pos) * (static_cast<double>(__ldg(a.theta + lane + 32 * i)) * 0.15915494309189533577);
-            sincospif(2.0f * static_cast<float>(turns - rint(turns)), &d[i], &c[i]);
+        for (int i = lane; i < HD / 2; i += 32) {
+            const unsigned long long turn = turns_of(__ldg(a.theta + i)) * static_cast<unsigned long long>(static_cast<long long>(pos));
+            // the part of a turn, -1/2 .. 1/2, in units of pi
+            sincospif(static_cast<float>(static_cast<int>(turn >> 32)) * 4.656612873077393e-10f, d + i, c + i);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int p = 8 * l + i, src = p & 31;
-            cs[i] = __shfl_sync(0xffffffffu, c[0], src);
-            sn[i] = __shfl_sync(0xffffffffu, d[0], src);
-            if constexpr (HD == 128) {
-                const float c1 = __shfl_sync(0xffffffffu, c[1], src), d1 = __shfl_sync(0xffffffffu, d[1], src);
-                if (p >= 32) {
-                    cs[i] = c1;
-                    sn[i] = d1;
-                }
-            }
-        }
+        __syncwarp();
     }
 
     TO* kc = static_cast<TO*>(a.kc);
     TO* vc = static_cast<TO*>(a.vc);
     const long long at = slot < 0 ? 0 : (slot >> s.page_log2) * s.page_stride + static_cast<long long>(slot & (s.page - 1)) * HD;
     const int heads = H + 2 * Hkv;
+    Raw8<TI> rx, ry;
+    auto fetch = [&](int h) {  // head h of q, k and v in a row
+        if (h >= heads || (h >= H && slot < 0)) return;
+        const TI* src = h < H         ? static_cast<const TI*>(a.q) + row * a.ldq + static_cast<long long>(h) * HD
+                        : h < H + Hkv ? static_cast<const TI*>(a.k) + row * a.ldk + static_cast<long long>(h - H) * HD
+                                      : static_cast<const TI*>(a.v) + row * a.ldv + static_cast<long long>(h - H - Hkv) * HD;
+        rx.load(src + 8 * l);
+        ry.load(src + HD / 2 + 8 * l);
+    };
+    fetch(part * kHeads + sub);
     for (int h0 = part * kHeads; h0 < heads; h0 += parts * kHeads) {
         const int h = h0 + sub;
         const bool is_q = h < H, is_k = !is_q && h < H + Hkv, live = h < heads && (is_q || slot >= 0);
         float x[8], y[8];
-        if (live) {
-            const TI* src = is_q   ? static_cast<const TI*>(a.q) + row * a.ldq + static_cast<long long>(h) * HD
-                            : is_k ? static_cast<const TI*>(a.k) + row * a.ldk + static_cast<long long>(h - H) * HD
-                                   : static_cast<const TI*>(a.v) + row * a.ldv + static_cast<long long>(h - H - Hkv) * HD;
-            load8(src + 8 * l, x);
-            load8(src + HD / 2 + 8 * l, y);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = y[i] = 0.0f;
-        }
+        rx.get(x);
+        ry.get(y);
+        fetch(h + parts * kHeads);
         float ss = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) ss += x[i] * x[i] + y[i] * y[i];
@@ -117,15 +140,23 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) k_serve_norm(ServeShape s, 
         if (is_q || is_k) {
             const float r = rsqrtf(ss * (1.0f / HD) + a.eps);
             const float* gain = is_q ? a.q_gain : a.k_gain;
+            float gx[8], gy[8], c[8], d[8];
+            if (gain) {
+                get8(gain + 8 * l, gx);
+                get8(gain + HD / 2 + 8 * l, gy);
+            }
+            const float4 *pc = angles[threadIdx.x >> 5][0] + 2 * l, *pd = angles[threadIdx.x >> 5][1] + 2 * l;
+            *reinterpret_cast<float4*>(c) = pc[0], *reinterpret_cast<float4*>(c + 4) = pc[1];
+            *reinterpret_cast<float4*>(d) = pd[0], *reinterpret_cast<float4*>(d + 4) = pd[1];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 float u = x[i] * r, w = y[i] * r;
                 if (gain) {
-                    u *= __ldg(gain + 8 * l + i);
-                    w *= __ldg(gain + HD / 2 + 8 * l + i);
+                    u *= gx[i];
+                    w *= gy[i];
                 }
-                x[i] = u * cs[i] - w * sn[i];
-                y[i] = w * cs[i] + u * sn[i];
+                x[i] = u * c[i] - w * d[i];
+                y[i] = w * c[i] + u * d[i];
             }
             dst = is_q ? static_cast<TO*>(a.q_out) + row * a.ld_out + static_cast<long long>(h) * HD
                        : kc + at + static_cast<long long>(h - H) * s.page * HD;
