@@ -67,7 +67,7 @@ struct ServeArrays {
     int4* info;           // [max_blocks]: first and last + 1 row of the request, the block's first key, n_keys - rows
     int4* pages;          // [max_blocks]: up to four pages (page < 64), or page and first place in it
     long long* tile_cum;  // [max_tiles + 1]: steps of a K/V head's tiles before this one
-    int* tile_first;      // [max_tiles]: its first own block (-1: a tile without any key, one empty step)
+    int* tile_first;      // [max_tiles]: its first own block
 };
 
 __host__ __device__ inline size_t serve_round(size_t n) { return (n + 255) / 256 * 256; }

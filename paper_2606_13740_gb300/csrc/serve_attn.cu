@@ -133,7 +133,7 @@ __device__ __forceinline__ uint32_t bit_run(int lo, int hi) {
 struct Walk {
     const ServeArrays& w;
     int Hkv, tile, hk, step, left;
-    int n, own0, own1;    // steps of the current segment; first own block of the tile (-1: none) and of the next tile
+    int n, own0, own1;    // steps of the current segment; first own block of the tile and of the next one
     long long first, next, after;  // the tile's place in the sums, and the ends of it and of the next tile
     __device__ Walk(const ServeArrays& w_, int Hkv_, int cta) : w(w_), Hkv(Hkv_) {
         const int4 d = __ldg(w.cta + cta);
@@ -275,10 +275,8 @@ __global__ void __launch_bounds__(kThreads, 2)
                         if (i + 3 < n_prefix) p.w = __ldg(a.prefix_pages + i + 3);
                     }
                 }
-            } else if (at.own0 >= 0) {
-                p = __ldg(w.pages + at.own0 + step - prefix_blocks);
             } else {
-                p.y = 0;
+                p = __ldg(w.pages + at.own0 + step - prefix_blocks);
             }
             return p;
         };
@@ -388,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                 const int tok0 = at.tile * s.tile_tokens;
                 auto live_of = [&](int step) {
                     int2 r = make_int2(0, kServeRows);
-                    if (step >= prefix_blocks && at.own0 >= 0) {
+                    if (step >= prefix_blocks) {
                         const int4 f = __ldg(w.info + at.own0 + step - prefix_blocks);
                         r.x = max(f.x - tok0, 0) * s.G;
                         r.y = min(f.y - tok0, s.tile_tokens) * s.G;
@@ -466,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                     if (step < prefix_blocks) {
                         valid = seen = prefix_len - step * kServeBlock;
                     } else {
-                        const int4 f = at.own0 >= 0 ? __ldg(w.info + at.own0 + step - prefix_blocks) : make_int4(0, 0, 0, 0);
+                        const int4 f = __ldg(w.info + at.own0 + step - prefix_blocks);
                         valid = min(kServeBlock, f.w + f.y - f.x - f.z);
                         live = there && tok >= f.x && tok < f.y;
                         seen = causal ? min(valid, f.w + tok - f.x + 1 - f.z) : valid;

@@ -1,14 +1,14 @@
 // The plan of a serving step: pages taken and given back, slots and positions of the new tokens, and the
 // attention's work list, from the requests' lengths (include/dllm_serve.h, dllm_serve_plan).
 //
-// Everything follows from four running sums over the requests: new tokens, pages taken, pages given back,
-// blocks of 64 keys.  Each CTA makes all four by itself in shared memory (up to 4096 requests: a few
-// thousand cycles, less than a round of launches or of waiting for one another would cost), then fills its
-// share of the rows, pages and blocks, the owner of an item found by binary search in the sums, so that
-// one long request among many short ones spreads over all CTAs.  CTA 0 cuts the attention's work instead.
-// The state that all of them read (held, ring_pos) is replaced by the CTA that ends last.  Pages come from
-// the ring's front and go to its end, so that what a plan takes and what it gives back never meet: the
-// free pages and those given back fit into the ring together.
+// Everything follows from running sums over the requests: new tokens, pages taken, pages given back, blocks
+// of 64 keys, steps of the attention.  Each CTA makes them all by itself in shared memory (up to 4096
+// requests: a few thousand cycles, less than a round of launches or of waiting for one another would cost),
+// then fills its share of the rows, pages, blocks and tiles, the owner of an item found by binary search in
+// the sums, so that one long request among many short ones spreads over all CTAs.  (One CTA that summed over
+// the tiles took 30 us for 19500 of them.)  The state that all CTAs read (held, ring_pos) is replaced by the
+// CTA that ends last.  Pages come from the ring's front and go to its end, so that what a plan takes and what
+// it gives back never meet: the free pages and those given back fit into the ring together.
 #include "serve.cuh"
 
 namespace dllm {
@@ -89,20 +89,54 @@ __device__ __forceinline__ Wants wants(const PlanArgs& a, int b) {
     return w;
 }
 
+// sum of floor((x + k d) / m), k = 0 .. n - 1, by Euclid's steps on the lattice points under the line
+__device__ long long floor_sum(long long n, long long m, long long d, long long x) {
+    long long sum = 0;
+    while (n > 0) {
+        sum += n * (n - 1) / 2 * (d / m) + n * (x / m);
+        d %= m;
+        x %= m;
+        const long long top = d * n + x;  // the line's end; below it the points are counted by columns of height 1
+        if (top < m) break;
+        n = top / m;
+        x = top % m;
+        const long long t = m;
+        m = d;
+        d = t;
+    }
+    return sum;
+}
+
+// Shared memory of a CTA: the sums before each request, and what is read of the requests.
+struct Sums {
+    long long *scan, *steps;  // [3][kWarps]; [B + 1]: own steps of the tiles of the requests before
+    int *row, *grow, *shrink, *block;  // [B + 1]
+    int *len, *held;                   // [B]
+    uint8_t* refused;                  // [B]
+    __device__ Sums(void* base, int B) {
+        scan = static_cast<long long*>(base);
+        steps = scan + 3 * kWarps;
+        row = reinterpret_cast<int*>(steps + B + 1);
+        grow = row + B + 1;
+        shrink = grow + B + 1;
+        block = shrink + B + 1;
+        len = block + B + 1;
+        held = len + B;
+        refused = reinterpret_cast<uint8_t*>(held + B);
+    }
+};
+size_t plan_smem(int B) {
+    return sizeof(long long) * (3 * kWarps + B + 1) + sizeof(int) * (4 * (static_cast<size_t>(B) + 1) + 2 * B) + B;
+}
+
 __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__ PlanArgs a) {
     extern __shared__ long long smem[];
     const int B = a.batch;
-    long long* scan_buf = smem;                          // [4][kWarps]
-    long long* tile_sum = scan_buf + 4 * kWarps;         // [kThreads + 1], CTA 0
-    int* first_row = reinterpret_cast<int*>(tile_sum + kThreads + 1);  // [B + 1] each: sums before a request
-    int* first_grow = first_row + B + 1;
-    int* first_shrink = first_grow + B + 1;
-    int* first_block = first_shrink + B + 1;
-    uint8_t* refused = reinterpret_cast<uint8_t*>(first_block + B + 1);  // [B]
+    const Sums u(smem, B);
     __shared__ int s_taken, s_refused, s_last;
 
     const dllm_serve_tables& t = a.t;
-    const int n_pages = a.s.n_pages, page = a.s.page, lg = a.s.page_log2;
+    const int n_pages = a.s.n_pages, page = a.s.page, lg = a.s.page_log2, tt = a.s.tile_tokens;
     ServeArrays w;
     serve_arrays(a.s, t.work, &w);
     if (threadIdx.x == 0) s_taken = s_refused = 0;
@@ -122,105 +156,108 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
         run[1] += max(x.need - x.held, 0);
         run[2] += max(x.held - x.need, 0);
     }
-    block_scan(run, all, scan_buf);
+    block_scan(run, all, u.scan);
     int taken = 0, n_refused = 0;
-    long long blocks[1] = {0}, all_blocks[1];
+    // Blocks of a request that has rows to see them; a refused one has an empty block, so that every tile has a
+    // step.  And their steps, tile by tile: all blocks in the last of its tiles (and, not causal, in all of
+    // them); causal, in the tiles before, up to the tile's last row.
+    auto blocks_of = [&](int rows, int L, bool no) { return rows == 0 ? 0 : no ? 1 : (L + rows + kServeBlock - 1) / kServeBlock; };
+    auto steps_of = [&](int n_blocks, int row0, int rows, int L, bool no, int tiles) {  // of its first `tiles` tiles
+        if (rows == 0) return 0ll;
+        const int first = row0 / tt, whole = (row0 + rows - 1) / tt - first;  // tiles but the last
+        if (!a.causal || no) return static_cast<long long>(n_blocks) * min(tiles, whole + 1);
+        const long long seen = static_cast<long long>(L) - row0 + static_cast<long long>(first + 1) * tt;  // keys, first tile
+        return floor_sum(min(tiles, whole), kServeBlock, tt, seen + kServeBlock - 1) + (tiles > whole ? n_blocks : 0);
+    };
+    long long more[2] = {0, 0}, all_more[2];
     for (int b = b0; b < b1; ++b) {
         const Wants x = wants(a, b);
-        const int grow = max(x.need - x.held, 0);
-        first_row[b] = clip(run[0]);
-        first_grow[b] = clip(run[1]);
-        first_shrink[b] = clip(run[2]);
-        run[0] += x.rows;
+        const int grow = max(x.need - x.held, 0), L = __ldg(a.len + b);
+        u.row[b] = clip(run[0]);
+        u.grow[b] = clip(run[1]);
+        u.shrink[b] = clip(run[2]);
+        u.len[b] = L;
+        u.held[b] = x.held;
         run[1] += grow;
-        run[2] += max(x.held - x.need, 0);
         const bool no = x.bad || (grow > 0 && run[1] > free_n);
         if (x.state) bits |= DLLM_SERVE_STATE;
         else if (x.bad) bits |= DLLM_SERVE_LENGTHS;
         else if (no) bits |= DLLM_SERVE_PAGES;
         if (!no && grow > 0) taken = max(taken, static_cast<int>(run[1]));
         n_refused += no;
-        refused[b] = no;
-        // a request without new tokens has no rows to see its keys
-        if (!no && x.rows > 0) blocks[0] += (__ldg(a.len + b) + x.rows + kServeBlock - 1) / kServeBlock;
+        u.refused[b] = no;
+        const int n = blocks_of(x.rows, L, no);
+        more[0] += n;
+        more[1] += steps_of(n, u.row[b], x.rows, L, no, kMost);
+        run[0] += x.rows;
+        run[2] += max(x.held - x.need, 0);
     }
     if (taken) atomicMax(&s_taken, taken);
     if (n_refused) atomicAdd(&s_refused, n_refused);
-    block_scan(blocks, all_blocks, scan_buf);
-    if (all_blocks[0] > a.s.max_blocks) bits |= DLLM_SERVE_STATE;  // more keys than the pool has places
+    block_scan(more, all_more, u.scan);
     for (int b = b0; b < b1; ++b) {
-        first_block[b] = static_cast<int>(min(blocks[0], static_cast<long long>(a.s.max_blocks)));
-        const Wants x = wants(a, b);
-        if (!refused[b] && x.rows > 0) blocks[0] += (__ldg(a.len + b) + x.rows + kServeBlock - 1) / kServeBlock;
+        u.block[b] = clip(more[0]);
+        u.steps[b] = more[1];
+        const int rows = max(__ldg(a.q_len + b), 0), n = blocks_of(rows, u.len[b], u.refused[b]);
+        more[0] += n;
+        more[1] += steps_of(n, u.row[b], rows, u.len[b], u.refused[b], kMost);
     }
     if (threadIdx.x == 0) {
-        first_row[B] = clip(all[0]);
-        first_grow[B] = clip(all[1]);
-        first_shrink[B] = clip(all[2]);
-        first_block[B] = static_cast<int>(min(all_blocks[0], static_cast<long long>(a.s.max_blocks)));
+        u.row[B] = clip(all[0]);
+        u.grow[B] = clip(all[1]);
+        u.shrink[B] = clip(all[2]);
+        u.block[B] = clip(all_more[0]);
+        u.steps[B] = all_more[1];
     }
     __syncthreads();
     taken = s_taken;
-    const int given = min(first_shrink[B], n_pages), n_blocks = first_block[B];
-    const int rows = min(first_row[B], a.rows);
+    const int given = min(u.shrink[B], n_pages), rows = min(u.row[B], a.rows);
     if (all[0] > a.rows) bits |= DLLM_SERVE_ROWS;
+    const bool fits = all_more[0] <= a.s.max_blocks;  // else there are more keys than the pool has places: no work list
+    if (!fits) bits |= DLLM_SERVE_STATE;
+    const int n_blocks = fits ? u.block[B] : 0, tiles = fits ? (rows + tt - 1) / tt : 0;
+    const int pb = (a.prefix_len + kServeBlock - 1) / kServeBlock;
 
     // page idx of request b after the plan (b not refused, idx below its need)
     auto page_of = [&](int b, int idx) {
-        const int h = t.held[b];
+        const int h = u.held[b];
         if (idx < h) return t.table[static_cast<size_t>(b) * a.s.max_pages + idx];
-        return t.ring[(static_cast<unsigned>(head) + first_grow[b] + (idx - h)) % static_cast<unsigned>(n_pages)];
+        return t.ring[(static_cast<unsigned>(head) + u.grow[b] + (idx - h)) % static_cast<unsigned>(n_pages)];
+    };
+    // steps of a K/V head's tiles before tile i
+    auto cum = [&](int i) {
+        const long long own = static_cast<long long>(i) * tt;
+        long long n = static_cast<long long>(i) * pb;
+        if (own >= u.row[B]) return n + u.steps[B];
+        const int b = find(u.row, B, static_cast<int>(own));
+        return n + u.steps[b] + steps_of(u.block[b + 1] - u.block[b], u.row[b], u.row[b + 1] - u.row[b], u.len[b], u.refused[b],
+                                         i - u.row[b] / tt);
     };
 
     if (blockIdx.x == 0) {
-        // -------------------------------------------- row starts, key counts, the attention's work
+        // -------------------------------------------- row starts, key counts, the CTAs' runs
         for (int b = threadIdx.x; b <= B; b += kThreads) {
-            t.row_start[b] = first_row[b];
-            if (b < B) t.n_keys[b] = refused[b] ? 0 : __ldg(a.len + b) + __ldg(a.q_len + b);
+            t.row_start[b] = u.row[b];
+            if (b < B) t.n_keys[b] = u.refused[b] ? 0 : u.len[b] + __ldg(a.q_len + b);
         }
-        const int tt = a.s.tile_tokens, tiles = (rows + tt - 1) / tt;
-        const int pb = (a.prefix_len + kServeBlock - 1) / kServeBlock;
-        long long carry = 0;
-        for (int base = 0; base < tiles; base += kThreads) {
-            const int tile = base + threadIdx.x;
-            long long steps[1] = {0}, sum[1];
-            if (tile < tiles) {
-                const int tok0 = tile * tt, tok1 = min(tok0 + tt, rows) - 1;
-                const int r0 = find(first_row, B, tok0), r1 = find(first_row, B, tok1);
-                const int s0 = first_block[r0];
-                int s1 = first_block[r1 + 1];
-                if (a.causal) {  // the tile's last row sees no further
-                    const int seen = __ldg(a.len + r1) + tok1 - first_row[r1] + 1;
-                    s1 = min(s1, first_block[r1] + (max(seen, 0) + kServeBlock - 1) / kServeBlock);
-                }
-                steps[0] = pb + s1 - s0;
-                w.tile_first[tile] = steps[0] ? s0 : -1;
-                steps[0] = max(steps[0], 1ll);
-            }
-            block_scan(steps, sum, scan_buf);
-            if (tile < tiles) {
-                w.tile_cum[tile] = carry + steps[0];
-                if (tiles <= kThreads) tile_sum[tile] = steps[0];
-            }
-            carry += sum[0];
-        }
-        if (threadIdx.x == 0) {
-            w.tile_cum[tiles] = carry;
-            tile_sum[min(tiles, kThreads)] = carry;
-        }
-        __syncthreads();
-        const long long total = carry * a.s.Hkv;
+        const long long total = tiles ? cum(tiles) * a.s.Hkv : 0;
         const int ctas = static_cast<int>(min((total + 1) / 2, static_cast<long long>(a.max_ctas)));
         for (int c = threadIdx.x; c < kServeCtas; c += kThreads) {
             int4 d = make_int4(0, 0, 0, 0);
             if (c < ctas) {
-                const long long x = c * total / ctas, y = (c + 1) * total / ctas;
-                const long long* sums = tiles <= kThreads ? tile_sum : w.tile_cum;
-                // tile: the one whose units (all heads) hold step x
-                d.x = find(sums, tiles, x / a.s.Hkv);
-                const long long steps = sums[d.x + 1] - sums[d.x], in = x - sums[d.x] * a.s.Hkv;
-                d.y = static_cast<int>(in / steps);
-                d.z = static_cast<int>(in - d.y * steps);
+                const long long x = c * total / ctas, y = (c + 1) * total / ctas, own = x / a.s.Hkv;
+                int lo = 0, hi = tiles;  // the tile whose units (all heads) hold step x
+                long long at = 0, end = total / a.s.Hkv;
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    const long long v = cum(mid);
+                    if (v <= own) lo = mid, at = v;
+                    else hi = mid, end = v;
+                }
+                const long long in = x - at * a.s.Hkv;
+                d.x = lo;
+                d.y = static_cast<int>(in / (end - at));
+                d.z = static_cast<int>(in - d.y * (end - at));
                 d.w = static_cast<int>(y - x);
             }
             w.cta[c] = d;
@@ -231,24 +268,22 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
             w.head->prefix_len = a.prefix_len;
             w.head->prefix_blocks = pb;
             w.head->tiles = tiles;
-            w.head->rows = rows;
+            w.head->rows = fits ? rows : 0;
             w.head->total = total;
             serve_key(a.s, w.head->shape);
             t.status[1] = s_refused;
             t.status[2] = taken;
             t.status[3] = given;
         }
-    }
-    if (blockIdx.x > 0 || gridDim.x == 1) {
-        // -------------------------------------------- rows, pages, blocks
-        const int first = (gridDim.x == 1 ? 0 : blockIdx.x - 1) * kThreads + threadIdx.x;
-        const int step = (gridDim.x == 1 ? 1 : gridDim.x - 1) * kThreads;
+    } else {
+        // -------------------------------------------- rows, pages, blocks, tiles
+        const int first = (blockIdx.x - 1) * kThreads + threadIdx.x, step = (gridDim.x - 1) * kThreads;
         for (int r = first; r < a.rows; r += step) {
             int slot = -1, pos = 0, req = -1;
             if (r < rows) {
-                req = find(first_row, B, r);
-                if (!refused[req]) {
-                    const int at = __ldg(a.len + req) + r - first_row[req];
+                req = find(u.row, B, r);
+                if (!u.refused[req]) {
+                    const int at = u.len[req] + r - u.row[req];
                     const int p = page_of(req, at >> lg);
                     if (p >= 0 && p < n_pages) slot = p * page + (at & (page - 1));
                     else bits |= DLLM_SERVE_STATE;
@@ -260,33 +295,38 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
             t.req[r] = req;
         }
         for (int k = first; k < taken; k += step) {
-            const int b = find(first_grow, B, k);
-            const int idx = t.held[b] + k - first_grow[b];
+            const int b = find(u.grow, B, k);
+            const int idx = u.held[b] + k - u.grow[b];
             t.table[static_cast<size_t>(b) * a.s.max_pages + idx] =
                 t.ring[(static_cast<unsigned>(head) + k) % static_cast<unsigned>(n_pages)];
         }
         for (int k = first; k < given; k += step) {
-            const int b = find(first_shrink, B, k);
-            const int idx = wants(a, b).need + k - first_shrink[b];
+            const int b = find(u.shrink, B, k);
+            const int idx = wants(a, b).need + k - u.shrink[b];
             int* p = t.table + static_cast<size_t>(b) * a.s.max_pages + idx;
             t.ring[(static_cast<unsigned>(head) + free_n + k) % static_cast<unsigned>(n_pages)] = *p;
             *p = -1;
         }
         for (int k = first; k < n_blocks; k += step) {
-            const int b = find(first_block, B, k), key0 = (k - first_block[b]) * kServeBlock;
-            const int L = __ldg(a.len + b), q = __ldg(a.q_len + b);
-            w.info[k] = make_int4(first_row[b], first_row[b + 1], key0, L);
-            int4 p = make_int4(-1, -1, -1, -1);
-            if (page >= kServeBlock) {
-                p.x = page_of(b, key0 >> lg);
-                p.y = key0 & (page - 1);
-            } else {
-                int* pp = &p.x;
-                const int last = (L + q - 1) >> lg;
-                for (int i = 0; i < kServeBlock >> lg; ++i)
-                    if ((key0 >> lg) + i <= last) pp[i] = page_of(b, (key0 >> lg) + i);
+            const int b = find(u.block, B, k), key0 = (k - u.block[b]) * kServeBlock;
+            const int q = u.row[b + 1] - u.row[b], L = u.refused[b] ? -q : u.len[b];  // (refused: no keys)
+            w.info[k] = make_int4(u.row[b], u.row[b + 1], key0, L);
+            int4 p = make_int4(-1, page >= kServeBlock ? key0 & (page - 1) : -1, -1, -1);
+            if (!u.refused[b]) {
+                if (page >= kServeBlock) {
+                    p.x = page_of(b, key0 >> lg);
+                } else {
+                    int* pp = &p.x;
+                    const int last = (L + q - 1) >> lg;
+                    for (int i = 0; i < kServeBlock >> lg; ++i)
+                        if ((key0 >> lg) + i <= last) pp[i] = page_of(b, (key0 >> lg) + i);
+                }
             }
             w.pages[k] = p;
+        }
+        for (int k = first; k <= tiles; k += step) {
+            w.tile_cum[k] = cum(k);
+            if (k < tiles) w.tile_first[k] = u.block[find(u.row, B, k * tt)];
         }
     }
     if (bits) atomicOr(t.status, bits);
@@ -300,7 +340,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
     __syncthreads();
     if (!s_last) return;
     for (int b = threadIdx.x; b < B; b += kThreads)
-        if (!refused[b]) t.held[b] = wants(a, b).need;
+        if (!u.refused[b]) t.held[b] = wants(a, b).need;
     if (threadIdx.x == 0) {
         t.ring_pos[0] = static_cast<int>((static_cast<unsigned>(head) + taken) % static_cast<unsigned>(n_pages));
         t.ring_pos[1] = min(free_n - taken + given, n_pages);
@@ -323,10 +363,6 @@ __global__ void k_serve_reset(ServeShape s, dllm_serve_tables t) {
     if (i0 < sizeof(ServeWork) / 4) t.work[i0] = 0;
 }
 
-size_t plan_smem(int batch) {
-    return sizeof(long long) * (4 * kWarps + kThreads + 1) + sizeof(int) * 4 * (static_cast<size_t>(batch) + 1) + batch;
-}
-
 }  // namespace
 
 cudaError_t launch_serve_reset(const ServeShape& s, const dllm_serve_tables& t, cudaStream_t st) {
@@ -343,9 +379,9 @@ cudaError_t launch_serve_plan(const ServeShape& s, const dllm_serve_tables& t, c
         if (e != cudaSuccess) return e;
     }
     PlanArgs a{s, t, len, q_len, batch, rows, prefix_len, causal, 2 * sms < kServeCtas ? 2 * sms : kServeCtas};
-    // one CTA for the work list, and one for every eight items a thread of the others
+    // one CTA for the runs, and one for every two items a thread of the others
     const long long items = rows + 64ll * batch;
-    long long fill = (items + 8 * kThreads - 1) / (8 * kThreads);
+    long long fill = (items + 2 * kThreads - 1) / (2 * kThreads);
     if (fill > sms - 1) fill = sms - 1;
     if (fill < 1) fill = 1;
     k_serve_plan<<<static_cast<unsigned>(1 + fill), kThreads, plan_smem(batch), st>>>(a);

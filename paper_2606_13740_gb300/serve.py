@@ -7,6 +7,7 @@ Argument marshalling only.  Calls run on torch's current stream and do not wait;
 from __future__ import annotations
 
 import ctypes as C
+import functools
 from dataclasses import dataclass
 
 from .dllm import _check, lib
@@ -90,31 +91,26 @@ def dllm_serve_bytes(cfg: ServeConfig) -> int:
     return n.value
 
 
+@functools.cache
 def _names():
     import torch
 
     return {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 
-def _stream(device):
+@functools.cache
+def _stream_of():
+    """index of a device -> handle of torch's current stream there."""
     import torch
 
-    return torch.cuda.current_stream(device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream
 
 
-def _need(name, x, dtype, shape=None, cols=None):
-    """A CUDA tensor of a type and shape whose rows are dense."""
-    if not x.is_cuda or x.dtype != dtype:
-        raise ValueError(f"{name} must be a CUDA tensor of {dtype}, not {x.dtype} on {x.device}")
-    if shape is not None and tuple(x.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(x.shape)}")
-    if cols is not None and (x.dim() < 2 or x[0].numel() != cols):
-        raise ValueError(f"{name} must have rows of {cols} values, not shape {tuple(x.shape)}")
-    return x
-
-
-def _ptr(x):
-    return None if x is None else x.data_ptr()
+@functools.cache
+def _logits_bytes(rows, vocab):
+    n = _SZ()
+    _check(serve_lib().dllm_serve_logits_bytes(rows, vocab, C.byref(n)))
+    return n.value
 
 
 class Serve:
@@ -128,16 +124,19 @@ class Serve:
         self.cfg = cfg
         self._c = cfg.c()
         self._cp = C.byref(self._c)
-        L = serve_lib()
+        self._L = L = serve_lib()
         n = dllm_serve_bytes(cfg)
         self.buffer = torch.empty(n, dtype=torch.uint8, device=device or "cuda")
-        self.device = self.buffer.device
+        self.device, self._index = self.buffer.device, self.buffer.device.index
         self._t = dllm_serve_tables()
         self._tp = C.byref(self._t)
         self._dt = {"bf16": torch.bfloat16, "f16": torch.float16}[cfg.dtype]
-        self._kinds = _names()
-        with torch.cuda.device(self.device):
-            _check(L.dllm_serve_layout(self._cp, self.buffer.data_ptr(), self._tp, None))
+        self._i32, self._f32, self._empty, self._kinds = torch.int32, torch.float32, torch.empty, _names()
+        self._H, self._Hkv, self._hd, self._scale = cfg.n_heads, cfg.n_kv_heads, cfg.head_dim, cfg.head_dim ** -0.5
+        self._cache_shape = (cfg.n_pages, cfg.n_kv_heads, cfg.page, cfg.head_dim)
+        row = cfg.page * cfg.head_dim
+        self._cache_strides = (cfg.page_stride or cfg.n_kv_heads * row, row, cfg.head_dim, 1)
+        _check(L.dllm_serve_layout(self._cp, self.buffer.data_ptr(), self._tp, None))
         base = self.buffer.data_ptr()
 
         def view(name, *shape):
@@ -155,103 +154,105 @@ class Serve:
         self.rows = self.prefix_len = 0
         self.dllm_serve_reset()
 
+    def _stream(self):
+        return _stream_of()(self._index)
+
     def dllm_serve_reset(self):
         """Nothing held, every page free."""
-        _check(serve_lib().dllm_serve_reset(self._cp, self._tp, _stream(self.device)))
+        _check(self._L.dllm_serve_reset(self._cp, self._tp, self._stream()))
         self.rows = self.prefix_len = 0
 
     def dllm_serve_plan(self, length, q_len, rows, prefix_len=0, causal=False):
         """length, q_len: int32 CUDA tensors [batch], own positions cached and new tokens; rows: rows of the step's
         packed arrays (at least the sum of q_len, else the last are left out)."""
-        import torch
-
-        _need("length", length, torch.int32)
-        _need("q_len", q_len, torch.int32, length.shape)
-        if not (length.is_contiguous() and q_len.is_contiguous()):
-            raise ValueError("length and q_len must be contiguous")
-        _check(serve_lib().dllm_serve_plan(self._cp, self._tp, length.data_ptr(), q_len.data_ptr(), length.numel(), rows,
-                                           prefix_len, causal, _stream(self.device)))
+        i32 = self._i32
+        if (length.dtype != i32 or q_len.dtype != i32 or length.shape != q_len.shape or not length.is_cuda
+                or not q_len.is_cuda or not length.is_contiguous() or not q_len.is_contiguous()):
+            raise ValueError("length and q_len must be contiguous int32 CUDA tensors of one shape")
+        rc = self._L.dllm_serve_plan(self._cp, self._tp, length.data_ptr(), q_len.data_ptr(), length.numel(), rows,
+                                     prefix_len, causal, self._stream())
+        if rc:
+            _check(rc)
         self.rows, self.prefix_len = rows, prefix_len
 
-    def _rows(self, name, x, heads, dtype=None):
-        """x as rows of heads * head_dim values: (pointer, stride of a row)."""
-        n = heads * self.cfg.head_dim
-        if not x.is_cuda or (dtype is not None and x.dtype != dtype):
-            raise ValueError(f"{name} must be a CUDA tensor of {dtype}, not {x.dtype} on {x.device}")
-        st = x.stride()
-        if x.dim() == 2 and x.shape[1] == n and (st[1] == 1 or n == 1):
-            return x.data_ptr(), max(st[0], n) if x.shape[0] < 2 else st[0]
-        if x.dim() == 3 and x.shape[1:] == (heads, self.cfg.head_dim) and st[2] == 1 and (
-                st[1] == self.cfg.head_dim or heads == 1):
-            return x.data_ptr(), max(st[0], n) if x.shape[0] < 2 else st[0]
-        raise ValueError(f"{name} must be [rows][{n}] or [rows][{heads}][{self.cfg.head_dim}] with dense rows, "
-                         f"not shape {tuple(x.shape)} of strides {st}")
+    def _row_stride(self, name, x, heads, dtype):
+        """Elements from row to row of x: [rows][heads * head_dim] or [rows][heads][head_dim], rows dense."""
+        st, shape, hd = x.stride(), x.shape, self._hd
+        if x.dtype == dtype and x.is_cuda:
+            n = heads * hd
+            if (len(shape) == 2 and shape[1] == n and st[1] == 1) or (
+                    len(shape) == 3 and shape[1] == heads and shape[2] == hd and st[2] == 1 and (st[1] == hd or heads == 1)):
+                return st[0] if shape[0] > 1 or st[0] >= n else n
+        raise ValueError(f"{name} must be a CUDA tensor [rows][{heads * hd}] or [rows][{heads}][{hd}] of {dtype} with dense "
+                         f"rows, not {x.dtype} {tuple(shape)} of strides {st} on {x.device}")
 
     def _cache(self, name, x):
-        c = self.cfg
-        _need(name, x, self._dt, (c.n_pages, c.n_kv_heads, c.page, c.head_dim))
-        st, dense = x.stride(), c.n_kv_heads * c.page * c.head_dim
-        if st[1:] != (c.page * c.head_dim, c.head_dim, 1) or (c.n_pages > 1 and st[0] != (c.page_stride or dense)):
-            raise ValueError(f"{name}: strides {st} are not those of the config")
+        if x.dtype != self._dt or not x.is_cuda or x.shape != self._cache_shape or (
+                x.stride() != self._cache_strides and not (x.shape[0] == 1 and x.stride()[1:] == self._cache_strides[1:])):
+            raise ValueError(f"{name} must be a CUDA tensor {self._cache_shape} of {self._dt}, strides {self._cache_strides}, "
+                             f"not {tuple(x.shape)} of {x.dtype}, strides {x.stride()}")
+        return x.data_ptr()
+
+    def _vector(self, name, x, n):
+        if x is None:
+            return None
+        if x.dtype != self._f32 or x.shape != (n,) or not x.is_cuda or not x.is_contiguous():
+            raise ValueError(f"{name} must be {n} contiguous fp32 values on the GPU")
         return x.data_ptr()
 
     def dllm_serve_qk_norm_rope(self, q, k, v, theta, kc, vc, q_gain=None, k_gain=None, eps=1e-5, out=None):
         """q [rows][n_heads * head_dim], k, v [rows][n_kv_heads * head_dim] (views of one projection's output, of
         the config's dtype or fp32) -> q normalised and rotated [rows][n_heads][head_dim]; k and v go to their slots."""
-        import torch
-
-        c = self.cfg
-        rows = q.shape[0]
-        if k.shape[0] != rows or v.shape[0] != rows or k.dtype != q.dtype or v.dtype != q.dtype:
-            raise ValueError("q, k and v must have the same rows and type")
-        qp, ldq = self._rows("q", q, c.n_heads)
-        kp, ldk = self._rows("k", k, c.n_kv_heads)
-        vp, ldv = self._rows("v", v, c.n_kv_heads)
-        for name, x, n in (("theta", theta, c.head_dim // 2), ("q_gain", q_gain, c.head_dim), ("k_gain", k_gain, c.head_dim)):
-            if x is not None and (x.dtype != torch.float32 or x.shape != (n,) or not x.is_cuda or not x.is_contiguous()):
-                raise ValueError(f"{name} must be {n} contiguous fp32 values on the GPU")
+        rows, dtype, H, Hkv = q.shape[0], q.dtype, self._H, self._Hkv
+        ldq, ldk, ldv = (self._row_stride("q", q, H, dtype), self._row_stride("k", k, Hkv, dtype),
+                         self._row_stride("v", v, Hkv, dtype))
+        if k.shape[0] != rows or v.shape[0] != rows:
+            raise ValueError("q, k and v must have the same rows")
         if out is None:
-            out = torch.empty((rows, c.n_heads, c.head_dim), dtype=self._dt, device=self.device)
-        op, ld_out = self._rows("out", out, c.n_heads, self._dt)
-        if out.shape[0] != rows:
-            raise ValueError("out must have q's rows")
-        _check(serve_lib().dllm_serve_qk_norm_rope(self._cp, self._tp, qp, kp, vp, self._kinds.get(q.dtype, -1), ldq, ldk, ldv,
-                                                   _ptr(q_gain), _ptr(k_gain), eps, theta.data_ptr(), op, ld_out,
-                                                   self._cache("kc", kc), self._cache("vc", vc), rows,
-                                                   _stream(self.device)))
+            out, ld_out = self._empty((rows, H, self._hd), dtype=self._dt, device=self.device), H * self._hd
+        else:
+            ld_out = self._row_stride("out", out, H, self._dt)
+            if out.shape[0] != rows:
+                raise ValueError("out must have q's rows")
+        rc = self._L.dllm_serve_qk_norm_rope(
+            self._cp, self._tp, q.data_ptr(), k.data_ptr(), v.data_ptr(), self._kinds.get(dtype, -1), ldq, ldk, ldv,
+            self._vector("q_gain", q_gain, self._hd), self._vector("k_gain", k_gain, self._hd), eps,
+            self._vector("theta", theta, self._hd // 2), out.data_ptr(), ld_out, self._cache("kc", kc),
+            self._cache("vc", vc), rows, self._stream())
+        if rc:
+            _check(rc)
         return out
 
     def dllm_serve_attention(self, q, kc, vc, prefix_pages=None, scale=None, lse=False, out=None):
         """q [rows][n_heads][head_dim] of the plan's rows -> [rows][n_heads * head_dim] (with lse: and the
         logarithms of the softmax sums, fp32 [rows][n_heads])."""
-        import torch
-
-        c = self.cfg
-        rows, n_prefix = q.shape[0], 0
-        qp, ldq = self._rows("q", q, c.n_heads, self._dt)
+        rows, n_prefix, pages = q.shape[0], 0, None
+        ldq = self._row_stride("q", q, self._H, self._dt)
         if rows != self.rows:
             raise ValueError(f"q has {rows} rows, the plan {self.rows}")
         if prefix_pages is not None:
-            n_prefix = _need("prefix_pages", prefix_pages, torch.int32).numel()
-            if not prefix_pages.is_contiguous():
-                raise ValueError("prefix_pages must be contiguous")
-        if n_prefix * c.page < self.prefix_len:
-            raise ValueError(f"{n_prefix} prefix pages of {c.page} for a prefix of {self.prefix_len}")
+            if prefix_pages.dtype != self._i32 or not prefix_pages.is_cuda or not prefix_pages.is_contiguous():
+                raise ValueError("prefix_pages must be a contiguous int32 CUDA tensor")
+            n_prefix, pages = prefix_pages.numel(), prefix_pages.data_ptr()
+        if n_prefix * self.cfg.page < self.prefix_len:
+            raise ValueError(f"{n_prefix} prefix pages of {self.cfg.page} for a prefix of {self.prefix_len}")
         if out is None:
-            out = torch.empty((rows, c.n_heads * c.head_dim), dtype=self._dt, device=self.device)
-        elif out.numel() != rows * c.n_heads * c.head_dim or not out.is_contiguous() or out.dtype != self._dt:
+            out = self._empty((rows, self._H * self._hd), dtype=self._dt, device=self.device)
+        elif (out.numel() != rows * self._H * self._hd or not out.is_contiguous() or out.dtype != self._dt
+              or not out.is_cuda):
             raise ValueError("out must be contiguous, of q's rows and type")
-        ls = torch.empty((rows, c.n_heads), dtype=torch.float32, device=self.device) if lse else None
-        _check(serve_lib().dllm_serve_attention(self._cp, self._tp, qp, ldq, self._cache("kc", kc), self._cache("vc", vc),
-                                                _ptr(prefix_pages), n_prefix,
-                                                c.head_dim ** -0.5 if scale is None else scale, out.data_ptr(), _ptr(ls),
-                                                rows, _stream(self.device)))
+        ls = self._empty((rows, self._H), dtype=self._f32, device=self.device) if lse else None
+        rc = self._L.dllm_serve_attention(self._cp, self._tp, q.data_ptr(), ldq, self._cache("kc", kc), self._cache("vc", vc),
+                                          pages, n_prefix, self._scale if scale is None else scale, out.data_ptr(),
+                                          None if ls is None else ls.data_ptr(), rows, self._stream())
+        if rc:
+            _check(rc)
         return (out, ls) if lse else out
 
     def dllm_serve_check(self):
         """Waits for the stream; raises DllmError for what the kernels found wrong since the last check."""
         bits = _I()
-        _check(serve_lib().dllm_serve_check(self._tp, C.byref(bits), _stream(self.device)))
+        _check(self._L.dllm_serve_check(self._tp, C.byref(bits), self._stream()))
 
 
 def dllm_serve_logits(logits, mask_id=-1, req=None, hist=None, hist_len=None, rep=None, freq=None, pres=None,
@@ -261,58 +262,53 @@ def dllm_serve_logits(logits, mask_id=-1, req=None, hist=None, hist_len=None, re
     conf, tokconf), tokconf None without cur.  out: where the processed logits go (logits itself: in place)."""
     import torch
 
-    if logits.dim() != 2 or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
+    shape, st = logits.shape, logits.stride()
+    if len(shape) != 2 or not logits.is_cuda or (shape[1] > 1 and st[1] != 1):
         raise ValueError("logits must be a CUDA tensor [rows][vocab] with dense rows")
-    rows, vocab = logits.shape
-    dev, kind = logits.device, _names().get(logits.dtype, -1)
-    a = dllm_serve_logits_args()
-    a.logits, a.ld, a.dtype, a.rows, a.vocab, a.mask_id = (logits.data_ptr(), max(logits.stride(0), vocab) if rows < 2
-                                                            else logits.stride(0), kind, rows, vocab, mask_id)
-    if out is not None:
-        if out.shape != logits.shape or out.dtype != logits.dtype or (vocab > 1 and out.stride(1) != 1):
-            raise ValueError("out must be like logits")
-        a.out, a.ld_out = out.data_ptr(), max(out.stride(0), vocab) if rows < 2 else out.stride(0)
-    i32, f32 = torch.int32, torch.float32
-    lists = [x for x in (hist, bias_ids) if x is not None]
-    n_req = lists[0].shape[0] if lists else 0
-    a.n_req = n_req
-    for name, x, dtype, shape in (
-            ("req", req, i32, (rows,)), ("hist", hist, i32, None), ("hist_len", hist_len, i32, (n_req,)),
-            ("rep", rep, f32, (n_req,)), ("freq", freq, f32, (n_req,)), ("pres", pres, f32, (n_req,)),
-            ("bias_ids", bias_ids, i32, None), ("bias", bias, f32, None if bias_ids is None else bias_ids.shape),
-            ("bias_len", bias_len, i32, (n_req,)), ("grammar", grammar, i32, None), ("grammar_row", grammar_row, i32, (rows,)),
-            ("cur", cur, i32, (rows,))):
+    rows, vocab = shape
+    i32, f32, dev = torch.int32, torch.float32, logits.device
+    n_req = hist.shape[0] if hist is not None else bias_ids.shape[0] if bias_ids is not None else 0
+
+    def at(name, x, dtype, want):
         if x is None:
-            continue
-        if x.dtype != dtype or not x.is_cuda or not x.is_contiguous() or (shape is not None and x.shape != shape):
-            raise ValueError(f"{name} must be a contiguous CUDA tensor of {dtype}" + (f" {tuple(shape)}" if shape else ""))
-        setattr(a, name, x.data_ptr())
-    for name, x in (("hist", hist), ("bias_ids", bias_ids)):
-        if x is not None and (x.dim() != 2 or x.shape[0] != n_req):
-            raise ValueError(f"{name} must be [requests][length]")
-    if req is None and n_req and n_req != rows:
-        raise ValueError("without req there is a list for each row")
-    if hist is None and (rep is not None or freq is not None or pres is not None or hist_len is not None):
-        raise ValueError("penalties come with hist")
+            return None
+        if x.dtype != dtype or x.shape != want or not x.is_cuda or not x.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous CUDA tensor of {dtype} {tuple(want)}, not {x.dtype} {tuple(x.shape)}")
+        return x.data_ptr()
+
+    hist_ld = bias_ld = n_grammar = ld_out = 0
     if hist is not None:
-        a.hist_ld = hist.shape[1]
+        hist_ld = hist.shape[-1]
+    elif rep is not None or freq is not None or pres is not None or hist_len is not None:
+        raise ValueError("penalties come with hist")
     if bias_ids is not None:
+        bias_ld = bias_ids.shape[-1]
         if bias is None:
             raise ValueError("bias_ids come with bias")
-        a.bias_ld = bias_ids.shape[1]
     if grammar is not None:
-        if grammar.dim() != 2 or grammar.shape[1] != (vocab + 31) // 32:
-            raise ValueError(f"grammar must be [masks][{(vocab + 31) // 32}]")
-        a.n_grammar = grammar.shape[0]
-    x0 = torch.empty(rows, dtype=i32, device=dev)
-    conf = torch.empty((2 if cur is not None else 1, rows), dtype=f32, device=dev)
-    a.x0, a.conf = x0.data_ptr(), conf.data_ptr()
-    if cur is not None:
-        a.tokconf = conf.data_ptr() + 4 * rows
+        n_grammar = grammar.shape[0]
+    if req is None and n_req and n_req != rows:
+        raise ValueError("without req there is a list for each row")
+    if out is not None:
+        so = out.stride()
+        if out.shape != shape or out.dtype != logits.dtype or not out.is_cuda or (vocab > 1 and so[1] != 1):
+            raise ValueError("out must be like logits")
+        ld_out = so[0] if rows > 1 else max(so[0], vocab)
     if ws is None:
-        n = _SZ()
-        _check(serve_lib().dllm_serve_logits_bytes(rows, vocab, C.byref(n)))
-        ws = torch.empty(n.value, dtype=torch.uint8, device=dev)
-    a.ws, a.ws_bytes = ws.data_ptr(), ws.numel()
-    _check(serve_lib().dllm_serve_logits(C.byref(a), _stream(dev)))
-    return x0, conf[0], conf[1] if cur is not None else None
+        ws = torch.empty(_logits_bytes(rows, vocab), dtype=torch.uint8, device=dev)
+    x0 = torch.empty(rows, dtype=i32, device=dev)
+    conf, tokconf = torch.empty((2, rows), dtype=f32, device=dev).unbind(0)
+    per_row, per_req = (rows,), (n_req,)
+    a = dllm_serve_logits_args(
+        logits.data_ptr(), None if out is None else out.data_ptr(), st[0] if rows > 1 else max(st[0], vocab), ld_out,
+        _names().get(logits.dtype, -1), rows, vocab, mask_id, n_req, at("req", req, i32, per_row),
+        at("hist", hist, i32, (n_req, hist_ld)), at("hist_len", hist_len, i32, per_req), hist_ld, at("rep", rep, f32, per_req),
+        at("freq", freq, f32, per_req), at("pres", pres, f32, per_req), at("bias_ids", bias_ids, i32, (n_req, bias_ld)),
+        at("bias", bias, f32, (n_req, bias_ld)), at("bias_len", bias_len, i32, per_req), bias_ld,
+        at("grammar", grammar, i32, (n_grammar, (vocab + 31) // 32)), at("grammar_row", grammar_row, i32, per_row), n_grammar,
+        at("cur", cur, i32, per_row), x0.data_ptr(), conf.data_ptr(), None if cur is None else tokconf.data_ptr(),
+        ws.data_ptr(), ws.numel())
+    rc = serve_lib().dllm_serve_logits(C.byref(a), _stream_of()(dev.index))
+    if rc:
+        _check(rc)
+    return x0, conf, None if cur is None else tokconf
