@@ -703,6 +703,7 @@ cudaError_t go(const ServeShape& s, const dllm_serve_tables& t, const ServeAttnA
     if (!make_tmap_16bit(&maps.q, a.q, f16, 4, qdims, qstr, qbox) || !make_tmap_16bit(&maps.k, a.kc, f16, 3, kdims, kstr, kbox) ||
         !make_tmap_16bit(&maps.v, a.vc, f16, 3, kdims, kstr, kbox))
         return cudaErrorInvalidValue;
+    // (an attribute of the function in the current device's context; a call takes about a microsecond)
     cudaError_t err = cudaFuncSetAttribute(reinterpret_cast<const void*>(k_serve_attn<HD, T>),
                                            cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<HD>);
     if (err != cudaSuccess) return err;
