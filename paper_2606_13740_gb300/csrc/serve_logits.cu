@@ -25,7 +25,7 @@ constexpr int kPiece = kGroup * kGroups;
 constexpr int kCountBits = 20;
 constexpr float kLog2e = 1.4426950408889634f;
 
-struct Part {
+struct alignas(16) Part {
     float m, s;  // largest z, sum of exp(z - m)
     int arg, pad;
 };
@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
             float best = -INFINITY, best_one = -INFINITY;
             int best_piece = -1, arg = kChunk;
 
-            // The stream: the whole pieces, without the mask id's; what is in the list is left out.
+            // The stream: the whole pieces; what is in the list is left out, and the mask id of the decision.
             const int pm = mask >= 0 && mask < n ? mask / kPiece : -1, pw = min(p1, n / kPiece);
             auto load = [&](const T* p, float (&z)[kGroups][4]) {
 #pragma unroll
@@ -252,7 +252,6 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
                 float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
                 const T* ps = src + p0 * kPiece + 4 * lane;
                 for (int q = p0; q < pw; ++q, ps += kPiece) {
-                    if (q == pm) continue;
                     float z[kGroups][4];
                     load(ps, z);
                     uint32_t todo = 0;
@@ -280,6 +279,13 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
                                 for (int i = 0; i < 4; ++i)
                                     if ((todo >> (4 * u + i)) & 1u) z[u][i] = -INFINITY;
                         }
+                    }
+                    if (q == pm) {
+#pragma unroll
+                        for (int u = 0; u < kGroups; ++u)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (mask == q * kPiece + u * kGroup + 4 * lane + i) z[u][i] = -INFINITY;
                     }
                     float mx = z[0][0];
 #pragma unroll
@@ -324,17 +330,23 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
                 if (run.above(y)) run.raise(y);
                 run.s += run.weight(y);
             };
-            auto by_ones = [&](int p) {  // a piece that is not whole, or has the mask id
-                for (int v = p * kPiece + lane; v < min(n, (p + 1) * kPiece); v += 32)
-                    if (!asks || !word[v]) one(v, Io<T>::get(src + v));
+            auto by_ones = [&](int p) {  // a piece that is not whole
+                const int end = min(n, (p + 1) * kPiece);
+                for (int v = p * kPiece + lane; v < end; v += 4 * 32) {
+                    float y[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y[i] = v + 32 * i < end ? Io<T>::get(src + v + 32 * i) : 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (v + 32 * i < end && (!asks || !word[v + 32 * i])) one(v + 32 * i, y[i]);
+                }
             };
             if (__any_sync(0xffffffffu, !run.plain())) {  // (the stream's exponents are for finite ones)
                 run = Running();
                 best = -INFINITY;
                 for (int p = p0; p < p1; ++p) by_ones(p);
-            } else {
-                if (pm >= p0 && pm < pw) by_ones(pm);
-                if (pw < p1) by_ones(pw);
+            } else if (pw < p1) {
+                by_ones(pw);
             }
             // the current id, if the stream had it
             if (lane == 0 && cur >= p0 * kPiece && cur < min(n, p1 * kPiece) && !(asks && word[cur]))
@@ -380,7 +392,10 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
                 for (int u = kGroups - 1; u >= 0; --u)
 #pragma unroll
                     for (int i = 3; i >= 0; --i)
-                        if (z[u][i] == m && !((todo >> (4 * u + i)) & 1u)) arg = min(arg, best_piece * kPiece + 4 * lane + u * kGroup + i);
+                        {
+                        const int v = best_piece * kPiece + 4 * lane + u * kGroup + i;
+                        if (z[u][i] == m && v != mask && !((todo >> (4 * u + i)) & 1u)) arg = min(arg, v);
+                    }
             }
             __syncwarp();
             arg = __reduce_min_sync(0xffffffffu, arg);
@@ -405,12 +420,19 @@ __global__ void __launch_bounds__(128) k_merge(const __grid_constant__ dllm_serv
     if (row >= a.rows) return;
     float m = -INFINITY, s = 0.0f;
     int arg = a.vocab;
-    for (int i = lane; i < parts; i += 32) {
-        const Part p = part[static_cast<size_t>(row) * parts + i];
-        const float mx = fmaxf(m, p.m);
-        s = s * (m == mx ? 1.0f : exp_below(m, mx)) + p.s * (p.m == mx ? 1.0f : exp_below(p.m, mx));
-        if (p.m > m) arg = p.arg;
-        m = mx;
+    constexpr int kAtOnce = 8;
+    for (int i0 = lane; i0 < parts; i0 += 32 * kAtOnce) {
+        Part p[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+            p[k] = i0 + 32 * k < parts ? part[static_cast<size_t>(row) * parts + i0 + 32 * k] : Part{-INFINITY, 0.0f, 0, 0};
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const float mx = fmaxf(m, p[k].m);
+            s = s * (m == mx ? 1.0f : exp_below(m, mx)) + p[k].s * (p[k].m == mx ? 1.0f : exp_below(p[k].m, mx));
+            if (p[k].m > m) arg = p[k].arg;
+            m = mx;
+        }
     }
 #pragma unroll
     for (int d = 16; d; d /= 2) {
