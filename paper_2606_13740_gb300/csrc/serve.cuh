@@ -63,6 +63,8 @@ __device__ inline bool serve_same_shape(const ServeShape& s, const ServeWork& w)
 
 struct ServeArrays {
     ServeWork* head;
+    int4* join;           // [kServeCtas]: where a CTA's run ends inside a unit that begins in it: the unit's tile and K/V
+                          // head, and its first and last CTA; else last < first
     int4* cta;            // [kServeCtas]: tile, K/V head, step within the unit, number of steps
     int4* info;           // [max_blocks]: first and last + 1 row of the request, the block's first key, n_keys - rows
     int4* pages;          // [max_blocks]: up to four pages (page < 64), or page and first place in it
@@ -79,6 +81,8 @@ __host__ __device__ inline size_t serve_arrays(const ServeShape& s, void* base, 
     ServeArrays r;
     r.head = reinterpret_cast<ServeWork*>(b + at);
     at += serve_round(sizeof(ServeWork));
+    r.join = reinterpret_cast<int4*>(b + at);
+    at += serve_round(sizeof(int4) * kServeCtas);
     r.cta = reinterpret_cast<int4*>(b + at);
     at += serve_round(sizeof(int4) * kServeCtas);
     r.info = reinterpret_cast<int4*>(b + at);

@@ -606,10 +606,10 @@ __global__ void __launch_bounds__(kThreads, 2)
 }
 
 // Joins the parts of units that several CTAs share, in the order of their keys: a thread a row and 16
-// features.  The blocks of CTA c take the unit that its run begins in, if it begins inside one and is the
-// second of its CTAs.  A part is its CTA's first (the unit begins before its run) or its last.  (Joined by the
-// CTA that stores the last part instead, one warp reads what here all SMs share: 96 tokens under 8001 keys
-// 45 -> 74 us.)
+// features, the blocks of CTA c for the unit that begins in its run and ends in another's.  A part is its CTA's
+// first (the unit begins before its run) or its last.  Bound by the trips to L2 that depend on one another: the
+// unit, the rows' maxima and sums, the parts.  (Joined by the warp that stores the last part instead, one SM's
+// loads in flight take longer than this launch: 96 tokens under 8001 keys 41 -> 71 us.)
 template <int HD, typename T>
 __global__ void __launch_bounds__(kServeRows) k_serve_join(const __grid_constant__ ServeShape s,
                                                            const __grid_constant__ dllm_serve_tables t,
@@ -617,22 +617,12 @@ __global__ void __launch_bounds__(kServeRows) k_serve_join(const __grid_constant
     constexpr int kBatch = 4;  // parts whose loads are in flight together
     ServeArrays w;
     serve_arrays(s, t.work, &w);
-    const int c = blockIdx.x + 1, r = threadIdx.x, f0 = static_cast<int>(blockIdx.y) * 16;
-    const bool same = serve_same_shape(s, *w.head);
-    const int rows = same ? min(w.head->rows, a.rows) : 0, ctas = same ? w.head->ctas : 0;
-    const int4 d = c < ctas ? __ldg(w.cta + c) : make_int4(0, 0, 0, 0);
-    int first = 0, last = 0;
-    bool mine = d.z > 0;
-    if (mine) {
-        const long long total = w.head->total, c0 = w.tile_cum[d.x], steps = w.tile_cum[d.x + 1] - c0;
-        const long long x0 = c0 * s.Hkv + d.y * steps, x1 = x0 + steps;
-        // the CTA that holds step x: the last whose run begins at or before it
-        first = static_cast<int>(((x0 + 1) * ctas - 1) / total);
-        last = static_cast<int>((x1 * ctas - 1) / total);
-        mine = first == c - 1;
-    }
+    const int r = threadIdx.x, f0 = static_cast<int>(blockIdx.y) * 16;
+    const int4 d = __ldg(w.join + blockIdx.x);
+    const int first = d.z, last = d.w;
     const int tok_off = r / s.G, g = r - tok_off * s.G, n = d.x * s.tile_tokens + tok_off;
-    mine = mine && tok_off < s.tile_tokens && n < rows;
+    const bool mine = last > first && static_cast<int>(blockIdx.x) < w.head->ctas && serve_same_shape(s, *w.head) &&
+                      tok_off < s.tile_tokens && n < min(w.head->rows, a.rows);
     pdl_wait();
     if (!mine) return;
     const float2* ml = reinterpret_cast<const float2*>(t.partials + static_cast<size_t>(2 * kServeCtas) * kServeRows * HD) + r;

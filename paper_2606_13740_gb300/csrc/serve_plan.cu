@@ -244,6 +244,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
         const int ctas = static_cast<int>(min((total + 1) / 2, static_cast<long long>(a.max_ctas)));
         for (int c = threadIdx.x; c < kServeCtas; c += kThreads) {
             int4 d = make_int4(0, 0, 0, 0);
+            long long d_steps = 0;  // of the unit that the run begins in
             if (c < ctas) {
                 const long long x = c * total / ctas, y = (c + 1) * total / ctas, own = x / a.s.Hkv;
                 int lo = 0, hi = tiles;  // the tile whose units (all heads) hold step x
@@ -259,9 +260,22 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
                 d.y = static_cast<int>(in / (end - at));
                 d.z = static_cast<int>(in - d.y * (end - at));
                 d.w = static_cast<int>(y - x);
+                d_steps = end - at;
             }
             w.cta[c] = d;
+            // a run that begins inside a unit is the second of the unit's, or a later one
+            if (c > 0) {
+                int4 join = make_int4(0, 0, 0, -1);
+                if (d.z > 0) {
+                    const long long x0 = c * total / ctas - d.z, x1 = x0 + d_steps;
+                    // the CTA that holds step x: the last whose run begins at or before it
+                    join = make_int4(d.x, d.y, static_cast<int>(((x0 + 1) * ctas - 1) / total), static_cast<int>((x1 * ctas - 1) / total));
+                    if (join.z != c - 1) join.w = -1;
+                }
+                w.join[c - 1] = join;
+            }
         }
+        if (threadIdx.x == 0) w.join[kServeCtas - 1] = make_int4(0, 0, 0, -1);
         if (threadIdx.x == 0) {
             w.head->ctas = ctas;
             w.head->causal = a.causal;
