@@ -12,8 +12,9 @@
 //   S_j = Q K_j^T         tcgen05.mma, Q and K_j in shared memory (K-major), S_j in tensor memory
 //   P_j = exp2(S_j - m)   one thread a query row; P_j (16 bit) written back over S_j
 //   O  += P_j V_j         tcgen05.mma, P_j from tensor memory, V_j in shared memory (MN-major)
-// The running maximum m moves only when a block's maximum exceeds it by more than 8 (log2 units); only then
-// are O and the row's sum rescaled, so P stays below 2^8.  P is rounded to the cache's type, as the tensor
+// The running maximum m is the first block's, and moves only where a block's sum of P passes 2^12 (no maximum is
+// looked for otherwise); only then are O and the row's sum rescaled.  P, a floating-point number, loses nothing by
+// being larger than 1, and stays far below what f16 holds.  P is rounded to the cache's type, as the tensor
 // cores take it; the sum is of the unrounded values.  Warps 0-3: softmax and output (a thread a row); warps 4
 // and 7: TMA loads of Q and K, and of V, a box a page and 64 features; warps 5 and 6: the MMAs of S and of
 // P V.  (With one warp for the loads and one for the MMAs each spent 2000 cycles a step on them, twice what
@@ -29,6 +30,7 @@ constexpr int kThreads = 256;
 constexpr int kHalfQ = kServeRows * 128;    // bytes of 64 features of the Q tile
 constexpr int kHalfKV = kServeBlock * 128;  // and of a K or V block
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kSumMax = 4096.0f;  // of a row's P in a block, before its m moves
 
 template <int HD>
 constexpr int kStages = HD == 128 ? 2 : 4;  // K/V blocks in flight, two CTAs an SM
@@ -115,6 +117,19 @@ __device__ __forceinline__ void st_32b(void* p, const uint32_t* v) {
                  "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                  : "memory");
 }
+// 16 registers per thread -> its lane, 16 columns; tmem_wait_st waits for all of a warp's stores
+__device__ __forceinline__ void tmem_st_32x16_async(uint32_t taddr, const float* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+        "%15, %16};" ::"r"(taddr),
+        "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])),
+        "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])),
+        "r"(__float_as_uint(v[8])), "r"(__float_as_uint(v[9])), "r"(__float_as_uint(v[10])),
+        "r"(__float_as_uint(v[11])), "r"(__float_as_uint(v[12])), "r"(__float_as_uint(v[13])),
+        "r"(__float_as_uint(v[14])), "r"(__float_as_uint(v[15]))
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // 2^x by the special function unit; below 2^-126: 0
 __device__ __forceinline__ float ex2(float x) {
     float r;
@@ -485,51 +500,59 @@ __global__ void __launch_bounds__(kThreads, 2)
                         for (int k = 0; k < 64; ++k)
                             if (k >= seen) v[k] = -INFINITY;
                     }
-                    float mx;
-                    {
+                    // P and its sum with the m there is; a row whose m is too small for the block, or not yet there, takes
+                    // the block's maximum, and the warp makes P again
+                    float sum = 0.0f;
+                    auto weigh = [&] {
+                        const float ref = m == -INFINITY ? 0.0f : -m;
+                        const float2 sl = make_float2(sl2, sl2), nm = make_float2(ref, ref);
+                        float2 ls[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float pk[16];
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) {
+                                float2 e = fma2(make_float2(v[32 * h + 2 * k], v[32 * h + 2 * k + 1]), sl, nm);
+                                e.x = ex2(e.x);
+                                e.y = ex2(e.y);
+                                ls[k & 1] = add2(ls[k & 1], e);
+                                pk[k] = __uint_as_float(Half2<T>::pack(e.x, e.y));
+                            }
+                            tmem_st_32x16_async(ts + static_cast<uint32_t>(16 * h), pk);
+                        }
+                        sum = (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
+                    };
+                    weigh();
+                    const bool redo = live && (m == -INFINITY ? seen > 0 : !(sum <= kSumMax));
+                    if (__any_sync(0xffffffffu, redo)) {
                         float mi[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-                        for (int k = 4; k < 64; k += 8) {
+                        for (int k = 4; k < 64; k += 4) {
 #pragma unroll
-                            for (int u = 0; u < 4; ++u)
-                                mi[u] = k + 4 < 64 ? fmaxf(fmaxf(mi[u], v[k + u]), v[k + 4 + u]) : fmaxf(mi[u], v[k + u]);
+                            for (int u = 0; u < 4; ++u) mi[u] = fmaxf(mi[u], v[k + u]);
                         }
-                        mx = fmaxf(fmaxf(mi[0], mi[1]), fmaxf(mi[2], mi[3])) * sl2;
-                    }
-                    const bool up = live && mx > m + 8.0f;  // (m = -inf: the row's first keys)
-                    if (__any_sync(0xffffffffu, up)) {
+                        const float mx = fmaxf(fmaxf(mi[0], mi[1]), fmaxf(mi[2], mi[3])) * sl2;
+                        const bool up = redo && mx > m;
                         if (__any_sync(0xffffffffu, up && m != -INFINITY)) {
                             ok = wait(&pvdone[(j - 1) % 2], static_cast<uint32_t>(((j - 1) / 2) & 1));
                             if (!ok) break;
                             tc_fence_after();
                             const float al = up && m != -INFINITY ? ex2(m - mx) : 1.0f;
-                            float o[32];
+                            float o[16];
 #pragma unroll 1
-                            for (int c = 0; c < HD; c += 32) {
-                                tmem_ld_32x32(t_o + static_cast<uint32_t>(c), o);
+                            for (int c = 0; c < HD; c += 16) {
+                                tmem_ld_32x16(t_o + static_cast<uint32_t>(c), o);
 #pragma unroll
-                                for (int k = 0; k < 32; ++k) o[k] *= al;
-                                tmem_st_32x32(t_o + static_cast<uint32_t>(c), o);
+                                for (int k = 0; k < 16; ++k) o[k] *= al;
+                                tmem_st_32x16(t_o + static_cast<uint32_t>(c), o);
                             }
                             l *= al;
                         }
                         if (up) m = mx;
+                        weigh();
                     }
-                    const float ref = m == -INFINITY ? 0.0f : -m;
-                    uint32_t pk[32];
-                    float2 ls[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-                    const float2 sl = make_float2(sl2, sl2), nm = make_float2(ref, ref);
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        float2 e = fma2(make_float2(v[2 * k], v[2 * k + 1]), sl, nm);
-                        e.x = ex2(e.x);
-                        e.y = ex2(e.y);
-                        ls[k & 1] = add2(ls[k & 1], e);
-                        pk[k] = Half2<T>::pack(e.x, e.y);
-                    }
-                    const float sum = (ls[0].x + ls[0].y) + (ls[1].x + ls[1].y);
                     if (live) l += sum;
-                    tmem_st_32u(ts, pk);
+                    tmem_wait_st();
                 } else if (any_live) {
                     // rows of the block's request, all before its keys: nothing, but their lanes do take part
                     uint32_t zero[32];
