@@ -68,8 +68,7 @@ struct ServeArrays {
     int4* cta;            // [kServeCtas]: tile, K/V head, step within the unit, number of steps
     int4* info;           // [max_blocks]: first and last + 1 row of the request, the block's first key, n_keys - rows
     int4* pages;          // [max_blocks]: up to four pages (page < 64), or page and first place in it
-    long long* tile_cum;  // [max_tiles + 1]: steps of a K/V head's tiles before this one
-    int* tile_first;      // [max_tiles]: its first own block
+    int2* tile;           // [max_tiles]: its first own block, its steps
 };
 
 __host__ __device__ inline size_t serve_round(size_t n) { return (n + 255) / 256 * 256; }
@@ -89,10 +88,8 @@ __host__ __device__ inline size_t serve_arrays(const ServeShape& s, void* base, 
     at += serve_round(sizeof(int4) * s.max_blocks);
     r.pages = reinterpret_cast<int4*>(b + at);
     at += serve_round(sizeof(int4) * s.max_blocks);
-    r.tile_cum = reinterpret_cast<long long*>(b + at);
-    at += serve_round(sizeof(long long) * (s.max_tiles + 1));
-    r.tile_first = reinterpret_cast<int*>(b + at);
-    at += serve_round(sizeof(int) * s.max_tiles);
+    r.tile = reinterpret_cast<int2*>(b + at);
+    at += serve_round(sizeof(int2) * s.max_tiles);
     if (out) *out = r;
     return at;
 }
@@ -118,6 +115,23 @@ struct Half2<__half> {
     }
     static __device__ __forceinline__ float2 unpack(uint32_t u) { return __half22float2(*reinterpret_cast<__half2*>(&u)); }
 };
+
+// A launch that begins while the one before it in the stream ends: the kernel calls pdl_wait before it reads or
+// writes anything that another launch may have to do with.
+template <typename... P, typename... A>
+cudaError_t serve_launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
 
 cudaError_t launch_serve_reset(const ServeShape& s, const dllm_serve_tables& t, cudaStream_t st);
 cudaError_t launch_serve_plan(const ServeShape& s, const dllm_serve_tables& t, const int* len, const int* q_len,

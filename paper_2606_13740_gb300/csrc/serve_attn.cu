@@ -146,30 +146,26 @@ __device__ __forceinline__ uint32_t bit_run(int lo, int hi) {
 
 // One CTA's run of steps, unit by unit: the same walk in every role.
 struct Walk {
-    const ServeArrays& w;
-    int Hkv, tile, hk, step, left;
-    int n, own0, own1;    // steps of the current segment; first own block of the tile and of the next one
-    long long first, next, after;  // the tile's place in the sums, and the ends of it and of the next tile
-    __device__ Walk(const ServeArrays& w_, int Hkv_, int cta) : w(w_), Hkv(Hkv_) {
-        const int4 d = __ldg(w.cta + cta);
+    const int2* tiles;
+    int n_tiles, Hkv, tile, hk, step, left;
+    int n, own0, steps;  // steps of the current segment; the tile's first own block, its unit's steps
+    int2 next;           // of the next tile, asked for a unit ahead
+    __device__ Walk(const ServeArrays& w, int Hkv_, int cta) : tiles(w.tile), n_tiles(w.head->tiles), Hkv(Hkv_) {
+        const int4 d = w.cta[cta];
         tile = d.x;
         hk = d.y;
         step = d.z;
         left = d.w;
-        first = __ldg(w.tile_cum + tile);
-        next = __ldg(w.tile_cum + tile + 1);
-        own0 = __ldg(w.tile_first + tile);
-        look();
-        n = min(left, steps() - step);
+        next = tiles[tile];
+        enter();
+        n = min(left, steps - step);
     }
-    // the next tile's figures, which the walk comes to a unit later
-    __device__ void look() {
-        const int t = min(tile + 1, w.head->tiles - 1);
-        after = __ldg(w.tile_cum + t + 1);
-        own1 = __ldg(w.tile_first + t);
+    __device__ void enter() {
+        own0 = next.x;
+        steps = next.y;
+        next = tiles[min(tile + 1, n_tiles - 1)];
     }
-    __device__ int steps() const { return static_cast<int>(next - first); }
-    __device__ bool whole() const { return step == 0 && n == steps(); }
+    __device__ bool whole() const { return step == 0 && n == steps; }
     // to the next segment; false: that was the last
     __device__ bool advance() {
         left -= n;
@@ -178,12 +174,9 @@ struct Walk {
         if (++hk == Hkv) {
             hk = 0;
             ++tile;
-            first = next;
-            next = after;
-            own0 = own1;
-            look();
+            enter();
         }
-        n = min(left, steps());
+        n = min(left, steps);
         return n > 0;
     }
 };
@@ -197,17 +190,6 @@ __global__ void __launch_bounds__(kThreads, 2)
     ServeArrays w;
     serve_arrays(s, t.work, &w);
     const int cta = blockIdx.x;
-    const bool same = serve_same_shape(s, *w.head);  // else the plan of another config, or none
-    const int rows = same ? min(w.head->rows, a.rows) : 0, ctas = same ? w.head->ctas : 0;
-    if (!same && w.head->ctas && threadIdx.x == 0 && cta == 0) atomicOr(t.status, DLLM_SERVE_STATE);
-    // rows that are padding
-    for (long long i = static_cast<long long>(rows) * s.H * (HD / 8) + static_cast<long long>(cta) * kThreads + threadIdx.x;
-         i < static_cast<long long>(a.rows) * s.H * (HD / 8); i += static_cast<long long>(gridDim.x) * kThreads) {
-        reinterpret_cast<uint4*>(a.out)[i] = make_uint4(0, 0, 0, 0);
-        if (a.lse && i % (HD / 8) == 0) a.lse[i / (HD / 8)] = -INFINITY;
-    }
-    if (cta >= ctas) return;
-
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t *sQ = smem, *sK = sQ + kQ, *sV = sK + NB * kKV;
@@ -217,7 +199,6 @@ __global__ void __launch_bounds__(kThreads, 2)
     uint64_t *kfull = sy.kfull, *vfull = sy.vfull, *kempty = sy.kempty, *vempty = sy.vempty;
     int& s_abort = sy.abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int prefix_blocks = w.head->prefix_blocks, prefix_len = w.head->prefix_len;
 
     if (threadIdx.x == 0) {
         mbar_init(&qfull, 1);
@@ -252,7 +233,30 @@ __global__ void __launch_bounds__(kThreads, 2)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sy.tmem;
+    if (threadIdx.x == 0) {
+        tma_prefetch_desc(&maps.q);
+        tma_prefetch_desc(&maps.k);
+        tma_prefetch_desc(&maps.v);
+    }
+    // All before this may run while the launch before ends; from here on data and the plan are read (by plain loads:
+    // read-only ones need not stay behind the wait).
+    pdl_wait();
     pdl_launch_dependents();
+    const bool same = serve_same_shape(s, *w.head);  // else the plan of another config, or none
+    const int rows = same ? min(w.head->rows, a.rows) : 0, ctas = same ? w.head->ctas : 0;
+    const int prefix_blocks = w.head->prefix_blocks, prefix_len = w.head->prefix_len;
+    if (!same && w.head->ctas && threadIdx.x == 0 && cta == 0) atomicOr(t.status, DLLM_SERVE_STATE);
+    // rows that are padding
+    for (long long i = static_cast<long long>(rows) * s.H * (HD / 8) + static_cast<long long>(cta) * kThreads + threadIdx.x;
+         i < static_cast<long long>(a.rows) * s.H * (HD / 8); i += static_cast<long long>(gridDim.x) * kThreads) {
+        reinterpret_cast<uint4*>(a.out)[i] = make_uint4(0, 0, 0, 0);
+        if (a.lse && i % (HD / 8) == 0) a.lse[i / (HD / 8)] = -INFINITY;
+    }
+    if (cta >= ctas) {  // (the whole CTA)
+        __syncthreads();
+        if (warp == 4) tmem_dealloc(tmem, 256);
+        return;
+    }
 
     // The load and MMA warps run their loops whole, the outcomes of their waits voted, and one elected lane
     // issues.  Barrier phases count the steps j of the whole run, across its segments.
@@ -264,10 +268,6 @@ __global__ void __launch_bounds__(kThreads, 2)
         // ------------------------------------------------ loads
         const bool leader = elect_one(), is_k = warp == 4;
         const CUtensorMap* tm = is_k ? &maps.k : &maps.v;
-        if (leader) {
-            if (is_k) tma_prefetch_desc(&maps.q);
-            tma_prefetch_desc(tm);
-        }
         const uint64_t once = policy_evict_first(), often = policy_evict_last();
         const int lg = s.page_log2, page = s.page, boxes = page < kServeBlock ? kServeBlock >> lg : 1;
         const int n_prefix = min(a.n_prefix, (prefix_len + page - 1) >> lg);
@@ -280,18 +280,18 @@ __global__ void __launch_bounds__(kThreads, 2)
             int4 p = make_int4(-1, -1, -1, -1);
             if (step < prefix_blocks) {
                 const int i = step * kServeBlock >> lg;
-                if (i < n_prefix) p.x = __ldg(a.prefix_pages + i);
+                if (i < n_prefix) p.x = a.prefix_pages[i];
                 if (page >= kServeBlock) {
                     p.y = step * kServeBlock & (page - 1);
                 } else {
-                    if (i + 1 < n_prefix) p.y = __ldg(a.prefix_pages + i + 1);
+                    if (i + 1 < n_prefix) p.y = a.prefix_pages[i + 1];
                     if (boxes == 4) {
-                        if (i + 2 < n_prefix) p.z = __ldg(a.prefix_pages + i + 2);
-                        if (i + 3 < n_prefix) p.w = __ldg(a.prefix_pages + i + 3);
+                        if (i + 2 < n_prefix) p.z = a.prefix_pages[i + 2];
+                        if (i + 3 < n_prefix) p.w = a.prefix_pages[i + 3];
                     }
                 }
             } else {
-                p = __ldg(w.pages + at.own0 + step - prefix_blocks);
+                p = w.pages[at.own0 + step - prefix_blocks];
             }
             return p;
         };
@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                 auto live_of = [&](int step) {
                     int2 r = make_int2(0, kServeRows);
                     if (step >= prefix_blocks) {
-                        const int4 f = __ldg(w.info + at.own0 + step - prefix_blocks);
+                        const int4 f = w.info[at.own0 + step - prefix_blocks];
                         r.x = max(f.x - tok0, 0) * s.G;
                         r.y = min(f.y - tok0, s.tile_tokens) * s.G;
                     }
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                     if (step < prefix_blocks) {
                         valid = seen = prefix_len - step * kServeBlock;
                     } else {
-                        const int4 f = __ldg(w.info + at.own0 + step - prefix_blocks);
+                        const int4 f = w.info[at.own0 + step - prefix_blocks];
                         valid = min(kServeBlock, f.w + f.y - f.x - f.z);
                         live = there && tok >= f.x && tok < f.y;
                         seen = causal ? min(valid, f.w + tok - f.x + 1 - f.z) : valid;
@@ -721,19 +721,9 @@ cudaError_t go(const ServeShape& s, const dllm_serve_tables& t, const ServeAttnA
                                            cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem<HD>);
     if (err != cudaSuccess) return err;
     const int ctas = 2 * sms < kServeCtas ? 2 * sms : kServeCtas;
-    k_serve_attn<HD, T><<<ctas, kThreads, kSmem<HD>, st>>>(maps, s, t, a);
-    err = cudaGetLastError();
+    err = serve_launch(k_serve_attn<HD, T>, dim3(ctas), kThreads, kSmem<HD>, st, maps, s, t, a);
     if (err != cudaSuccess) return err;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(ctas - 1, HD / 16);
-    cfg.blockDim = dim3(kServeRows);
-    cfg.stream = st;
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_serve_join<HD, T>, s, t, a);
+    return serve_launch(k_serve_join<HD, T>, dim3(ctas - 1, HD / 16), kServeRows, 0, st, s, t, a);
 }
 
 }  // namespace

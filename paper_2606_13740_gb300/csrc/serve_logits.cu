@@ -119,17 +119,18 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
     const int row0 = blockIdx.x * cut.rows_cta, row1 = min(a.rows, row0 + cut.rows_cta);
     const int words = (a.vocab + 31) / 32, pieces = (n + kPiece - 1) / kPiece;
 
+    pdl_wait();  // (inputs by plain loads, which stay behind it)
     int r0 = row0;
     while (r0 < row1) {
         // the run of rows of one request (without lists: all rows)
-        const int req = a.req ? __ldg(a.req + r0) : r0;
+        const int req = a.req ? a.req[r0] : r0;
         int r1 = a.hist || a.bias_ids ? r0 + 1 : row1;
-        while (r1 < row1 && (a.req ? __ldg(a.req + r1) : r1) == req) ++r1;
+        while (r1 < row1 && (a.req ? a.req[r1] : r1) == req) ++r1;
         const bool asks = req >= 0 && req < a.n_req && (a.hist || a.bias_ids);
         int n_list = 0;
         if (asks) {
-            const int n_bias = !a.bias_ids ? 0 : a.bias_len ? min(max(__ldg(a.bias_len + req), 0), a.bias_ld) : a.bias_ld;
-            const int n_hist = !a.hist ? 0 : a.hist_len ? min(max(__ldg(a.hist_len + req), 0), a.hist_ld) : a.hist_ld;
+            const int n_bias = !a.bias_ids ? 0 : a.bias_len ? min(max(a.bias_len[req], 0), a.bias_ld) : a.bias_ld;
+            const int n_hist = !a.hist ? 0 : a.hist_len ? min(max(a.hist_len[req], 0), a.hist_ld) : a.hist_ld;
             for (int i = tid; i < (cut.chunk + cut.chunk / 32) / 4; i += threads) reinterpret_cast<uint4*>(word)[i] = make_uint4(0, 0, 0, 0);
             // the history in whole 16-byte pieces, and what is before and behind them; the first of them on their way
             // while the biases are marked
@@ -140,11 +141,11 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
             constexpr int kAhead = 4;
             int4 x[kAhead];
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) x[k] = tid + k * threads < n4 ? __ldg(h4 + tid + k * threads) : make_int4(-1, -1, -1, -1);
+            for (int k = 0; k < kAhead; ++k) x[k] = tid + k * threads < n4 ? h4[tid + k * threads] : make_int4(-1, -1, -1, -1);
             const int* ids = a.bias_ids + static_cast<size_t>(req) * a.bias_ld;
-            int id = tid < n_bias ? __ldg(ids + tid) : -1;
+            int id = tid < n_bias ? ids[tid] : -1;
             __syncthreads();
-            for (int i = tid; i < n_bias; i += threads, id = i < n_bias ? __ldg(ids + i) : -1) {
+            for (int i = tid; i < n_bias; i += threads, id = i < n_bias ? ids[i] : -1) {
                 const unsigned v = static_cast<unsigned>(id - v0);
                 if (v < static_cast<unsigned>(n) && id >= 0) {
                     atomicMax(&word[v], static_cast<uint32_t>(i + 1) << kCountBits);
@@ -159,8 +160,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
                     atomicOr(&bits[bit_word(v >> 5)], 1u << (v & 31));
                 }
             };
-            if (tid < lead) count(__ldg(h + tid));
-            if (tid < tail) count(__ldg(h + lead + 4 * n4 + tid));
+            if (tid < lead) count(h[tid]);
+            if (tid < tail) count(h[lead + 4 * n4 + tid]);
             for (int i = tid;;) {
 #pragma unroll
                 for (int k = 0; k < kAhead; ++k) {
@@ -173,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
                 i += kAhead * threads;
                 if (i >= n4) break;
 #pragma unroll
-                for (int k = 0; k < kAhead; ++k) x[k] = i + k * threads < n4 ? __ldg(h4 + i + k * threads) : make_int4(-1, -1, -1, -1);
+                for (int k = 0; k < kAhead; ++k) x[k] = i + k * threads < n4 ? h4[i + k * threads] : make_int4(-1, -1, -1, -1);
             }
             __syncthreads();
             // the list, in the order of the bits
@@ -200,9 +201,9 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
             }
             n_list = base;
         }
-        const float rep = asks && a.rep ? __ldg(a.rep + req) : 1.0f;
-        const float freq = asks && a.freq ? __ldg(a.freq + req) : 0.0f;
-        const float pres = asks && a.pres ? __ldg(a.pres + req) : 0.0f;
+        const float rep = asks && a.rep ? a.rep[req] : 1.0f;
+        const float freq = asks && a.freq ? a.freq[req] : 0.0f;
+        const float pres = asks && a.pres ? a.pres[req] : 0.0f;
         const float* bias = a.bias_ids && asks ? a.bias + static_cast<size_t>(req) * a.bias_ld : nullptr;
 
         // warp jobs: (row, share of the stretch), shares of whole pieces
@@ -211,9 +212,9 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
             const int p0 = pieces * share / cut.split, p1 = pieces * (share + 1) / cut.split;
             const T* src = static_cast<const T*>(a.logits) + static_cast<size_t>(row) * a.ld + v0;
             T* dst = a.out ? static_cast<T*>(a.out) + static_cast<size_t>(row) * a.ld_out + v0 : nullptr;
-            const int g = a.grammar ? __ldg(a.grammar_row + row) : -1;
+            const int g = a.grammar ? a.grammar_row[row] : -1;
             const uint32_t* allow = g >= 0 && g < a.n_grammar ? a.grammar + static_cast<size_t>(g) * words + v0 / 32 : nullptr;
-            const int cur = a.cur ? __ldg(a.cur + row) - v0 : -1, mask = a.mask_id < 0 ? -1 : a.mask_id - v0;
+            const int cur = a.cur ? a.cur[row] - v0 : -1, mask = a.mask_id < 0 ? -1 : a.mask_id - v0;
             Running run;
             // the stream's largest value, and the first piece that has it; that of ids taken one by one, and the id
             float best = -INFINITY, best_one = -INFINITY;
@@ -242,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
             auto only_allowed = [&](int q, float (&z)[kGroups][4]) {
 #pragma unroll
                 for (int u = 0; u < kGroups; ++u) {
-                    const uint32_t ok = __ldg(allow + 16 * q + 4 * u + (lane >> 3)) >> (4 * lane & 31);
+                    const uint32_t ok = allow[16 * q + 4 * u + (lane >> 3)] >> (4 * lane & 31);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         if (!((ok >> i) & 1u)) z[u][i] = -INFINITY;
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
             }
             // One id with its value, all asked of it done: into out, the decision, the sum.
             auto one = [&](int v, float y) {
-                if (allow && !((__ldg(allow + (v >> 5)) >> (v & 31)) & 1u)) y = -INFINITY;
+                if (allow && !((allow[v >> 5] >> (v & 31)) & 1u)) y = -INFINITY;
                 if (dst) Io<T>::put(dst + v, y);
                 if (v == cur) zcur[row] = y;
                 if (v == mask) y = -INFINITY;
@@ -350,7 +351,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
             }
             // the current id, if the stream had it
             if (lane == 0 && cur >= p0 * kPiece && cur < min(n, p1 * kPiece) && !(asks && word[cur]))
-                zcur[row] = allow && !((__ldg(allow + (cur >> 5)) >> (cur & 31)) & 1u) ? -INFINITY : Io<T>::get(src + cur);
+                zcur[row] = allow && !((allow[cur >> 5] >> (cur & 31)) & 1u) ? -INFINITY : Io<T>::get(src + cur);
             // The ids asked for, spread over the row's warps whatever pieces they lie in (half of a history falls into
             // a few hundred ids): only here they are read and stored.  Four gathers a lane in flight.
             if (asks) {
@@ -373,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
                             f = f > 0.0f ? __fdiv_rn(f, rep) : __fmul_rn(f, rep);
                             f = __fsub_rn(f, __fadd_rn(__fmul_rn(freq, static_cast<float>(c)), pres));
                         }
-                        if (nth) f = __fadd_rn(f, __ldg(bias + nth - 1));
+                        if (nth) f = __fadd_rn(f, bias[nth - 1]);
                         one(v[i], f);
                     }
                 }
@@ -414,7 +415,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
 
 // A warp joins a row's parts (in order of ids).
 __global__ void __launch_bounds__(128) k_merge(const __grid_constant__ dllm_serve_logits_args a, int parts,
-                                               const Part* __restrict__ part, const float* __restrict__ zcur) {
+                                               const Part* part, const float* zcur) {
     pdl_wait();
     const int row = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (row >= a.rows) return;
@@ -490,19 +491,10 @@ cudaError_t go(const dllm_serve_logits_args& a, const Cut& c, Part* part, float*
     if (smem > 48 * 1024)
         e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    kernel<<<grid, c.warps * 32, smem, st>>>(a, c, part, zcur);
-    e = cudaGetLastError();
+    e = serve_launch(kernel, grid, c.warps * 32, smem, st, a, c, part, zcur);
     if (e != cudaSuccess || !(a.x0 || a.conf || a.tokconf)) return e;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((a.rows + 3) / 4);
-    cfg.blockDim = dim3(128);
-    cfg.stream = st;
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_merge, a, c.chunks * c.split, static_cast<const Part*>(part), static_cast<const float*>(zcur));
+    return serve_launch(k_merge, dim3((a.rows + 3) / 4), 128, 0, st, a, c.chunks * c.split, static_cast<const Part*>(part),
+                        static_cast<const float*>(zcur));
 }
 
 }  // namespace

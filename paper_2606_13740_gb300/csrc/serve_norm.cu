@@ -50,7 +50,7 @@ struct Raw8<float> {
     }
 };
 __device__ __forceinline__ void get8(const float* p, float* v) {  // 16-byte aligned
-    const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
     v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
 }
 // theta / 2 pi in units of 2^-64 of a turn, whole turns dropped: theta is a whole number below 2^24 times a
@@ -87,10 +87,11 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) k_serve_norm(ServeShape s, 
     const long long wid = static_cast<long long>(blockIdx.x) * kWarpsPerCta + (threadIdx.x >> 5);
     const long long row = wid / parts;
     const int part = static_cast<int>(wid - row * parts);
+    pdl_wait();
     if (row >= a.rows) return;
     const int H = s.H, Hkv = s.Hkv;
-    const int pos = __ldg(a.pos + row);
-    int slot = __ldg(a.slot + row);
+    const int pos = a.pos[row];
+    int slot = a.slot[row];
     if (slot >= s.n_pages * s.page) {
         if (lane == 0) atomicOr(a.status, DLLM_SERVE_SLOT);
         slot = -1;
@@ -102,7 +103,7 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) k_serve_norm(ServeShape s, 
         float* d = reinterpret_cast<float*>(angles[threadIdx.x >> 5][1]);
 #pragma unroll
         for (int i = lane; i < HD / 2; i += 32) {
-            const unsigned long long turn = turns_of(__ldg(a.theta + i)) * static_cast<unsigned long long>(static_cast<long long>(pos));
+            const unsigned long long turn = turns_of(a.theta[i]) * static_cast<unsigned long long>(static_cast<long long>(pos));
             // the part of a turn, -1/2 .. 1/2, in units of pi
             sincospif(static_cast<float>(static_cast<int>(turn >> 32)) * 4.656612873077393e-10f, d + i, c + i);
         }
@@ -176,8 +177,7 @@ cudaError_t go(const ServeShape& s, const ServeNormArgs& a, int sms, cudaStream_
     long long parts = (static_cast<long long>(sms) * 64 + a.rows - 1) / a.rows;
     if (parts > passes) parts = passes;
     const long long ctas = (a.rows * parts + kWarpsPerCta - 1) / kWarpsPerCta;
-    k_serve_norm<HD, TI, TO><<<static_cast<unsigned>(ctas), kWarpsPerCta * 32, 0, st>>>(s, a, static_cast<int>(parts));
-    return cudaGetLastError();
+    return serve_launch(k_serve_norm<HD, TI, TO>, dim3(static_cast<unsigned>(ctas)), kWarpsPerCta * 32, 0, st, s, a, static_cast<int>(parts));
 }
 template <int HD>
 cudaError_t go_types(const ServeShape& s, const ServeNormArgs& a, int in_dtype, int sms, cudaStream_t st) {

@@ -27,6 +27,8 @@ struct PlanArgs {
     int batch, rows, prefix_len, causal, max_ctas;
 };
 
+// An input: a plain load, which stays behind pdl_wait (a read-only one need not).
+__device__ __forceinline__ int load_in(const int* p) { return *p; }
 __device__ __forceinline__ int clip(long long v) { return static_cast<int>(v < kMost ? v : kMost); }
 
 // Exclusive sums over the block of N values a thread; totals in sum.  buf: [N][kWarps].
@@ -78,7 +80,7 @@ struct Wants {
     bool bad, state;       // its lengths make no sense, or its held does not
 };
 __device__ __forceinline__ Wants wants(const PlanArgs& a, int b) {
-    const int L = __ldg(a.len + b), q = __ldg(a.q_len + b), held = a.t.held[b];
+    const int L = load_in(a.len + b), q = load_in(a.q_len + b), held = a.t.held[b];
     Wants w;
     w.rows = max(q, 0);
     w.state = held < 0 || held > a.s.max_pages;
@@ -141,6 +143,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
     serve_arrays(a.s, t.work, &w);
     if (threadIdx.x == 0) s_taken = s_refused = 0;
     int bits = 0;
+    pdl_wait();
 
     // ------------------------------------------------ the sums
     const int per = (B + kThreads - 1) / kThreads;
@@ -172,7 +175,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
     long long more[2] = {0, 0}, all_more[2];
     for (int b = b0; b < b1; ++b) {
         const Wants x = wants(a, b);
-        const int grow = max(x.need - x.held, 0), L = __ldg(a.len + b);
+        const int grow = max(x.need - x.held, 0), L = load_in(a.len + b);
         u.row[b] = clip(run[0]);
         u.grow[b] = clip(run[1]);
         u.shrink[b] = clip(run[2]);
@@ -198,7 +201,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
     for (int b = b0; b < b1; ++b) {
         u.block[b] = clip(more[0]);
         u.steps[b] = more[1];
-        const int rows = max(__ldg(a.q_len + b), 0), n = blocks_of(rows, u.len[b], u.refused[b]);
+        const int rows = max(load_in(a.q_len + b), 0), n = blocks_of(rows, u.len[b], u.refused[b]);
         more[0] += n;
         more[1] += steps_of(n, u.row[b], rows, u.len[b], u.refused[b], kMost);
     }
@@ -238,7 +241,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
         // -------------------------------------------- row starts, key counts, the CTAs' runs
         for (int b = threadIdx.x; b <= B; b += kThreads) {
             t.row_start[b] = u.row[b];
-            if (b < B) t.n_keys[b] = u.refused[b] ? 0 : u.len[b] + __ldg(a.q_len + b);
+            if (b < B) t.n_keys[b] = u.refused[b] ? 0 : u.len[b] + load_in(a.q_len + b);
         }
         const long long total = tiles ? cum(tiles) * a.s.Hkv : 0;
         const int ctas = static_cast<int>(min((total + 1) / 2, static_cast<long long>(a.max_ctas)));
@@ -338,10 +341,8 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
             }
             w.pages[k] = p;
         }
-        for (int k = first; k <= tiles; k += step) {
-            w.tile_cum[k] = cum(k);
-            if (k < tiles) w.tile_first[k] = u.block[find(u.row, B, k * tt)];
-        }
+        for (int k = first; k < tiles; k += step)
+            w.tile[k] = make_int2(u.block[find(u.row, B, k * tt)], static_cast<int>(cum(k + 1) - cum(k)));
     }
     if (bits) atomicOr(t.status, bits);
 
@@ -398,8 +399,7 @@ cudaError_t launch_serve_plan(const ServeShape& s, const dllm_serve_tables& t, c
     long long fill = (items + 2 * kThreads - 1) / (2 * kThreads);
     if (fill > sms - 1) fill = sms - 1;
     if (fill < 1) fill = 1;
-    k_serve_plan<<<static_cast<unsigned>(1 + fill), kThreads, plan_smem(batch), st>>>(a);
-    return cudaGetLastError();
+    return serve_launch(k_serve_plan, dim3(static_cast<unsigned>(1 + fill)), kThreads, plan_smem(batch), st, a);
 }
 
 }  // namespace dllm
