@@ -29,7 +29,7 @@ struct ServeShape {
 // The work list.  Rows (token, query head of the group) of a K/V head are cut into tiles of tile_tokens
 // tokens; tile x K/V head is a unit.  A unit's keys are steps of up to 64: the prefix's blocks, then the
 // own blocks of the requests that have rows in the tile, which stand side by side in the block arrays.
-// All units' steps in order (tile, head, step) are cut into `ctas` equal runs, one a CTA.
+// All units' steps in order (tile, head, step) are cut into `ctas` runs of equal cost, one a CTA.
 struct ServeWork {
     int ticket;          // CTAs of a plan that are done
     int ctas;
@@ -41,7 +41,7 @@ struct ServeWork {
     int pad;
     long long total;     // steps of all units
     int shape[5];        // what the list was made for (serve_same_shape)
-    int pad2;
+    int joins;           // units that several CTAs share
 };
 static_assert(sizeof(ServeWork) == 64, "the arrays behind it are 16-byte aligned");
 
@@ -63,9 +63,8 @@ __device__ inline bool serve_same_shape(const ServeShape& s, const ServeWork& w)
 
 struct ServeArrays {
     ServeWork* head;
-    int4* join;           // [kServeCtas]: where a CTA's run ends inside a unit that begins in it: the unit's tile and K/V
-                          // head, and its first and last CTA; else last < first
-    int4* cta;            // [kServeCtas]: tile, K/V head, step within the unit, number of steps
+    int4* join;           // [joins]: the unit's tile and K/V head, the first and the last CTA that holds a part of it
+    int4* cta;            // [kServeCtas][2]: tile, K/V head, step within the unit, number of steps; the tile's entry
     int4* info;           // [max_blocks]: first and last + 1 row of the request, the block's first key, n_keys - rows
     int4* pages;          // [max_blocks]: up to four pages (page < 64), or page and first place in it
     int2* tile;           // [max_tiles]: its first own block, its steps
@@ -83,7 +82,7 @@ __host__ __device__ inline size_t serve_arrays(const ServeShape& s, void* base, 
     r.join = reinterpret_cast<int4*>(b + at);
     at += serve_round(sizeof(int4) * kServeCtas);
     r.cta = reinterpret_cast<int4*>(b + at);
-    at += serve_round(sizeof(int4) * kServeCtas);
+    at += serve_round(sizeof(int4) * 2 * kServeCtas);
     r.info = reinterpret_cast<int4*>(b + at);
     at += serve_round(sizeof(int4) * s.max_blocks);
     r.pages = reinterpret_cast<int4*>(b + at);

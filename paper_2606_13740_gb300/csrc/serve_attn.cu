@@ -151,12 +151,12 @@ struct Walk {
     int n, own0, steps;  // steps of the current segment; the tile's first own block, its unit's steps
     int2 next;           // of the next tile, asked for a unit ahead
     __device__ Walk(const ServeArrays& w, int Hkv_, int cta) : tiles(w.tile), n_tiles(w.head->tiles), Hkv(Hkv_) {
-        const int4 d = w.cta[cta];
+        const int4 d = w.cta[2 * cta], e = w.cta[2 * cta + 1];
         tile = d.x;
         hk = d.y;
         step = d.z;
         left = d.w;
-        next = tiles[tile];
+        next = make_int2(e.x, e.y);
         enter();
         n = min(left, steps - step);
     }
@@ -628,78 +628,82 @@ __global__ void __launch_bounds__(kThreads, 2)
     if (warp == 4) tmem_dealloc(tmem, 256);
 }
 
-// Joins the parts of units that several CTAs share, in the order of their keys: a thread a row and 16
-// features, the blocks of CTA c for the unit that begins in its run and ends in another's.  A part is its CTA's
-// first (the unit begins before its run) or its last.  Bound by the trips to L2 that depend on one another: the
-// unit, the rows' maxima and sums, the parts.  (Joined by the warp that stores the last part instead, one SM's
-// loads in flight take longer than this launch: 96 tokens under 8001 keys 41 -> 71 us.)
+// Joins the parts of units that several CTAs share, in the order of their keys: blocks take a unit and 16
+// features at a time, a thread a row.  A part is its CTA's first (the unit begins before its run) or its last.
+// Bound by the trips to L2 that depend on one another: the unit, the rows' maxima and sums, the parts.  (Joined
+// by the warp that stores the last part instead, one SM's loads in flight take longer than this launch: 96
+// tokens under 8001 keys 41 -> 71 us.)
+constexpr int kJoinBlocks = 6;  // of an SM
 template <int HD, typename T>
-__global__ void __launch_bounds__(kServeRows) k_serve_join(const __grid_constant__ ServeShape s,
-                                                           const __grid_constant__ dllm_serve_tables t,
-                                                           const __grid_constant__ ServeAttnArgs a) {
-    constexpr int kBatch = 4;  // parts whose loads are in flight together
+__global__ void __launch_bounds__(kServeRows, kJoinBlocks) k_serve_join(const __grid_constant__ ServeShape s,
+                                                                        const __grid_constant__ dllm_serve_tables t,
+                                                                        const __grid_constant__ ServeAttnArgs a) {
+    constexpr int kBatch = 2;  // parts whose loads are in flight together
     ServeArrays w;
     serve_arrays(s, t.work, &w);
-    const int r = threadIdx.x, f0 = static_cast<int>(blockIdx.y) * 16;
-    const int4 d = __ldg(w.join + blockIdx.x);
-    const int first = d.z, last = d.w;
-    const int tok_off = r / s.G, g = r - tok_off * s.G, n = d.x * s.tile_tokens + tok_off;
-    const bool mine = last > first && static_cast<int>(blockIdx.x) < w.head->ctas && serve_same_shape(s, *w.head) &&
-                      tok_off < s.tile_tokens && n < min(w.head->rows, a.rows);
+    // (the plan was there before the launch that this one overlaps with waited for it)
+    const int items = serve_same_shape(s, *w.head) ? w.head->joins * (HD / 16) : 0, rows = min(w.head->rows, a.rows);
+    const int r = threadIdx.x, tok_off = r / s.G, g = r - tok_off * s.G;
+    int4 d = static_cast<int>(blockIdx.x) < items ? w.join[blockIdx.x / (HD / 16)] : make_int4(0, 0, 0, 0);
     pdl_wait();
-    if (!mine) return;
-    const float2* ml = reinterpret_cast<const float2*>(t.partials + static_cast<size_t>(2 * kServeCtas) * kServeRows * HD) + r;
-    const float4* pp = reinterpret_cast<const float4*>(t.partials) + static_cast<size_t>(f0 / 4) * kServeRows + r;
-    auto slot = [&](int k) { return (2 * static_cast<size_t>(k) + (k == first ? 1 : 0)) * kServeRows; };
-    float acc[16] = {}, M = -INFINITY, L = 0.0f;
-    float2 x[kBatch];
-    auto fetch = [&](int k0) {
+    for (int item = blockIdx.x; item < items;) {
+        const int f0 = item % (HD / 16) * 16, first = d.z, last = d.w, n = d.x * s.tile_tokens + tok_off;
+        const long long row_head = static_cast<long long>(n) * s.H + d.y * s.G + g;
+        item += gridDim.x;
+        if (item < items) d = w.join[item / (HD / 16)];
+        if (tok_off >= s.tile_tokens || n >= rows) continue;
+        const float2* ml = reinterpret_cast<const float2*>(t.partials + static_cast<size_t>(2 * kServeCtas) * kServeRows * HD) + r;
+        const float4* pp = reinterpret_cast<const float4*>(t.partials) + static_cast<size_t>(f0 / 4) * kServeRows + r;
+        auto slot = [&](int k) { return (2 * static_cast<size_t>(k) + (k == first ? 1 : 0)) * kServeRows; };
+        float acc[16] = {}, M = -INFINITY, L = 0.0f;
+        float2 x[kBatch];
+        auto fetch = [&](int k0) {
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) x[i] = k0 + i <= last ? ml[slot(k0 + i)] : make_float2(-INFINITY, 0.0f);
-    };
-    fetch(first);
-    for (int k0 = first; k0 <= last; k0 += kBatch) {
-        float4 v[kBatch][4];
-        float wt[kBatch], mx = M;
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                v[i][u] = x[i].y != 0.0f ? pp[slot(k0 + i) * (HD / 4) + u * kServeRows] : make_float4(0.f, 0.f, 0.f, 0.f);
-            mx = fmaxf(mx, x[i].x);
-        }
-        const float ref = mx == -INFINITY ? 0.0f : mx, al = M == -INFINITY ? 0.0f : exp2f(M - ref);
-        M = mx;
-        L *= al;
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) {
-            wt[i] = x[i].y != 0.0f ? exp2f(x[i].x - ref) : 0.0f;
-            L += x[i].y * wt[i];
-        }
-        fetch(k0 + kBatch);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            float4 o = make_float4(acc[4 * u] * al, acc[4 * u + 1] * al, acc[4 * u + 2] * al, acc[4 * u + 3] * al);
+            for (int i = 0; i < kBatch; ++i) x[i] = k0 + i <= last ? ml[slot(k0 + i)] : make_float2(-INFINITY, 0.0f);
+        };
+        fetch(first);
+        for (int k0 = first; k0 <= last; k0 += kBatch) {
+            float4 v[kBatch][4];
+            float wt[kBatch], mx = M;
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) {
-                o.x += v[i][u].x * wt[i];
-                o.y += v[i][u].y * wt[i];
-                o.z += v[i][u].z * wt[i];
-                o.w += v[i][u].w * wt[i];
-            }
-            acc[4 * u] = o.x;
-            acc[4 * u + 1] = o.y;
-            acc[4 * u + 2] = o.z;
-            acc[4 * u + 3] = o.w;
-        }
-    }
-    const float il = L != 0.0f ? 1.0f / L : 0.0f;
-    uint32_t o[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) o[k] = Half2<T>::pack(acc[2 * k] * il, acc[2 * k + 1] * il);
-    const long long row_head = static_cast<long long>(n) * s.H + d.y * s.G + g;
-    st_32b(static_cast<T*>(a.out) + row_head * HD + f0, o);
-    if (a.lse && f0 == 0) a.lse[row_head] = (M + log2f(L)) * kLn2;
+                for (int u = 0; u < 4; ++u)
+                    v[i][u] = x[i].y != 0.0f ? pp[slot(k0 + i) * (HD / 4) + u * kServeRows] : make_float4(0.f, 0.f, 0.f, 0.f);
+                mx = fmaxf(mx, x[i].x);
+            }
+            const float ref = mx == -INFINITY ? 0.0f : mx, al = M == -INFINITY ? 0.0f : exp2f(M - ref);
+            M = mx;
+            L *= al;
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                wt[i] = x[i].y != 0.0f ? exp2f(x[i].x - ref) : 0.0f;
+                L += x[i].y * wt[i];
+            }
+            fetch(k0 + kBatch);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                float4 o = make_float4(acc[4 * u] * al, acc[4 * u + 1] * al, acc[4 * u + 2] * al, acc[4 * u + 3] * al);
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    o.x += v[i][u].x * wt[i];
+                    o.y += v[i][u].y * wt[i];
+                    o.z += v[i][u].z * wt[i];
+                    o.w += v[i][u].w * wt[i];
+                }
+                acc[4 * u] = o.x;
+                acc[4 * u + 1] = o.y;
+                acc[4 * u + 2] = o.z;
+                acc[4 * u + 3] = o.w;
+            }
+        }
+        const float il = L != 0.0f ? 1.0f / L : 0.0f;
+        uint32_t o[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] = Half2<T>::pack(acc[2 * k] * il, acc[2 * k + 1] * il);
+        st_32b(static_cast<T*>(a.out) + row_head * HD + f0, o);
+        if (a.lse && f0 == 0) a.lse[row_head] = (M + log2f(L)) * kLn2;
+    }
 }
 
 template <int HD, typename T>
@@ -723,7 +727,7 @@ cudaError_t go(const ServeShape& s, const dllm_serve_tables& t, const ServeAttnA
     const int ctas = 2 * sms < kServeCtas ? 2 * sms : kServeCtas;
     err = serve_launch(k_serve_attn<HD, T>, dim3(ctas), kThreads, kSmem<HD>, st, maps, s, t, a);
     if (err != cudaSuccess) return err;
-    return serve_launch(k_serve_join<HD, T>, dim3(ctas - 1, HD / 16), kServeRows, 0, st, s, t, a);
+    return serve_launch(k_serve_join<HD, T>, dim3(kJoinBlocks * sms), kServeRows, 0, st, s, t, a);
 }
 
 }  // namespace
