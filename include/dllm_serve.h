@@ -79,9 +79,10 @@ enum {
     DLLM_SERVE_LENGTHS = 2,   /* a negative length, or more pages than max_pages: request refused */
     DLLM_SERVE_PAGES = 4,     /* the pool ran out: request refused */
     DLLM_SERVE_ROWS = 8,      /* the new tokens are more than the plan's rows: the last ones are left out */
-    DLLM_SERVE_PREFIX = 16,   /* fewer prefix pages than the plan's prefix_len needs */
+    DLLM_SERVE_PREFIX = 16,   /* fewer prefix pages than the plan's prefix_len needs, or one outside the pool */
     DLLM_SERVE_SLOT = 32,     /* a slot outside the pool: its row was not stored */
-    DLLM_SERVE_STATE = 64     /* table, held or ring_pos are not what a plan leaves: keys left out */
+    DLLM_SERVE_STATE = 64     /* table, held or ring_pos are not what a plan leaves (request refused, or its keys read
+                               * as zeros), or an attention after no plan of its config (zeros) */
 };
 
 /* Bytes of the buffers for cfg (bytes nullable) and, with mem (16-byte aligned

@@ -281,6 +281,7 @@ __global__ void __launch_bounds__(kThreads, 2)
             if (step < prefix_blocks) {
                 const int i = step * kServeBlock >> lg;
                 if (i < n_prefix) p.x = a.prefix_pages[i];
+                if (i < n_prefix && (p.x < 0 || p.x >= s.n_pages)) atomicOr(t.status, DLLM_SERVE_PREFIX);
                 if (page >= kServeBlock) {
                     p.y = step * kServeBlock & (page - 1);
                 } else {

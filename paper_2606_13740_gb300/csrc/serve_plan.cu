@@ -353,6 +353,13 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
                 }
             }
             w.pages[k] = p;
+            if (!u.refused[b]) {  // pages outside the pool read as zeros, and are reported
+                const int n_own = page >= kServeBlock ? 1 : min(kServeBlock >> lg, ((L + q - 1) >> lg) - (key0 >> lg) + 1);
+                const int id[4] = {p.x, n_own > 1 ? p.y : 0, n_own > 2 ? p.z : 0, n_own > 3 ? p.w : 0};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (id[i] < 0 || id[i] >= n_pages) bits |= DLLM_SERVE_STATE;
+            }
         }
         for (int k = first; k < tiles; k += step)
             w.tile[k] = make_int2(u.block[find(u.row, B, k * tt)], static_cast<int>(cum(k + 1) - cum(k)));

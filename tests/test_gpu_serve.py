@@ -429,6 +429,45 @@ def test_attention_repeats_its_bits_and_runs_in_a_graph_on_another_stream(dev):
     x.s.dllm_serve_check()
 
 
+def test_attention_reads_pages_outside_the_pool_as_zeros(dev):
+    """Page numbers outside the pool, in a request's row or the prefix: zeros for keys and values, and a report."""
+    from paper_2606_13740_gb300 import DllmError
+    for page in (16, 64):
+        x = Paged([20, 90], [2, 3], 70, page, 4, 2, 64, seed=16)
+        clean = x.check()
+        x.s.table[1, 0] = 1 << 30
+        x.s.dllm_serve_plan(_i32([20, 90]), _i32([2, 3]), 5, prefix_len=70)
+        out = x.call()
+        with pytest.raises(DllmError, match="status bits 64"):
+            x.s.dllm_serve_check()
+        n = min(page, 93)
+        x.k[2][:n] = 0
+        x.v[2][:n] = 0
+        want, size, _ = x.want()
+        assert torch.equal(out[:2], clean[:2])
+        assert bool(((out.double() - want).abs() <= U["bf16"] * want.abs() + (U["bf16"] + 2e-5) * size).all())
+        bad = x.prefix.clone()
+        bad[0] = -7
+        x.s.dllm_serve_attention(x.q, x.kc, x.vc, bad)
+        with pytest.raises(DllmError, match="status bits 16"):
+            x.s.dllm_serve_check()
+
+
+def test_attention_random_batches(dev):
+    """Ragged batches at random: requests without rows, of one token and of many, causal or not, tiles that several
+    requests share, pages of every size."""
+    r = random.Random(17)
+    for k in range(24):
+        H, Hkv, hd = r.choice(SHAPES)
+        B = r.choice([1, 2, 5, 23])
+        top = r.choice([1, 9, 140])
+        Q = [r.choice([0, 1, r.randint(1, top)]) for _ in range(B)]
+        Q[r.randrange(B)] = top
+        L = [r.choice([0, r.randint(0, 300)]) for _ in range(B)]
+        Paged(L, Q, r.choice([0, 1, 63, 64, 500]), r.choice([16, 32, 64, 128, 256]), H, Hkv, hd, causal=r.random() < 0.5,
+              dtype=r.choice(["bf16", "f16"]), seed=100 + k, pad=r.choice([0, 0, 4])).check()
+
+
 def test_attention_without_a_plan_writes_zeros(dev):
     s = _serve(max_batch=2, max_rows=8, page=16, n_pages=4, max_pages=2, n_heads=4, n_kv_heads=2, head_dim=64)
     q = torch.ones(8, 4, 64, device="cuda", dtype=torch.bfloat16)
