@@ -49,10 +49,6 @@ struct Raw8<float> {
         }
     }
 };
-__device__ __forceinline__ void get8(const float* p, float* v) {  // 16-byte aligned
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-}
 // theta / 2 pi in units of 2^-64 of a turn, whole turns dropped: theta is a whole number below 2^24 times a
 // power of two, the number's product with the first 64 bits of 1 / 2 pi is exact, and what the bits behind
 // them would add is below 2^-40 / 2^23 of a turn a position (theta <= 1).
@@ -81,7 +77,7 @@ __device__ __forceinline__ void store8(T* p, const float* v) {
 // parts: warps that share a row.  Not __restrict__ / read-only for q: q_out may be q (a warp reads a head
 // before it writes it, and nobody else reads it).
 template <int HD, typename TI, typename TO>
-__global__ void __launch_bounds__(kWarpsPerCta * 32) k_serve_norm(ServeShape s, ServeNormArgs a, int parts) {
+__global__ void __launch_bounds__(kWarpsPerCta * 32, 3) k_serve_norm(ServeShape s, ServeNormArgs a, int parts) {
     constexpr int kLanes = HD / 16, kHeads = 32 / kLanes;  // lanes of a head, heads of a warp's pass
     const int lane = threadIdx.x & 31, l = lane % kLanes, sub = lane / kLanes;
     const long long wid = static_cast<long long>(blockIdx.x) * kWarpsPerCta + (threadIdx.x >> 5);
@@ -96,6 +92,24 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) k_serve_norm(ServeShape s, 
         if (lane == 0) atomicOr(a.status, DLLM_SERVE_SLOT);
         slot = -1;
     }
+
+    const int heads = H + 2 * Hkv, step = parts * kHeads;
+    struct Pass {
+        Raw8<TI> x, y;
+    };
+    auto fetch = [&](int h, Pass& r) {  // head h of q, k and v in a row
+        if (h >= heads || (h >= H && slot < 0)) return;
+        const TI* src = h < H         ? static_cast<const TI*>(a.q) + row * a.ldq + static_cast<long long>(h) * HD
+                        : h < H + Hkv ? static_cast<const TI*>(a.k) + row * a.ldk + static_cast<long long>(h - H) * HD
+                                      : static_cast<const TI*>(a.v) + row * a.ldv + static_cast<long long>(h - H - Hkv) * HD;
+        r.x.load(src + 8 * l);
+        r.y.load(src + HD / 2 + 8 * l);
+    };
+    // two passes on their way while a third is worked on
+    Pass r0, r1;
+    int h = part * kHeads + sub;
+    fetch(h, r0);
+    fetch(h + step, r1);
 
     __shared__ float4 angles[kWarpsPerCta][2][HD / 8];  // cosines, sines
     {
@@ -113,51 +127,39 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) k_serve_norm(ServeShape s, 
     TO* kc = static_cast<TO*>(a.kc);
     TO* vc = static_cast<TO*>(a.vc);
     const long long at = slot < 0 ? 0 : (slot >> s.page_log2) * s.page_stride + static_cast<long long>(slot & (s.page - 1)) * HD;
-    const int heads = H + 2 * Hkv;
-    Raw8<TI> rx, ry;
-    auto fetch = [&](int h) {  // head h of q, k and v in a row
-        if (h >= heads || (h >= H && slot < 0)) return;
-        const TI* src = h < H         ? static_cast<const TI*>(a.q) + row * a.ldq + static_cast<long long>(h) * HD
-                        : h < H + Hkv ? static_cast<const TI*>(a.k) + row * a.ldk + static_cast<long long>(h - H) * HD
-                                      : static_cast<const TI*>(a.v) + row * a.ldv + static_cast<long long>(h - H - Hkv) * HD;
-        rx.load(src + 8 * l);
-        ry.load(src + HD / 2 + 8 * l);
-    };
-    fetch(part * kHeads + sub);
-    for (int h0 = part * kHeads; h0 < heads; h0 += parts * kHeads) {
-        const int h = h0 + sub;
+    auto work = [&](int h, Pass& r) {
         const bool is_q = h < H, is_k = !is_q && h < H + Hkv, live = h < heads && (is_q || slot >= 0);
         float x[8], y[8];
-        rx.get(x);
-        ry.get(y);
-        fetch(h + parts * kHeads);
+        r.x.get(x);
+        r.y.get(y);
+        fetch(h + 2 * step, r);
         float ss = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) ss += x[i] * x[i] + y[i] * y[i];
 #pragma unroll
         for (int d = 1; d < kLanes; d *= 2) ss += __shfl_xor_sync(0xffffffffu, ss, d);
-        if (!live) continue;
+        if (!live) return;
         TO* dst;
         if (is_q || is_k) {
-            const float r = rsqrtf(ss * (1.0f / HD) + a.eps);
+            const float scale = rsqrtf(ss * (1.0f / HD) + a.eps);
             const float* gain = is_q ? a.q_gain : a.k_gain;
-            float gx[8], gy[8], c[8], d[8];
-            if (gain) {
-                get8(gain + 8 * l, gx);
-                get8(gain + HD / 2 + 8 * l, gy);
-            }
             const float4 *pc = angles[threadIdx.x >> 5][0] + 2 * l, *pd = angles[threadIdx.x >> 5][1] + 2 * l;
-            *reinterpret_cast<float4*>(c) = pc[0], *reinterpret_cast<float4*>(c + 4) = pc[1];
-            *reinterpret_cast<float4*>(d) = pd[0], *reinterpret_cast<float4*>(d + 4) = pd[1];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float u = x[i] * r, w = y[i] * r;
+            for (int k = 0; k < 2; ++k) {
+                const float4 c4 = pc[k], d4 = pd[k];
+                const float c[4] = {c4.x, c4.y, c4.z, c4.w}, d[4] = {d4.x, d4.y, d4.z, d4.w};
+                float gx[4] = {1.0f, 1.0f, 1.0f, 1.0f}, gy[4] = {1.0f, 1.0f, 1.0f, 1.0f};
                 if (gain) {
-                    u *= gx[i];
-                    w *= gy[i];
+                    const float4 g4 = reinterpret_cast<const float4*>(gain + 8 * l)[k], h4 = reinterpret_cast<const float4*>(gain + HD / 2 + 8 * l)[k];
+                    gx[0] = g4.x, gx[1] = g4.y, gx[2] = g4.z, gx[3] = g4.w;
+                    gy[0] = h4.x, gy[1] = h4.y, gy[2] = h4.z, gy[3] = h4.w;
                 }
-                x[i] = u * c[i] - w * d[i];
-                y[i] = w * c[i] + u * d[i];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float u = x[4 * k + i] * scale * gx[i], w = y[4 * k + i] * scale * gy[i];
+                    x[4 * k + i] = u * c[i] - w * d[i];
+                    y[4 * k + i] = w * c[i] + u * d[i];
+                }
             }
             dst = is_q ? static_cast<TO*>(a.q_out) + row * a.ld_out + static_cast<long long>(h) * HD
                        : kc + at + static_cast<long long>(h - H) * s.page * HD;
@@ -166,6 +168,11 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) k_serve_norm(ServeShape s, 
         }
         store8(dst + 8 * l, x);
         store8(dst + HD / 2 + 8 * l, y);
+    };
+    const int passes = (heads - part * kHeads + step - 1) / step;  // the warp's
+    for (int i = 0; i < passes; i += 2, h += 2 * step) {
+        work(h, r0);
+        if (i + 1 < passes) work(h + step, r1);
     }
 }
 
@@ -173,8 +180,10 @@ template <int HD, typename TI, typename TO>
 cudaError_t go(const ServeShape& s, const ServeNormArgs& a, int sms, cudaStream_t st) {
     constexpr int kHeads = 32 / (HD / 16);
     const int passes = (s.H + 2 * s.Hkv + kHeads - 1) / kHeads;
-    // few rows: a warp for each pass; many: a warp for a whole row, whose angles are made once
-    long long parts = (static_cast<long long>(sms) * 64 + a.rows - 1) / a.rows;
+    // Few rows: a warp for each pass; many: half a row a warp, which makes the row's angles for that.  (1201 rows of 9
+    // passes: 9 warps a row 8.6 us, 5 7.6; 16384 rows of 24: one 134, two 130.)
+    long long parts = (static_cast<long long>(sms) * 32 + a.rows - 1) / a.rows;
+    if (parts < 2) parts = 2;
     if (parts > passes) parts = passes;
     const long long ctas = (a.rows * parts + kWarpsPerCta - 1) / kWarpsPerCta;
     return serve_launch(k_serve_norm<HD, TI, TO>, dim3(static_cast<unsigned>(ctas)), kWarpsPerCta * 32, 0, st, s, a, static_cast<int>(parts));
