@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
     const int B = a.batch;
     const Sums u(smem, B);
     __shared__ int s_taken, s_refused, s_last, s_joins;
-    __shared__ long long tile_sum[kServeCtas + 1];
+    __shared__ long long begin[kServeCtas + 1], sampled[kThreads];  // a run's first step among all; costs before some tiles
 
     const dllm_serve_tables& t = a.t;
     const int n_pages = a.s.n_pages, page = a.s.page, lg = a.s.page_log2, tt = a.s.tile_tokens;
@@ -249,27 +249,32 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
         // The cost of a unit: its start, its prefix steps, its own steps; of all units of the tiles before tile i.
         // (Measured, in prefix steps of 0.78 us: an own step 1.17, a unit's start and end 1.5 to 2.7.  Cut by steps
         // alone, the CTAs of 16 windows of 32 under 4096 shared keys ended between 34 and 47 us.)
-        auto cost = [&](int i) { return static_cast<long long>(i) * (kStart + kPrefix * static_cast<long long>(pb)) + kOwnStep * (cum(i) - static_cast<long long>(i) * pb); };
-        const long long all_cost = tiles ? cost(tiles) * a.s.Hkv : 0, total = tiles ? cum(tiles) * a.s.Hkv : 0;
+        auto cost_of = [&](int i, long long steps) {  // of tile i, with cum(i)
+            return i * (kStart + kPrefix * static_cast<long long>(pb)) + kOwnStep * (steps - static_cast<long long>(i) * pb);
+        };
+        // at kThreads tiles side by side, so that a run's search goes over few of the others
+        const int stride = (tiles + kThreads - 1) / kThreads, samples = tiles ? (tiles + stride - 1) / stride : 0;
+        if (static_cast<int>(threadIdx.x) < samples) sampled[threadIdx.x] = cost_of(threadIdx.x * stride, cum(threadIdx.x * stride));
+        const long long per_head = tiles ? cum(tiles) : 0, total = per_head * a.s.Hkv, all_cost = cost_of(tiles, per_head) * a.s.Hkv;
         // (no run of less than two steps, so that only a run that begins where a unit does may be empty)
         const int ctas = static_cast<int>(min(all_cost ? max(all_cost / kLeast, 1ll) : 0ll, static_cast<long long>(a.max_ctas)));
-        long long* begin = tile_sum;  // [kServeCtas + 1]: a run's first step among all
         int4 d = make_int4(0, 0, 0, 0), e = d;
         long long unit0 = 0;  // the first step of the unit that this thread's run begins in
         static_assert(kServeCtas < kThreads, "a thread a run");
         const int c = threadIdx.x;
+        __syncthreads();
         if (c <= kServeCtas) {
             begin[c] = total;
             if (c < ctas) {
                 const long long x = all_cost / ctas * c + all_cost % ctas * c / ctas, own = x / a.s.Hkv;
-                int lo = 0, hi = tiles;  // the tile whose units (all heads) hold cost x
-                while (hi - lo > 1) {
+                int lo = samples > 1 ? find(sampled, samples, own) * stride : 0, hi = min(lo + stride, tiles);
+                while (hi - lo > 1) {  // the tile whose units (all heads) hold cost x
                     const int mid = (lo + hi) >> 1;
-                    if (cost(mid) <= own) lo = mid;
+                    if (cost_of(mid, cum(mid)) <= own) lo = mid;
                     else hi = mid;
                 }
-                const long long at = cost(lo), unit = cost(lo + 1) - at, in = x - at * a.s.Hkv;
-                const long long steps0 = cum(lo), steps = cum(lo + 1) - steps0;
+                const long long steps0 = cum(lo), steps1 = lo + 1 == tiles ? per_head : cum(lo + 1), steps = steps1 - steps0;
+                const long long at = cost_of(lo, steps0), unit = cost_of(lo + 1, steps1) - at, in = x - at * a.s.Hkv;
                 d.x = lo;
                 d.y = static_cast<int>(in / unit);
                 const long long o = max(in - d.y * unit - kStart, 0ll);
