@@ -13,3 +13,4 @@ from .dllm import (  # noqa: F401
     dllm_arena_bytes, dllm_op_attention,
     dllm_op_commit, dllm_op_gemm, dllm_op_lmhead, dllm_op_release_scratch, lib,
 )
+from .serve import Serve, ServeConfig, dllm_serve_bytes, dllm_serve_logits  # noqa: F401

