@@ -209,9 +209,11 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
         const float* bias = a.bias_ids && asks ? a.bias + static_cast<size_t>(req) * a.bias_ld : nullptr;
 
         // warp jobs: (row, share of the stretch), shares of whole pieces
-        for (int job = warp; job < (r1 - r0) * cut.split; job += cut.warps) {
-            const int row = r0 + job / cut.split, share = job % cut.split;
-            const int p0 = pieces * share / cut.split, p1 = pieces * (share + 1) / cut.split;
+        const int jobs = (r1 - r0) * cut.split;
+        for (int job0 = 0; job0 < jobs; job0 += cut.warps) {
+            const bool mine = job0 + warp < jobs;  // else nothing to do but the barrier
+            const int job = mine ? job0 + warp : 0, row = r0 + job / cut.split, share = job % cut.split;
+            const int p0 = pieces * share / cut.split, p1 = mine ? pieces * (share + 1) / cut.split : p0;
             const T* src = static_cast<const T*>(a.logits) + static_cast<size_t>(row) * a.ld + v0;
             T* dst = a.out ? static_cast<T*>(a.out) + static_cast<size_t>(row) * a.ld_out + v0 : nullptr;
             const int g = a.grammar ? a.grammar_row[row] : -1;
@@ -263,14 +265,12 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
                     if constexpr (decltype(with_out)::value) {
                         T* pd = dst + q * kPiece + 4 * lane;
 #pragma unroll
-                        for (int u = 0; u < kGroups; ++u) {
-                            const uint32_t skip = (todo >> (4 * u)) & 15u;
-                            if (VEC && !skip) {
+                        for (int u = 0; u < kGroups; ++u) {  // (those in the list too, whose values follow)
+                            if constexpr (VEC) {
                                 Io<T>::put4(pd + u * kGroup, z[u]);
                             } else {
 #pragma unroll
-                                for (int i = 0; i < 4; ++i)
-                                    if (!((skip >> i) & 1u)) Io<T>::put(pd + u * kGroup + i, z[u][i]);
+                                for (int i = 0; i < 4; ++i) Io<T>::put(pd + u * kGroup + i, z[u][i]);
                             }
                         }
                     }
@@ -355,10 +355,13 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
             if (lane == 0 && cur >= p0 * kPiece && cur < min(n, p1 * kPiece) && !(asks && word[cur]))
                 zcur[row] = allow && !((allow[cur >> 5] >> (cur & 31)) & 1u) ? -INFINITY : Io<T>::get(src + cur);
             // The ids asked for, spread over the row's warps whatever pieces they lie in (half of a history falls into
-            // a few hundred ids): only here they are read and stored.  Four gathers a lane in flight.
+            // a few hundred ids).  Their stores come behind the stream's, which wrote them as they were, so that their
+            // values are there still where out is logits.  Four gathers a lane in flight.
             if (asks) {
+                if (cut.split > 1 && a.out) __syncthreads();
+                else __syncwarp();
                 constexpr int kIds = 4;
-                for (int k0 = share * 32 + lane; k0 < n_list; k0 += kIds * 32 * cut.split) {
+                for (int k0 = mine ? share * 32 + lane : n_list; k0 < n_list; k0 += kIds * 32 * cut.split) {
                     int v[kIds];
                     float y[kIds];
 #pragma unroll
@@ -406,7 +409,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
             if (run.ref == -INFINITY) sum = run.s;  // nothing but -inf: 0, or NaN
 #pragma unroll
             for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-            if (lane == 0)
+            if (lane == 0 && mine)
                 part[(static_cast<size_t>(row) * cut.chunks + blockIdx.y) * cut.split + share] =
                     Part{m, sum, arg < kChunk ? v0 + arg : -1, 0};
         }
