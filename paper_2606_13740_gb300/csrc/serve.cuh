@@ -31,7 +31,7 @@ struct ServeShape {
 // own blocks of the requests that have rows in the tile, which stand side by side in the block arrays.
 // All units' steps in order (tile, head, step) are cut into `ctas` runs of equal cost, one a CTA.
 struct ServeWork {
-    int ticket;          // CTAs of a plan that are done
+    int ticket;          // CTAs of a plan that have read the state
     int ctas;
     int causal;
     int prefix_len;
