@@ -554,6 +554,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                             l *= al;
                         }
                         if (up) m = mx;
+                        tmem_wait_st();  // (nothing else orders two stores to the same columns)
                         weigh();
                     }
                     if (live) l += sum;
