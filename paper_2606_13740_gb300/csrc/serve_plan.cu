@@ -131,6 +131,8 @@ struct Sums {
         refused = reinterpret_cast<uint8_t*>(held + B);
     }
 };
+// static shared memory of k_serve_plan, at most: its two arrays and a few words (a launch counts it too)
+constexpr size_t kStaticSmem = sizeof(long long) * (kServeCtas + 1 + kThreads) + 256;
 size_t plan_smem(int B) {
     return sizeof(long long) * (3 * kWarps + B + 1) + sizeof(int) * (4 * (static_cast<size_t>(B) + 1) + 2 * B) + B;
 }
@@ -420,7 +422,7 @@ cudaError_t launch_serve_reset(const ServeShape& s, const dllm_serve_tables& t, 
 
 cudaError_t launch_serve_plan(const ServeShape& s, const dllm_serve_tables& t, const int* len, const int* q_len,
                               int batch, int rows, int prefix_len, int causal, int sms, cudaStream_t st) {
-    if (plan_smem(batch) > 48 * 1024) {
+    if (plan_smem(batch) + kStaticSmem > 48 * 1024) {  // has to be asked for: the most of any batch
         const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(k_serve_plan),
                                                    cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                    static_cast<int>(plan_smem(kServeMaxBatch)));

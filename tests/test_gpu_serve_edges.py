@@ -1,11 +1,17 @@
 """Edges of the serving operators: sizes, lengths, page numbers and values at the ends of what the calls take, beside
 the ordinary ones of test_gpu_serve.py."""
+import os
+import subprocess
+import sys
+
 import pytest
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from test_gpu_serve import Paged, dev  # noqa: E402,F401
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 # ------------------------------------------------------------------ attention
@@ -18,3 +24,25 @@ def test_attention_first_blocks_far_from_zero(dev, H, Hkv, hd, dtype):
     first = x.check()
     for _ in range(20):
         assert torch.equal(x.call(), first)
+
+
+# ------------------------------------------------------------------ shared memory that has to be asked for
+def _fresh(code):
+    """In a process of its own, whose kernels have no larger limit from an earlier call."""
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stderr[-2000:]
+
+
+def test_plan_batches_around_the_limit_of_shared_memory(dev):
+    """In ascending order, so that no larger batch has raised the limit before."""
+    _fresh("""
+import torch
+from paper_2606_13740_gb300 import serve
+for B in (1274, 1275, 1400, 1477, 1478, 4096):
+    s = serve.Serve(serve.ServeConfig(max_batch=B, max_rows=B, page=16, n_pages=B + 1, max_pages=2, n_heads=4, n_kv_heads=2,
+                                      head_dim=64))
+    L = torch.zeros(B, dtype=torch.int32, device="cuda")
+    s.dllm_serve_plan(L, L + 1, B)
+    s.dllm_serve_check()
+    assert torch.equal(s.slot.long(), torch.arange(B, device="cuda") * 16), B
+""")
