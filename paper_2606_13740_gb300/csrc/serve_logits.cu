@@ -495,7 +495,7 @@ cudaError_t go(const dllm_serve_logits_args& a, const Cut& c, Part* part, float*
                      reinterpret_cast<uintptr_t>(a.out) % (4 * sizeof(T)) == 0 && (!a.out || a.ld_out % 4 == 0);
     const auto kernel = vec ? k_logits<T, true> : k_logits<T, false>;
     cudaError_t e = cudaSuccess;
-    if (smem > 48 * 1024)
+    if (smem + static_cast<int>(sizeof(int)) * kWarps > 48 * 1024)  // (s_count's too: together they have to be asked for)
         e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     e = serve_launch(kernel, grid, c.warps * 32, smem, st, a, c, part, zcur);

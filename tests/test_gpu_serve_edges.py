@@ -46,3 +46,27 @@ for B in (1274, 1275, 1400, 1477, 1478, 4096):
     s.dllm_serve_check()
     assert torch.equal(s.slot.long(), torch.arange(B, device="cuda") * 16), B
 """)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_logits_lists_around_the_limit_of_shared_memory(dev, dtype):
+    """Histories (and biases) in ascending order, at a size that is cut into the longest stretches (64 x 11 of 8192)."""
+    _fresh(f"""
+import torch
+from paper_2606_13740_gb300 import serve
+N, V = 64, 90000
+z = torch.randn(N, V, device="cuda").to({'torch.float32' if dtype == 'f32' else 'torch.bfloat16'})
+for n, nb in ((7664, 0), (7665, 0), (7632, 48), (7680, 0), (7681, 0), (8192, 0), (20000, 0)):
+    ids = torch.randperm(V, device="cuda")[:n].to(torch.int32)
+    more = {{}} if not nb else dict(bias_ids=torch.full((N, nb), -1, dtype=torch.int32, device="cuda"),
+                                  bias=torch.zeros(N, nb, device="cuda"))
+    out = torch.empty_like(z)
+    x0, _, _ = serve.dllm_serve_logits(z, hist=ids.repeat(N, 1), rep=torch.full((N,), 2.0, device="cuda"), out=out, **more)
+    want = z.clone()
+    w = z[:, ids.long()]
+    want[:, ids.long()] = torch.where(w > 0, w / 2, w * 2)
+    assert torch.equal(out, want), (n, nb)
+    top = want.float().amax(1, keepdim=True)
+    first = torch.where(want.float() == top, torch.arange(V, device="cuda"), V).amin(1)
+    assert torch.equal(x0.long(), first), (n, nb)
+""")
