@@ -495,8 +495,11 @@ cudaError_t go(const dllm_serve_logits_args& a, const Cut& c, Part* part, float*
                      reinterpret_cast<uintptr_t>(a.out) % (4 * sizeof(T)) == 0 && (!a.out || a.ld_out % 4 == 0);
     const auto kernel = vec ? k_logits<T, true> : k_logits<T, false>;
     cudaError_t e = cudaSuccess;
-    if (smem + static_cast<int>(sizeof(int)) * kWarps > 48 * 1024)  // (s_count's too: together they have to be asked for)
-        e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    // with s_count over 48 KB it has to be asked for: the most of any call, so that host threads, whose limit is one and
+    // the same, do not lower it between another's asking and launch
+    constexpr int kMostSmem = kChunk * 4 + kChunk / 8 + kChunk * 2;
+    if (smem + static_cast<int>(sizeof(int)) * kWarps > 48 * 1024)
+        e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem);
     if (e != cudaSuccess) return e;
     e = serve_launch(kernel, grid, c.warps * 32, smem, st, a, c, part, zcur);
     if (e != cudaSuccess || !(a.x0 || a.conf || a.tokconf)) return e;

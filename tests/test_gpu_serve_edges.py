@@ -3,6 +3,7 @@ the ordinary ones of test_gpu_serve.py."""
 import os
 import subprocess
 import sys
+import threading
 
 import pytest
 
@@ -70,3 +71,40 @@ for n, nb in ((7664, 0), (7665, 0), (7632, 48), (7680, 0), (7681, 0), (8192, 0),
     first = torch.where(want.float() == top, torch.arange(V, device="cuda"), V).amin(1)
     assert torch.equal(x0.long(), first), (n, nb)
 """)
+
+
+def test_logits_of_two_host_threads(dev):
+    """Calls whose lists need shared memory of different sizes, on streams and workspaces of their own."""
+    from paper_2606_13740_gb300 import serve
+    import ctypes as C
+    L = serve.serve_lib()
+    N, V, wrong, keep = 64, 90000, [], []
+
+    def job(n_hist):
+        t = dict(z=torch.randn(N, V, device="cuda"), hist=torch.arange(n_hist, dtype=torch.int32, device="cuda").repeat(N, 1),
+                 x0=torch.empty(N, dtype=torch.int32, device="cuda"),
+                 ws=torch.empty(serve._logits_bytes(N, V), dtype=torch.uint8, device="cuda"), stream=torch.cuda.Stream())
+        a = serve.dllm_serve_logits_args()
+        a.logits, a.ld, a.dtype, a.rows, a.vocab, a.mask_id, a.n_req = t["z"].data_ptr(), V, 2, N, V, -1, N
+        a.hist, a.hist_ld, a.x0 = t["hist"].data_ptr(), n_hist, t["x0"].data_ptr()
+        a.ws, a.ws_bytes = t["ws"].data_ptr(), t["ws"].numel()
+        keep.append((t, a))
+
+        def loop():
+            for _ in range(20000):
+                rc = L.dllm_serve_logits(C.byref(a), t["stream"].cuda_stream)
+                if rc:
+                    wrong.append((n_hist, rc, L.dllm_last_error(None)))
+                    return
+        return loop
+
+    threads = [threading.Thread(target=job(n)) for n in (7700, 8192)]
+    torch.cuda.synchronize()
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not wrong, wrong
+    for t, _ in keep:
+        assert torch.equal(t["x0"].long(), t["z"].argmax(1))
