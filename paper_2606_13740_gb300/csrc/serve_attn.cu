@@ -284,17 +284,24 @@ __global__ void __launch_bounds__(kThreads, 2)
             int4 p = make_int4(-1, -1, -1, -1);
             if (step < prefix_blocks) {
                 const int i = step * kServeBlock >> lg;
-                if (i < n_prefix) p.x = a.prefix_pages[i];
-                if (i < n_prefix && (p.x < 0 || p.x >= s.n_pages)) atomicOr(t.status, DLLM_SERVE_PREFIX);
+                bool out = false;  // a page that is not of the pool
+                auto page_at = [&](int k) {
+                    if (k >= n_prefix) return -1;
+                    const int id = a.prefix_pages[k];
+                    out |= id < 0 || id >= s.n_pages;
+                    return id;
+                };
+                p.x = page_at(i);
                 if (page >= kServeBlock) {
                     p.y = step * kServeBlock & (page - 1);
                 } else {
-                    if (i + 1 < n_prefix) p.y = a.prefix_pages[i + 1];
+                    p.y = page_at(i + 1);
                     if (boxes == 4) {
-                        if (i + 2 < n_prefix) p.z = a.prefix_pages[i + 2];
-                        if (i + 3 < n_prefix) p.w = a.prefix_pages[i + 3];
+                        p.z = page_at(i + 2);
+                        p.w = page_at(i + 3);
                     }
                 }
+                if (out) atomicOr(t.status, DLLM_SERVE_PREFIX);
             } else {
                 p = w.pages[at.own0 + step - prefix_blocks];
             }

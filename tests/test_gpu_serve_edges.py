@@ -10,7 +10,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_serve import Paged, dev  # noqa: E402,F401
+from test_gpu_serve import U, Paged, dev  # noqa: E402,F401
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -108,3 +108,25 @@ def test_logits_of_two_host_threads(dev):
     assert not wrong, wrong
     for t, _ in keep:
         assert torch.equal(t["x0"].long(), t["z"].argmax(1))
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 256])
+def test_attention_reports_each_prefix_page_outside_the_pool(dev, page):
+    """Any page of the prefix, not the first of a block of 64 keys alone: reported, and read as zeros."""
+    from paper_2606_13740_gb300 import DllmError
+    x = Paged([20, 90], [2, 3], 300, page, 4, 2, 64, seed=22)
+    x.check()
+    k0, v0 = x.k[0].clone(), x.v[0].clone()
+    n_pages = x.kc.shape[0]
+    for i in range(x.prefix.numel()):
+        bad = x.prefix.clone()
+        bad[i] = (-1, n_pages, 1 << 30, -2 ** 31)[i % 4]
+        out = x.s.dllm_serve_attention(x.q, x.kc, x.vc, bad)
+        with pytest.raises(DllmError, match="status bits 16"):
+            x.s.dllm_serve_check()
+        x.k[0][i * page:(i + 1) * page] = 0
+        x.v[0][i * page:(i + 1) * page] = 0
+        want, size, _ = x.want()
+        assert bool(((out.double() - want).abs() <= U["bf16"] * want.abs() + (U["bf16"] + 2e-5) * size).all())
+        x.k[0].copy_(k0), x.v[0].copy_(v0)
+    x.check()
