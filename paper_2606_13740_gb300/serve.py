@@ -2,7 +2,8 @@
 paged K/V cache, under a prefix that all of them share.
 
 Argument marshalling only.  Calls run on torch's current stream and do not wait; what a kernel found wrong
-(lengths, a pool that ran out) is raised by ``Serve.dllm_serve_check``.
+(lengths, a pool that ran out) is raised by ``Serve.dllm_serve_check``.  The library launches on the current
+device: buffers and tensors of another one are refused.
 """
 from __future__ import annotations
 
@@ -106,6 +107,16 @@ def _stream_of():
     return torch._C._cuda_getCurrentRawStream
 
 
+def _stream_on(index):
+    """Handle of torch's current stream on device `index`, which has to be the current device."""
+    import torch
+
+    now = torch.cuda.current_device()
+    if now != index:
+        raise ValueError(f"cuda:{index} is not the current device, cuda:{now} is")
+    return _stream_of()(index)
+
+
 @functools.cache
 def _logits_bytes(rows, vocab):
     n = _SZ()
@@ -126,7 +137,12 @@ class Serve:
         self._cp = C.byref(self._c)
         self._L = L = serve_lib()
         n = dllm_serve_bytes(cfg)
-        self.buffer = torch.empty(n, dtype=torch.uint8, device=device or "cuda")
+        device = torch.device(device or "cuda")
+        if device.type != "cuda":
+            raise ValueError(f"device must be a CUDA device, not {device}")
+        if device.index is not None:
+            _stream_on(device.index)
+        self.buffer = torch.empty(n, dtype=torch.uint8, device=device)
         self.device, self._index = self.buffer.device, self.buffer.device.index
         self._t = dllm_serve_tables()
         self._tp = C.byref(self._t)
@@ -155,7 +171,7 @@ class Serve:
         self.dllm_serve_reset()
 
     def _stream(self):
-        return _stream_of()(self._index)
+        return _stream_on(self._index)
 
     def dllm_serve_reset(self):
         """Nothing held, every page free."""
@@ -165,10 +181,10 @@ class Serve:
     def dllm_serve_plan(self, length, q_len, rows, prefix_len=0, causal=False):
         """length, q_len: int32 CUDA tensors [batch], own positions cached and new tokens; rows: rows of the step's
         packed arrays (at least the sum of q_len, else the last are left out)."""
-        i32 = self._i32
-        if (length.dtype != i32 or q_len.dtype != i32 or length.shape != q_len.shape or not length.is_cuda
-                or not q_len.is_cuda or not length.is_contiguous() or not q_len.is_contiguous()):
-            raise ValueError("length and q_len must be contiguous int32 CUDA tensors of one shape")
+        i32, index = self._i32, self._index
+        if (length.dtype != i32 or q_len.dtype != i32 or length.shape != q_len.shape or length.get_device() != index
+                or q_len.get_device() != index or not length.is_contiguous() or not q_len.is_contiguous()):
+            raise ValueError(f"length and q_len must be contiguous int32 tensors of one shape on cuda:{index}")
         rc = self._L.dllm_serve_plan(self._cp, self._tp, length.data_ptr(), q_len.data_ptr(), length.numel(), rows,
                                      prefix_len, causal, self._stream())
         if rc:
@@ -178,26 +194,26 @@ class Serve:
     def _row_stride(self, name, x, heads, dtype):
         """Elements from row to row of x: [rows][heads * head_dim] or [rows][heads][head_dim], rows dense."""
         st, shape, hd = x.stride(), x.shape, self._hd
-        if x.dtype == dtype and x.is_cuda:
+        if x.dtype == dtype and x.get_device() == self._index:
             n = heads * hd
             if (len(shape) == 2 and shape[1] == n and st[1] == 1) or (
                     len(shape) == 3 and shape[1] == heads and shape[2] == hd and st[2] == 1 and (st[1] == hd or heads == 1)):
                 return st[0] if shape[0] > 1 or st[0] >= n else n
-        raise ValueError(f"{name} must be a CUDA tensor [rows][{heads * hd}] or [rows][{heads}][{hd}] of {dtype} with dense "
-                         f"rows, not {x.dtype} {tuple(shape)} of strides {st} on {x.device}")
+        raise ValueError(f"{name} must be [rows][{heads * hd}] or [rows][{heads}][{hd}] of {dtype} with dense rows on "
+                         f"cuda:{self._index}, not {x.dtype} {tuple(shape)} of strides {st} on {x.device}")
 
     def _cache(self, name, x):
-        if x.dtype != self._dt or not x.is_cuda or x.shape != self._cache_shape or (
+        if x.dtype != self._dt or x.get_device() != self._index or x.shape != self._cache_shape or (
                 x.stride() != self._cache_strides and not (x.shape[0] == 1 and x.stride()[1:] == self._cache_strides[1:])):
-            raise ValueError(f"{name} must be a CUDA tensor {self._cache_shape} of {self._dt}, strides {self._cache_strides}, "
-                             f"not {tuple(x.shape)} of {x.dtype}, strides {x.stride()}")
+            raise ValueError(f"{name} must be {self._cache_shape} of {self._dt}, strides {self._cache_strides}, on "
+                             f"cuda:{self._index}, not {tuple(x.shape)} of {x.dtype}, strides {x.stride()}, on {x.device}")
         return x.data_ptr()
 
     def _vector(self, name, x, n):
         if x is None:
             return None
-        if x.dtype != self._f32 or x.shape != (n,) or not x.is_cuda or not x.is_contiguous():
-            raise ValueError(f"{name} must be {n} contiguous fp32 values on the GPU")
+        if x.dtype != self._f32 or x.shape != (n,) or x.get_device() != self._index or not x.is_contiguous():
+            raise ValueError(f"{name} must be {n} contiguous fp32 values on cuda:{self._index}")
         return x.data_ptr()
 
     def dllm_serve_qk_norm_rope(self, q, k, v, theta, kc, vc, q_gain=None, k_gain=None, eps=1e-5, out=None):
@@ -231,16 +247,17 @@ class Serve:
         if rows != self.rows:
             raise ValueError(f"q has {rows} rows, the plan {self.rows}")
         if prefix_pages is not None:
-            if prefix_pages.dtype != self._i32 or not prefix_pages.is_cuda or not prefix_pages.is_contiguous():
-                raise ValueError("prefix_pages must be a contiguous int32 CUDA tensor")
+            if (prefix_pages.dtype != self._i32 or prefix_pages.get_device() != self._index
+                    or not prefix_pages.is_contiguous()):
+                raise ValueError(f"prefix_pages must be a contiguous int32 tensor on cuda:{self._index}")
             n_prefix, pages = prefix_pages.numel(), prefix_pages.data_ptr()
         if n_prefix * self.cfg.page < self.prefix_len:
             raise ValueError(f"{n_prefix} prefix pages of {self.cfg.page} for a prefix of {self.prefix_len}")
         if out is None:
             out = self._empty((rows, self._H * self._hd), dtype=self._dt, device=self.device)
         elif (out.numel() != rows * self._H * self._hd or not out.is_contiguous() or out.dtype != self._dt
-              or not out.is_cuda):
-            raise ValueError("out must be contiguous, of q's rows and type")
+              or out.get_device() != self._index):
+            raise ValueError("out must be contiguous, of q's rows, type and device")
         ls = self._empty((rows, self._H), dtype=self._f32, device=self.device) if lse else None
         rc = self._L.dllm_serve_attention(self._cp, self._tp, q.data_ptr(), ldq, self._cache("kc", kc), self._cache("vc", vc),
                                           pages, n_prefix, self._scale if scale is None else scale, out.data_ptr(),
@@ -266,14 +283,16 @@ def dllm_serve_logits(logits, mask_id=-1, req=None, hist=None, hist_len=None, re
     if len(shape) != 2 or not logits.is_cuda or (shape[1] > 1 and st[1] != 1):
         raise ValueError("logits must be a CUDA tensor [rows][vocab] with dense rows")
     rows, vocab = shape
-    i32, f32, dev = torch.int32, torch.float32, logits.device
+    i32, f32, dev, index = torch.int32, torch.float32, logits.device, logits.get_device()
+    stream = _stream_on(index)
     n_req = hist.shape[0] if hist is not None else bias_ids.shape[0] if bias_ids is not None else 0
 
     def at(name, x, dtype, want):
         if x is None:
             return None
-        if x.dtype != dtype or x.shape != want or not x.is_cuda or not x.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous CUDA tensor of {dtype} {tuple(want)}, not {x.dtype} {tuple(x.shape)}")
+        if x.dtype != dtype or x.shape != want or x.get_device() != index or not x.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous tensor of {dtype} {tuple(want)} on {dev}, not {x.dtype} "
+                             f"{tuple(x.shape)} on {x.device}")
         return x.data_ptr()
 
     hist_ld = bias_ld = n_grammar = ld_out = 0
@@ -291,11 +310,13 @@ def dllm_serve_logits(logits, mask_id=-1, req=None, hist=None, hist_len=None, re
         raise ValueError("without req there is a list for each row")
     if out is not None:
         so = out.stride()
-        if out.shape != shape or out.dtype != logits.dtype or not out.is_cuda or (vocab > 1 and so[1] != 1):
+        if out.shape != shape or out.dtype != logits.dtype or out.get_device() != index or (vocab > 1 and so[1] != 1):
             raise ValueError("out must be like logits")
         ld_out = so[0] if rows > 1 else max(so[0], vocab)
     if ws is None:
         ws = torch.empty(_logits_bytes(rows, vocab), dtype=torch.uint8, device=dev)
+    elif ws.get_device() != index or not ws.is_contiguous():
+        raise ValueError(f"ws must be contiguous on {dev}")
     x0 = torch.empty(rows, dtype=i32, device=dev)
     conf, tokconf = torch.empty((2, rows), dtype=f32, device=dev).unbind(0)
     per_row, per_req = (rows,), (n_req,)
@@ -307,8 +328,8 @@ def dllm_serve_logits(logits, mask_id=-1, req=None, hist=None, hist_len=None, re
         at("bias", bias, f32, (n_req, bias_ld)), at("bias_len", bias_len, i32, per_req), bias_ld,
         at("grammar", grammar, i32, (n_grammar, (vocab + 31) // 32)), at("grammar_row", grammar_row, i32, per_row), n_grammar,
         at("cur", cur, i32, per_row), x0.data_ptr(), conf.data_ptr(), None if cur is None else tokconf.data_ptr(),
-        ws.data_ptr(), ws.numel())
-    rc = serve_lib().dllm_serve_logits(C.byref(a), _stream_of()(dev.index))
+        ws.data_ptr(), ws.numel() * ws.element_size())
+    rc = serve_lib().dllm_serve_logits(C.byref(a), stream)
     if rc:
         _check(rc)
     return x0, conf, None if cur is None else tokconf
