@@ -82,7 +82,8 @@ enum {
     DLLM_SERVE_PREFIX = 16,   /* fewer prefix pages than the plan's prefix_len needs, or one outside the pool */
     DLLM_SERVE_SLOT = 32,     /* a slot outside the pool: its row was not stored */
     DLLM_SERVE_STATE = 64     /* table, held or ring_pos are not what a plan leaves (request refused, or its keys read
-                               * as zeros), or an attention after no plan of its config (zeros) */
+                               * as zeros), or an attention after another config's plan (zeros, as after a reset and
+                               * no plan, which sets no bit) */
 };
 
 /* Bytes of the buffers for cfg (bytes nullable) and, with mem (16-byte aligned
