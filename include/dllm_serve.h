@@ -150,7 +150,7 @@ int dllm_serve_check(const dllm_serve_tables* t, int* bits, void* stream);
  * For each id v, with c = how often v stands in hist[r][0 .. hist_len[r]):
  *   c > 0:  z = (z > 0 ? z / rep[r] : z * rep[r]) - (freq[r] * c + pres[r])
  *   v among bias_ids[r][0 .. bias_len[r]):  z = z + bias[r][i] (of several the last i)
- *   grammar_row[n] = g >= 0 and bit v % 32 of grammar[g][v / 32] clear:  z = -inf
+ *   grammar_row[n] = g >= 0 and bit v % 32 of grammar[g][v / 32] clear, or g >= n_grammar:  z = -inf
  * in fp32, in this order, each operation rounded on its own.  out: z, rounded to
  * dtype (nullable; may be logits itself).  The decision, as dllm_op_lmhead: x0 =
  * argmax without mask_id (ties: lowest id; -1: every id is -inf), conf =

@@ -420,12 +420,25 @@ __global__ void __launch_bounds__(kThreads, 4) k_logits(const __grid_constant__ 
     }
 }
 
-// A warp joins a row's parts (in order of ids).
+// A warp joins a row's parts (in order of ids).  A row whose grammar there is not, which allows no id, has passed
+// k_logits as one without a grammar: here it gets its -inf and its decision.
+template <typename T>
 __global__ void __launch_bounds__(128) k_merge(const __grid_constant__ dllm_serve_logits_args a, int parts,
                                                const Part* part, const float* zcur) {
     pdl_wait();
     const int row = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (row >= a.rows) return;
+    if (a.grammar && a.grammar_row[row] >= 0 && a.grammar_row[row] >= a.n_grammar) {
+        if (a.out) {
+            T* z = static_cast<T*>(a.out) + static_cast<size_t>(row) * a.ld_out;
+            for (int v = lane; v < a.vocab; v += 32) Io<T>::put(z + v, -INFINITY);
+        }
+        if (lane) return;
+        if (a.x0) a.x0[row] = -1;
+        if (a.conf) a.conf[row] = 0.0f;
+        if (a.tokconf) a.tokconf[row] = 0.0f;
+        return;
+    }
     float m = -INFINITY, s = 0.0f;
     int arg = a.vocab;
     constexpr int kAtOnce = 8;
@@ -502,8 +515,8 @@ cudaError_t go(const dllm_serve_logits_args& a, const Cut& c, Part* part, float*
         e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem);
     if (e != cudaSuccess) return e;
     e = serve_launch(kernel, grid, c.warps * 32, smem, st, a, c, part, zcur);
-    if (e != cudaSuccess || !(a.x0 || a.conf || a.tokconf)) return e;
-    return serve_launch(k_merge, dim3((a.rows + 3) / 4), 128, 0, st, a, c.chunks * c.split, static_cast<const Part*>(part),
+    if (e != cudaSuccess || !(a.x0 || a.conf || a.tokconf || (a.grammar && a.out))) return e;
+    return serve_launch(k_merge<T>, dim3((a.rows + 3) / 4), 128, 0, st, a, c.chunks * c.split, static_cast<const Part*>(part),
                         static_cast<const float*>(zcur));
 }
 

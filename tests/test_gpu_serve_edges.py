@@ -5,12 +5,13 @@ import subprocess
 import sys
 import threading
 
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_serve import U, Paged, dev  # noqa: E402,F401
+from test_gpu_serve import U, Paged, _logits_case, _logits_run, dev  # noqa: E402,F401
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -130,3 +131,24 @@ def test_attention_reports_each_prefix_page_outside_the_pool(dev, page):
         assert bool(((out.double() - want).abs() <= U["bf16"] * want.abs() + (U["bf16"] + 2e-5) * size).all())
         x.k[0].copy_(k0), x.v[0].copy_(v0)
     x.check()
+
+
+# ------------------------------------------------------------------ logits
+@pytest.mark.parametrize("N,V,R,dtype", [(6, 20001, 6, "f32"), (64, 1024, 2, "bf16"), (6, 3000, 2, "f16")])
+def test_logits_of_a_grammar_that_there_is_not(dev, N, V, R, dtype):
+    """A row that names a grammar past the last one is allowed nothing; the others are as they were."""
+    c = _logits_case(N, V, R, dtype, 23)
+    c["grammar_row"][1::3] = 0
+    c["cur"][:] = c["cur"] % (V - 1)
+    good = {k: v.copy() if isinstance(v, np.ndarray) else v for k, v in c.items()}
+    rows = np.arange(0, N, 3)
+    c["grammar_row"][rows] = np.array([3, 1 << 30, 4] * N, np.int32)[:len(rows)]
+    for kw in (dict(), dict(inplace=True), dict(ld=V + 3)):
+        z, x0, conf, tok = _logits_run(c, V - 1, **kw)
+        want = _logits_run(good, V - 1, **kw)
+        assert np.all(z[rows] == -np.inf) and np.all(x0[rows] == -1) and np.all(conf[rows] == 0) and np.all(tok[rows] == 0)
+        rest = np.setdiff1d(np.arange(N), rows)
+        for got, w in zip((z, x0, conf, tok), want):
+            assert np.array_equal(got[rest], w[rest])
+    _, x0, conf, _ = _logits_run(c, V - 1, out=False)
+    assert np.all(x0[rows] == -1) and np.all(conf[rows] == 0)
