@@ -174,9 +174,11 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
     auto blocks_of = [&](int rows, int L, bool no) { return rows == 0 ? 0 : no ? 1 : static_cast<int>((static_cast<unsigned>(L) + rows + kServeBlock - 1) / kServeBlock); };
     auto steps_of = [&](int n_blocks, int row0, int rows, int L, bool no, int tiles) {  // of its first `tiles` tiles
         if (rows == 0) return 0ll;
-        const int first = row0 / tt, whole = (row0 + rows - 1) / tt - first;  // tiles but the last
+        // tiles but the last (a row's number past 2^31, of a request that is refused, is past the plan's rows)
+        const unsigned end = static_cast<unsigned>(row0) + static_cast<unsigned>(rows) - 1u;
+        const int first = row0 / tt, whole = static_cast<int>(min(end / static_cast<unsigned>(tt), kMost - 1u)) - first;
         if (!a.causal || no) return static_cast<long long>(n_blocks) * min(tiles, whole + 1);
-        const long long seen = static_cast<long long>(L) - row0 + static_cast<long long>(first + 1) * tt;  // keys, first tile
+        const long long seen = static_cast<long long>(L) - row0 + (first + 1ll) * tt;  // keys, first tile
         return floor_sum(min(tiles, whole), kServeBlock, tt, seen + kServeBlock - 1) + (tiles > whole ? n_blocks : 0);
     };
     long long more[2] = {0, 0}, all_more[2];

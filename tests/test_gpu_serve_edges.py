@@ -11,7 +11,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_serve import U, Paged, _logits_case, _logits_run, dev  # noqa: E402,F401
+from test_gpu_serve import U, Paged, _i32, _logits_case, _logits_run, _serve, dev  # noqa: E402,F401
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -152,3 +152,33 @@ def test_logits_of_a_grammar_that_there_is_not(dev, N, V, R, dtype):
             assert np.array_equal(got[rest], w[rest])
     _, x0, conf, _ = _logits_run(c, V - 1, out=False)
     assert np.all(x0[rows] == -1) and np.all(conf[rows] == 0)
+
+
+# ------------------------------------------------------------------ plan
+def test_plan_lengths_at_the_end_of_32_bits(dev):
+    """A refused request of 2^31 - 1 new tokens: its rows are those that are left, the requests before it and their
+    attention are as without it."""
+    from paper_2606_13740_gb300 import DllmError
+    x = Paged([10, 70], [5, 3], 40, 16, 28, 4, 128, seed=24, pad=150)
+    x.check()
+    for causal in (False, True):
+        s = _serve(max_batch=5, max_rows=158, page=16, n_pages=x.kc.shape[0], max_pages=8, n_heads=28, n_kv_heads=4, head_dim=128)
+        s.table[:2, :6].copy_(x.s.table[:2]), s.held[:2].copy_(x.s.held[:2]), s.ring_pos.zero_()
+        most = 2 ** 31 - 1
+        s.dllm_serve_plan(_i32([10, 70, 0, 4, most]), _i32([5, 3, most, most, most]), 158, prefix_len=40, causal=causal)
+        assert s.row_start.cpu().tolist() == [0, 5, 8, most, most, most]
+        assert s.n_keys.cpu().tolist() == [15, 73, 0, 0, 0] and s.req.cpu().tolist() == [0] * 5 + [1] * 3 + [2] * 150
+        assert s.slot[8:].cpu().tolist() == [-1] * 150 and s.pos[8:].cpu().tolist() == [0] * 150
+        assert torch.equal(s.slot[:8], x.s.slot[:8]) and torch.equal(s.pos[:8], x.s.pos[:8])
+        out = s.dllm_serve_attention(x.q, x.kc, x.vc, x.prefix)
+        with pytest.raises(DllmError, match="status bits 10"):  # lengths, rows
+            s.dllm_serve_check()
+        # the refused rows see the prefix alone
+        x.causal = causal
+        want, size, _ = x.want()
+        k, v = (y[0].double().repeat_interleave(7, 1) for y in (x.k, x.v))
+        z = torch.einsum("thd,khd->htk", x.q[8:].double(), k) * 128 ** -0.5
+        p = torch.softmax(z, -1)
+        want[8:] = torch.einsum("htk,khd->thd", p, v).reshape(150, -1)
+        size[8:] = torch.einsum("htk,khd->thd", p, v.abs()).reshape(150, -1)
+        assert bool(((out.double() - want).abs() <= U["bf16"] * want.abs() + (U["bf16"] + 2e-5) * size).all())
