@@ -38,26 +38,27 @@ struct ServeWork {
     int prefix_blocks;
     int tiles;
     int rows;            // new tokens covered
-    int pad;
-    long long total;     // steps of all units
-    int shape[5];        // what the list was made for (serve_same_shape)
     int joins;           // units that several CTAs share
+    long long total;     // steps of all units
+    int shape[6];        // what the list was made for (serve_same_shape)
 };
 static_assert(sizeof(ServeWork) == 64, "the arrays behind it are 16-byte aligned");
 
-// Whether a work list was made for this config (calls with another one find its arrays elsewhere).
+// Whether a work list was made for this config (calls with another one find its arrays elsewhere, or want larger
+// partials behind it).
 __host__ __device__ inline void serve_key(const ServeShape& s, int* key) {
     key[0] = s.Hkv;
     key[1] = s.G;
     key[2] = s.page;
     key[3] = s.max_tiles;
     key[4] = s.max_blocks;
+    key[5] = s.hd;
 }
 __device__ inline bool serve_same_shape(const ServeShape& s, const ServeWork& w) {
-    int key[5];
+    int key[6];
     serve_key(s, key);
     bool same = true;
-    for (int i = 0; i < 5; ++i) same = same && key[i] == w.shape[i];
+    for (int i = 0; i < 6; ++i) same = same && key[i] == w.shape[i];
     return same;
 }
 

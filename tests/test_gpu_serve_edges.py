@@ -182,3 +182,22 @@ def test_plan_lengths_at_the_end_of_32_bits(dev):
         want[8:] = torch.einsum("htk,khd->thd", p, v).reshape(150, -1)
         size[8:] = torch.einsum("htk,khd->thd", p, v.abs()).reshape(150, -1)
         assert bool(((out.double() - want).abs() <= U["bf16"] * want.abs() + (U["bf16"] + 2e-5) * size).all())
+
+
+# ------------------------------------------------------------------ more of the attention
+def test_attention_refuses_the_plan_of_another_head_dim(dev):
+    """Buffers laid out and planned for heads of 64 are too small for the parts of heads of 128: zeros, and a report."""
+    import ctypes as C
+    from paper_2606_13740_gb300 import DllmError, serve
+    kw = dict(max_batch=2, max_rows=8, page=16, n_pages=8, max_pages=4, n_heads=4, n_kv_heads=2)
+    s = _serve(head_dim=64, **kw)
+    s.dllm_serve_plan(_i32([0, 20]), _i32([4, 4]), 8)
+    c = serve.ServeConfig(head_dim=128, **kw).c()
+    q = torch.ones(8, 4, 128, device="cuda", dtype=torch.bfloat16)
+    kc = torch.ones(8, 2, 16, 128, device="cuda", dtype=torch.bfloat16)
+    out = torch.full((8, 512), 9.0, device="cuda", dtype=torch.bfloat16)
+    assert s._L.dllm_serve_attention(C.byref(c), s._tp, q.data_ptr(), 512, kc.data_ptr(), kc.data_ptr(), None, 0, 0.1,
+                                     out.data_ptr(), None, 8, s._stream()) == 0
+    with pytest.raises(DllmError, match="status bits 64"):
+        s.dllm_serve_check()
+    assert bool((out == 0).all())
