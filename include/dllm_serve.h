@@ -94,7 +94,8 @@ int dllm_serve_layout(const dllm_serve_config* cfg, void* mem, dllm_serve_tables
 int dllm_serve_reset(const dllm_serve_config* cfg, const dllm_serve_tables* t, void* stream);
 
 /* The step's plan.  Request b < batch has len[b] own positions cached (after
- * the shared prefix) and q_len[b] new tokens (both dev int32 [batch]); it
+ * the shared prefix) and q_len[b] new tokens (both dev int32 [batch], apart from
+ * the tables but for len, which may be their n_keys: what the last plan left); it
  * needs ceil((len + q_len) / page) pages.  Those it holds beyond that go to the
  * ring's end, in order of requests and pages; those it lacks come from the ring's
  * front in order of requests, so a page given back is handed out again at the

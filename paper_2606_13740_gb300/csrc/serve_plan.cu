@@ -257,11 +257,8 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
     };
 
     if (blockIdx.x == 0) {
-        // -------------------------------------------- row starts, key counts, the CTAs' runs
-        for (int b = threadIdx.x; b <= B; b += kThreads) {
-            t.row_start[b] = u.row[b];
-            if (b < B) t.n_keys[b] = u.refused[b] ? 0 : u.len[b] + load_in(a.q_len + b);
-        }
+        // -------------------------------------------- row starts, the CTAs' runs
+        for (int b = threadIdx.x; b <= B; b += kThreads) t.row_start[b] = u.row[b];
         // The cost of a unit: its start, its prefix steps, its own steps; of all units of the tiles before tile i.
         // (Measured, in prefix steps of 0.78 us: an own step 1.17, a unit's start and end 1.5 to 2.7.  Cut by steps
         // alone, the CTAs of 16 windows of 32 under 4096 shared keys ended between 34 and 47 us.)
@@ -387,12 +384,15 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
     }
     if (bits) atomicOr(t.status, bits);
 
-    // ------------------------------------------------ the state, by the CTA that read it last
+    // ------------------------------------------------ the state, by the CTA that read it last (and the key counts, which
+    // may be the next plan's lengths)
     if (threadIdx.x == kThreads - 1) s_last = ticket == static_cast<int>(gridDim.x) - 1;
     __syncthreads();
     if (!s_last) return;
-    for (int b = threadIdx.x; b < B; b += kThreads)
+    for (int b = threadIdx.x; b < B; b += kThreads) {
         if (!u.refused[b]) t.held[b] = need_of(b);
+        t.n_keys[b] = u.refused[b] ? 0 : u.len[b] + load_in(a.q_len + b);
+    }
     if (threadIdx.x == 0) {
         t.ring_pos[0] = static_cast<int>((static_cast<unsigned>(head) + taken) % static_cast<unsigned>(n_pages));
         t.ring_pos[1] = min(free_n - taken + given, n_pages);

@@ -11,7 +11,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_serve import U, Paged, _i32, _logits_case, _logits_run, _serve, dev  # noqa: E402,F401
+from test_gpu_serve import U, Paged, Pool, _i32, _logits_case, _logits_run, _same_plan, _serve, dev  # noqa: E402,F401
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -182,6 +182,22 @@ def test_plan_lengths_at_the_end_of_32_bits(dev):
         want[8:] = torch.einsum("htk,khd->thd", p, v).reshape(150, -1)
         size[8:] = torch.einsum("htk,khd->thd", p, v.abs()).reshape(150, -1)
         assert bool(((out.double() - want).abs() <= U["bf16"] * want.abs() + (U["bf16"] + 2e-5) * size).all())
+
+
+@pytest.mark.parametrize("B", [1, 7, 300, 4096])
+def test_plan_takes_its_own_key_counts_as_lengths(dev, B):
+    """The step after: length is the plan's own n_keys, which it replaces."""
+    r = np.random.default_rng(B)
+    s = _serve(max_batch=B, max_rows=B * 20, page=16, n_pages=B * 8 + 8, max_pages=9, n_heads=4, n_kv_heads=2, head_dim=64)
+    pool, have = Pool(B, 16, B * 8 + 8, 9), [0] * B
+    for step in range(6):
+        Q = r.integers(0, 20, B).tolist()
+        rows = sum(Q)
+        want = pool.plan(have, Q, rows, 3)
+        s.dllm_serve_plan(s.n_keys[:B], _i32(Q), rows, prefix_len=3)
+        _same_plan(s, pool, want, B, rows)
+        s.dllm_serve_check()
+        have = want["n_keys"]
 
 
 # ------------------------------------------------------------------ more of the attention
