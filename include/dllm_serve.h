@@ -76,7 +76,8 @@ typedef struct {
 /* Bits of status[0], kept until dllm_serve_check. */
 enum {
     DLLM_SERVE_TIMEOUT = 1,   /* a bounded wait ran out: outputs are not valid */
-    DLLM_SERVE_LENGTHS = 2,   /* a negative length, or more pages than max_pages: request refused */
+    DLLM_SERVE_LENGTHS = 2,   /* a negative length, more pages than max_pages, or more than 2^31 - 1 positions with
+                               * the prefix: request refused */
     DLLM_SERVE_PAGES = 4,     /* the pool ran out: request refused */
     DLLM_SERVE_ROWS = 8,      /* the new tokens are more than the plan's rows: the last ones are left out */
     DLLM_SERVE_PREFIX = 16,   /* fewer prefix pages than the plan's prefix_len needs, or one outside the pool */

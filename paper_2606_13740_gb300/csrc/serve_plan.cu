@@ -89,8 +89,8 @@ __device__ __forceinline__ Wants wants(const PlanArgs& a, int b) {
     w.rows = max(q, 0);
     w.state = held < 0 || held > a.s.max_pages;
     w.held = min(max(held, 0), a.s.max_pages);
-    const long long need = (static_cast<long long>(L) + q + a.s.page - 1) >> a.s.page_log2;
-    w.bad = w.state || L < 0 || q < 0 || need > a.s.max_pages;
+    const long long own = static_cast<long long>(L) + q, need = (own + a.s.page - 1) >> a.s.page_log2;
+    w.bad = w.state || L < 0 || q < 0 || need > a.s.max_pages || a.prefix_len + own > kMost;
     w.need = w.bad ? w.held : static_cast<int>(need);
     return w;
 }

@@ -184,6 +184,22 @@ def test_plan_lengths_at_the_end_of_32_bits(dev):
         assert bool(((out.double() - want).abs() <= U["bf16"] * want.abs() + (U["bf16"] + 2e-5) * size).all())
 
 
+def test_plan_positions_stay_within_32_bits(dev):
+    """Prefix and own positions together fit 32 bits, or the request is refused (half a gigabyte of lists)."""
+    from paper_2606_13740_gb300 import DllmError
+    n = (1 << 22) + 2
+    s = _serve(max_batch=2, max_rows=8, page=256, n_pages=n, max_pages=n, n_heads=4, n_kv_heads=2, head_dim=64)
+    P = (1 << 30) - 1
+    s.dllm_serve_plan(_i32([(1 << 30) - 2, 3]), _i32([2, 2]), 4, prefix_len=P)
+    s.dllm_serve_check()
+    assert s.pos[:4].cpu().tolist() == [2 ** 31 - 3, 2 ** 31 - 2, P + 3, P + 4] and s.n_keys.cpu().tolist() == [1 << 30, 5]
+    s.dllm_serve_plan(_i32([(1 << 30) - 1, 5]), _i32([2, 1]), 3, prefix_len=P)
+    assert s.pos[:3].cpu().tolist() == [0, 0, P + 5] and s.slot[:2].cpu().tolist() == [-1, -1]
+    assert s.n_keys.cpu().tolist() == [0, 6] and s.held.cpu().tolist() == [1 << 22, 1]
+    with pytest.raises(DllmError, match="status bits 2"):
+        s.dllm_serve_check()
+
+
 @pytest.mark.parametrize("B", [1, 7, 300, 4096])
 def test_plan_takes_its_own_key_counts_as_lengths(dev, B):
     """The step after: length is the plan's own n_keys, which it replaces."""
