@@ -22,7 +22,8 @@
  * the tables' status words, which dllm_serve_check reads: no such case writes
  * outside the buffers or disturbs the other requests.  Device pointers that a
  * call takes as arrays of 16-bit values are 16-byte aligned, their strides (in
- * elements) multiples of 8.
+ * elements) multiples of 8; those of 32-bit values are 4-byte aligned; what
+ * differs is said at the call.  Other ones are refused.
  */
 #ifndef DLLM_SERVE_H
 #define DLLM_SERVE_H

@@ -32,6 +32,12 @@ int sm_count() {
 }
 
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+// 32-bit values, or null
+template <typename... P>
+bool words(const P*... p) {
+    static_assert(((sizeof(P) == 4) && ...), "");
+    return (aligned(p, 4) && ...);
+}
 
 // Fills s from cfg; what is wrong with it, or null.
 const char* shape_of(const dllm_serve_config* c, ServeShape* s) {
@@ -73,7 +79,9 @@ const char* shape_of(const dllm_serve_config* c, ServeShape* s) {
 
 bool whole(const dllm_serve_tables* t) {
     return t && t->table && t->held && t->ring && t->ring_pos && t->row_start && t->n_keys && t->slot && t->pos && t->req &&
-           t->status && t->work && t->partials;
+           t->status && t->work && t->partials &&
+           words(t->table, t->held, t->ring, t->ring_pos, t->row_start, t->n_keys, t->slot, t->pos, t->req, t->status) &&
+           aligned(t->work, 16) && aligned(t->partials, 16);
 }
 
 int launched(cudaError_t e, const char* what) {
@@ -116,7 +124,7 @@ int dllm_serve_layout(const dllm_serve_config* cfg, void* mem, dllm_serve_tables
 int dllm_serve_reset(const dllm_serve_config* cfg, const dllm_serve_tables* t, void* stream) {
     ServeShape s;
     if (const char* why = shape_of(cfg, &s)) return fail(DLLM_EINVAL, "serve config: %s", why);
-    if (!whole(t)) return fail(DLLM_EINVAL, "serve tables: null buffer");
+    if (!whole(t)) return fail(DLLM_EINVAL, "serve tables: null or misaligned buffer");
     return launched(launch_serve_reset(s, *t, static_cast<cudaStream_t>(stream)), "serve reset");
 }
 
@@ -124,7 +132,7 @@ int dllm_serve_plan(const dllm_serve_config* cfg, const dllm_serve_tables* t, co
                     int batch, int rows, int prefix_len, int causal, void* stream) {
     ServeShape s;
     if (const char* why = shape_of(cfg, &s)) return fail(DLLM_EINVAL, "serve config: %s", why);
-    if (!whole(t) || !len || !q_len) return fail(DLLM_EINVAL, "serve plan: null buffer");
+    if (!whole(t) || !len || !q_len || !words(len, q_len)) return fail(DLLM_EINVAL, "serve plan: null or misaligned buffer");
     if (batch < 1 || batch > s.max_batch) return fail(DLLM_EINVAL, "serve plan: batch must be 1 to max_batch");
     if (rows < 0 || rows > s.max_rows) return fail(DLLM_EINVAL, "serve plan: rows must be 0 to max_rows");
     if (prefix_len < 0 || prefix_len > 0x3fffffff) return fail(DLLM_EINVAL, "serve plan: prefix_len must be 0 to 2^30 - 1");
@@ -142,7 +150,7 @@ int dllm_serve_qk_norm_rope(const dllm_serve_config* cfg, const dllm_serve_table
     ServeShape s;
     if (const char* why = shape_of(cfg, &s)) return fail(DLLM_EINVAL, "serve config: %s", why);
     if (!whole(t) || !theta || !kc || !vc || (rows > 0 && (!q || !k || !v || !q_out)))
-        return fail(DLLM_EINVAL, "qk_norm_rope: null buffer");
+        return fail(DLLM_EINVAL, "qk_norm_rope: null buffer, or misaligned tables");
     if (in_dtype != s.dtype && in_dtype != DLLM_F32)
         return fail(DLLM_EINVAL, "qk_norm_rope: in_dtype must be the config's dtype or DLLM_F32");
     if (rows < 0 || rows > s.max_rows) return fail(DLLM_EINVAL, "qk_norm_rope: rows must be 0 to max_rows");
@@ -169,7 +177,7 @@ int dllm_serve_attention(const dllm_serve_config* cfg, const dllm_serve_tables* 
     ServeShape s;
     if (const char* why = shape_of(cfg, &s)) return fail(DLLM_EINVAL, "serve config: %s", why);
     if (!whole(t) || !kc || !vc || (rows > 0 && (!q || !out)) || (n_prefix > 0 && !prefix_pages))
-        return fail(DLLM_EINVAL, "serve attention: null buffer");
+        return fail(DLLM_EINVAL, "serve attention: null buffer, or misaligned tables");
     if (rows < 0 || rows > s.max_rows) return fail(DLLM_EINVAL, "serve attention: rows must be 0 to max_rows");
     if (n_prefix < 0) return fail(DLLM_EINVAL, "serve attention: negative n_prefix");
     if (!(scale > 0.0f) || !std::isfinite(scale)) return fail(DLLM_EINVAL, "serve attention: scale must be positive");
@@ -178,6 +186,7 @@ int dllm_serve_attention(const dllm_serve_config* cfg, const dllm_serve_tables* 
     for (const void* p : {q, kc, vc, static_cast<const void*>(out)})
         if (!aligned(p, 16)) return fail(DLLM_EINVAL, "serve attention: buffers must be 16-byte aligned");
     if (!aligned(out, 32)) return fail(DLLM_EINVAL, "serve attention: out must be 32-byte aligned");
+    if (!words(prefix_pages, lse)) return fail(DLLM_EINVAL, "serve attention: prefix_pages and lse must be 4-byte aligned");
     if (rows == 0) return DLLM_OK;
     const int sms = sm_count();
     if (sms <= 0) return fail(DLLM_ECUDA, "no CUDA device");
@@ -213,7 +222,10 @@ int dllm_serve_logits(const dllm_serve_logits_args* a, void* stream) {
     if (a->dtype != DLLM_F32 && a->dtype != DLLM_BF16 && a->dtype != DLLM_F16) return fail(DLLM_EINVAL, "serve logits: unknown dtype");
     if (a->mask_id < -1 || a->mask_id >= a->vocab) return fail(DLLM_EINVAL, "serve logits: mask_id outside the vocabulary");
     const size_t size = a->dtype == DLLM_F32 ? 4 : 2;
-    if (!aligned(a->logits, size) || !aligned(a->out, size)) return fail(DLLM_EINVAL, "serve logits: misaligned buffer");
+    if (!aligned(a->logits, size) || !aligned(a->out, size) ||
+        !words(a->req, a->hist, a->hist_len, a->rep, a->freq, a->pres, a->bias_ids, a->bias, a->bias_len, a->grammar,
+               a->grammar_row, a->cur, a->x0, a->conf, a->tokconf))
+        return fail(DLLM_EINVAL, "serve logits: misaligned buffer");
     if (a->out && a->out == a->logits && a->ld_out != a->ld) return fail(DLLM_EINVAL, "serve logits: in place, ld_out is ld");
     if ((a->hist || a->bias_ids) && a->n_req < 1) return fail(DLLM_EINVAL, "serve logits: n_req must be positive");
     if (a->hist && (a->hist_ld < 0 || a->hist_ld >= 1 << 20)) return fail(DLLM_EINVAL, "serve logits: hist_ld must be below 2^20");

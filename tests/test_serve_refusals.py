@@ -1,4 +1,6 @@
-"""Refusals of the serving calls that need no GPU: devices that are not the current one, tensors that lie elsewhere."""
+"""Refusals of the serving calls that need no GPU: devices that are not the current one, tensors that lie elsewhere,
+pointers of 32-bit values that are not aligned."""
+import ctypes as C
 from types import SimpleNamespace
 
 import pytest
@@ -115,3 +117,47 @@ def test_logits_take_tensors_of_one_device(serve, monkeypatch):
         for index in (1, -1):
             with pytest.raises(ValueError):
                 call(**{name: index})
+
+
+P = 1 << 20  # an aligned address that no refused call follows
+
+
+def test_misaligned_words_are_refused():
+    """Lengths, pages, lists and results two bytes off, and tables: a kernel would fault on them."""
+    from paper_2606_13740_gb300 import serve
+    L = serve.serve_lib()
+    c = serve.ServeConfig(max_batch=4, max_rows=64, n_heads=4, n_kv_heads=2, head_dim=64).c()
+    cp = C.byref(c)
+
+    def tables(**off):
+        t = serve.dllm_serve_tables()
+        assert L.dllm_serve_layout(cp, 4096, C.byref(t), None) == 0
+        for k, v in off.items():
+            setattr(t, k, getattr(t, k) + v)
+        return C.byref(t)
+
+    def plan(length=P, q_len=P, t=None):
+        return L.dllm_serve_plan(cp, t or tables(), length, q_len, 2, 8, 0, 0, None)
+
+    def attention(pages=P, lse=P, t=None):
+        return L.dllm_serve_attention(cp, t or tables(), P, 256, P, P, pages, 1, 0.1, P, lse, 4, None)
+
+    def norm(t):
+        return L.dllm_serve_qk_norm_rope(cp, t, P, P, P, 0, 256, 128, 128, None, None, 1e-5, P, P, 256, P, P, 4, None)
+
+    assert plan(length=P + 2) == -1 and plan(q_len=P + 1) == -1
+    assert attention(pages=P + 2) == -1 and attention(lse=P + 2) == -1
+    for name, _ in serve.dllm_serve_tables._fields_:
+        off = 8 if name in ("work", "partials") else 2
+        for call in (plan, attention):
+            assert call(t=tables(**{name: off})) == -1, name
+        assert norm(tables(**{name: off})) == -1 and L.dllm_serve_reset(cp, tables(**{name: off}), None) == -1, name
+
+    n = C.c_size_t()
+    assert L.dllm_serve_logits_bytes(4, 1000, C.byref(n)) == 0
+    words = ("req hist hist_len rep freq pres bias_ids bias bias_len grammar grammar_row cur x0 conf tokconf").split()
+    for name in words:
+        a = serve.dllm_serve_logits_args(ld=1000, dtype=2, rows=4, vocab=1000, mask_id=-1, n_req=4, hist_ld=8, bias_ld=8,
+                                         n_grammar=1, ws_bytes=n.value, logits=P, ws=P, **{w: P for w in words})
+        setattr(a, name, P + 2)
+        assert L.dllm_serve_logits(C.byref(a), None) == -1, name
