@@ -124,7 +124,8 @@ int dllm_serve_plan(const dllm_serve_config* cfg, const dllm_serve_tables* t, co
  * (the config's dtype, or DLLM_F32): row r at r * ldq, r * ldk, r * ldv
  * elements, heads one after another.  q goes to q_out [rows][n_heads][head_dim]
  * (ld_out elements from row to row), k and v to their slots in kc and vc; a row
- * of slot -1 is not stored.  q_out may be q itself (same type and stride). */
+ * of slot -1 is not stored.  q_out may be q itself (same type and stride).
+ * rows: no more than the plan's (slots past them are an earlier plan's). */
 int dllm_serve_qk_norm_rope(const dllm_serve_config* cfg, const dllm_serve_tables* t, const void* q, const void* k,
                             const void* v, int in_dtype, int64_t ldq, int64_t ldk, int64_t ldv, const float* q_gain,
                             const float* k_gain, float eps, const float* theta, void* q_out, int64_t ld_out, void* kc,

@@ -224,6 +224,8 @@ class Serve:
                          self._row_stride("v", v, Hkv, dtype))
         if k.shape[0] != rows or v.shape[0] != rows:
             raise ValueError("q, k and v must have the same rows")
+        if 0 < self.rows < rows:
+            raise ValueError(f"q has {rows} rows, the plan {self.rows}: slots past them are an earlier plan's")
         if out is None:
             out, ld_out = self._empty((rows, H, self._hd), dtype=self._dt, device=self.device), H * self._hd
         else:

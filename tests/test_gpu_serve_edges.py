@@ -233,3 +233,17 @@ def test_attention_refuses_the_plan_of_another_head_dim(dev):
     with pytest.raises(DllmError, match="status bits 64"):
         s.dllm_serve_check()
     assert bool((out == 0).all())
+
+
+def test_norm_refuses_rows_past_the_plan(dev):
+    """Slots past a plan's rows are an earlier plan's."""
+    s = _serve(max_batch=2, max_rows=8, page=16, n_pages=8, max_pages=4, n_heads=4, n_kv_heads=2, head_dim=64)
+    s.dllm_serve_plan(_i32([0, 0]), _i32([4, 4]), 8)
+    s.dllm_serve_plan(_i32([4, 4]), _i32([1, 1]), 2)
+    x = torch.randn(8, 8 * 64, device="cuda").to(torch.bfloat16)
+    kc = torch.zeros(8, 2, 16, 64, device="cuda", dtype=torch.bfloat16)
+    vc, theta = torch.zeros_like(kc), torch.ones(32, device="cuda")
+    with pytest.raises(ValueError, match="rows"):
+        s.dllm_serve_qk_norm_rope(x[:, :256], x[:, 256:384], x[:, 384:], theta, kc, vc)
+    s.dllm_serve_qk_norm_rope(x[:2, :256], x[:2, 256:384], x[:2, 384:], theta, kc, vc)
+    assert int((kc != 0).any(-1).any(1).sum()) == 2
