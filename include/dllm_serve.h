@@ -138,7 +138,8 @@ int dllm_serve_qk_norm_rope(const dllm_serve_config* cfg, const dllm_serve_table
  * [rows][n_heads * head_dim], 32-byte aligned; lse dev fp32 [rows][n_heads], nullable: the
  * natural logarithm of the row's softmax sum.  A row that sees no key, and
  * padding, gives zeros (lse -inf).  Keys and values past a request's n_keys,
- * or past the prefix, may hold anything, infinities and NaN included.
+ * or past the prefix, may hold anything, infinities and NaN included; so may
+ * those that a row does not see, for that row.
  * rows: those of the plan.  scale > 0. */
 int dllm_serve_attention(const dllm_serve_config* cfg, const dllm_serve_tables* t, const void* q, int64_t ldq,
                          const void* kc, const void* vc, const int32_t* prefix_pages, int n_prefix, float scale,

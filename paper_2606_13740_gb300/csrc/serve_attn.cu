@@ -20,10 +20,13 @@
 // P V.  (With one warp for the loads and one for the MMAs each spent 2000 cycles a step on them, twice what
 // the tensor cores and the softmax take.)
 // Keys past a request's end score -inf, and their values, which may be anything, are set to 0 in shared memory.
+// In a block that causal rows see in part, values that are infinities or NaN are set to 0 as well, as 0 times them
+// would reach the rows before them, and added at the unit's end for the rows that see them.  (The look at these blocks
+// costs 5 causal prompts under 2000 2.6 us, made while the tensor cores make S; after the softmax it was 4.)
 // Bound: 0.78 us a step, in which S, softmax and P V of a tile wait for one another, the SM's two CTAs side by side.
 // Measured in a graph, join included: 16 windows of 32 under 4096 shared keys, 32 heads of 128, 55.5 us (189 MB at
 // least: 3.4 TB/s); 96 tokens under 8001, 28 heads over 4, 39.9 us (151 MB, 3.8 TB/s); 5 causal prompts under
-// 2000, 104.8 us (127 GFLOP: 1.21 PFLOP/s); one token under 300 keys 9.1 us.
+// 2000, 107.9 us (127 GFLOP: 1.18 PFLOP/s); one token under 300 keys 9.3 us.
 #include "serve.cuh"
 
 namespace dllm {
@@ -44,6 +47,7 @@ struct Sync {
     uint64_t qfull, qempty, drain[2], sfull[2], pfull[2], pvdone[2], kfull[NB], vfull[NB], kempty[NB], vempty[NB];
     uint32_t tmem;
     int abort;
+    int odd;  // infinities or NaN were taken out of a block of V
 };
 // (768: from the 256-byte alignment that dynamic shared memory has here to the tiles' 1024)
 template <int HD>
@@ -148,6 +152,14 @@ __device__ __forceinline__ uint32_t bit_run(int lo, int hi) {
     return lo == 32 ? 0u : up & ~((1u << lo) - 1u);
 }
 
+// Which of two 16-bit values are infinities or NaN: bits 15 and 31.
+template <typename T>
+__device__ __forceinline__ uint32_t odd_halves(uint32_t u) {
+    constexpr uint32_t kExp = std::is_same<T, __half>::value ? 0x7c007c00u : 0x7f807f80u;
+    constexpr uint32_t kOne = std::is_same<T, __half>::value ? 0x04000400u : 0x00800080u;
+    return ((u & kExp) + kOne) & 0x80008000u;
+}
+
 // One CTA's run of steps, unit by unit: the same walk in every role.
 struct Walk {
     const int2* tiles;
@@ -220,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, 2)
             mbar_init(&pfull[i], 4);
             mbar_init(&pvdone[i], 1);
         }
-        s_abort = 0;
+        s_abort = sy.odd = 0;
         mbar_fence_init();
     }
     if (warp == 4) {
@@ -467,6 +479,10 @@ __global__ void __launch_bounds__(kThreads, 2)
         auto wait = [&](uint64_t* bar, uint32_t parity) {
             return __all_sync(0xffffffffu, mbar_wait(bar, parity, &s_abort, t.status)) != 0;
         };
+        // whether the first live row of a block sees less than all of it (f: its info)
+        auto unseen = [&](const int4& f, int valid) {
+            return f.w + max(at.tile * s.tile_tokens, f.x) - f.x + 1 - f.z < valid;
+        };
         int j = 0;
         bool ok = true;
         do {
@@ -486,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                 // Keys of the block that there are, and that this row sees.  A row that is not live (of another
                 // request) computes on, unmasked, and keeps its m and l: its lane of O is not written.
                 int valid = kServeBlock, seen = kServeBlock;
-                bool live = true, masked = false, some = true, any_live = true;
+                bool live = true, masked = false, some = true, any_live = true, partly = false;
                 if (step >= full_blocks) {
                     if (step < prefix_blocks) {
                         valid = seen = prefix_len - step * kServeBlock;
@@ -495,10 +511,43 @@ __global__ void __launch_bounds__(kThreads, 2)
                         valid = min(kServeBlock, f.w + f.y - f.x - f.z);
                         live = there && tok >= f.x && tok < f.y;
                         seen = causal ? min(valid, f.w + tok - f.x + 1 - f.z) : valid;
+                        partly = causal && unseen(f, valid);
                     }
                     masked = __any_sync(0xffffffffu, live && seen < kServeBlock);
                     some = __any_sync(0xffffffffu, live && seen > 0);
                     any_live = __any_sync(0xffffffffu, live);
+                }
+                if (partly) {
+                    // Values that some row must not see: its P is 0, but an infinity or NaN would come through the MMA
+                    // all the same.  They are taken out (while S is made), and put to the rows that see them at the end.
+                    const int st = j % NB;
+                    ok = wait(&vfull[st], static_cast<uint32_t>((j / NB) & 1));
+                    if (!ok) break;
+                    uint4* v4 = reinterpret_cast<uint4*>(sV + st * kKV) + r;
+                    uint32_t odd = 0;
+#pragma unroll
+                    for (int k = 0; k < kServeBlock * 8; k += 128) {
+                        if (k + r >= valid * 8) break;
+#pragma unroll
+                        for (int h = 0; h < kParts; ++h) {
+                            const uint4 x = v4[h * (kHalfKV / 16) + k];
+                            odd |= odd_halves<T>(x.x) | odd_halves<T>(x.y) | odd_halves<T>(x.z) | odd_halves<T>(x.w);
+                        }
+                    }
+                    if (odd) {
+#pragma unroll 1
+                        for (int k = 0; k + r < valid * 8; k += 128) {
+                            for (int h = 0; h < kParts; ++h) {
+                                uint4& x = v4[h * (kHalfKV / 16) + k];
+                                x.x &= ~((odd_halves<T>(x.x) >> 15) * 0xffffu);
+                                x.y &= ~((odd_halves<T>(x.y) >> 15) * 0xffffu);
+                                x.z &= ~((odd_halves<T>(x.z) >> 15) * 0xffffu);
+                                x.w &= ~((odd_halves<T>(x.w) >> 15) * 0xffffu);
+                            }
+                        }
+                        *const_cast<volatile int*>(&sy.odd) = 1;
+                        fence_proxy_async_smem();
+                    }
                 }
                 ok = wait(&sfull[sb], static_cast<uint32_t>((j / 2) & 1));
                 if (!ok) break;
@@ -594,6 +643,41 @@ __global__ void __launch_bounds__(kThreads, 2)
             ok = wait(&pvdone[(j - 1) % 2], static_cast<uint32_t>(((j - 1) / 2) & 1));
             if (!ok) break;
             tc_fence_after();
+            if (__any_sync(0xffffffffu, *const_cast<volatile int*>(&sy.odd))) {
+                // The infinities and NaN of blocks that are seen in part, from the cache: whatever its weight, one
+                // that a row sees makes the feature what it is itself.  (sy.odd may be of another segment: then
+                // nothing is found.)
+                const T* vc = static_cast<const T*>(a.vc) + static_cast<long long>(at.hk) * s.page * HD;
+#pragma unroll 1
+                for (int c = 0; c < HD; c += 16) {
+                    float o[16];
+                    tmem_ld_32x16(t_o + static_cast<uint32_t>(c), o);
+#pragma unroll 1
+                    for (int step = max(at.step, prefix_blocks); step < at.step + at.n; ++step) {
+                        const int4 f = w.info[at.own0 + step - prefix_blocks], pg = w.pages[at.own0 + step - prefix_blocks];
+                        const int valid = min(kServeBlock, f.w + f.y - f.x - f.z);
+                        if (!there || tok < f.x || tok >= f.y || !unseen(f, valid)) continue;
+                        const int seen = min(valid, f.w + tok - f.x + 1 - f.z);
+#pragma unroll 1
+                        for (int k = 0; k < seen; ++k) {
+                            const int nth = s.page >= kServeBlock ? 0 : k >> s.page_log2;
+                            const int id = nth == 0 ? pg.x : nth == 1 ? pg.y : nth == 2 ? pg.z : pg.w;
+                            const int place = s.page >= kServeBlock ? pg.y + k : k & (s.page - 1);
+                            if (id < 0 || id >= s.n_pages) continue;
+                            const uint32_t* v = reinterpret_cast<const uint32_t*>(vc + id * s.page_stride + static_cast<long long>(place) * HD + c);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const uint32_t u = v[i], odd = odd_halves<T>(u);
+                                const float2 x = Half2<T>::unpack(u);
+                                if (odd & 0x8000u) o[2 * i] += x.x;
+                                if (odd & 0x80000000u) o[2 * i + 1] += x.y;
+                            }
+                        }
+                    }
+                    __syncwarp();
+                    tmem_st_32x16(t_o + static_cast<uint32_t>(c), o);
+                }
+            }
             const bool whole = at.whole();
             const float il = l != 0.0f ? 1.0f / l : 0.0f;
             const long long row_head = static_cast<long long>(tok) * s.H + at.hk * s.G + g;

@@ -235,6 +235,48 @@ def test_attention_refuses_the_plan_of_another_head_dim(dev):
     assert bool((out == 0).all())
 
 
+@pytest.mark.parametrize("H,Hkv,hd,dtype", [(28, 4, 128, "bf16"), (4, 4, 64, "f16"), (32, 32, 128, "f16"), (3, 1, 128, "bf16")])
+@pytest.mark.parametrize("L,Q,P,page", [([0, 100], [300, 70], 200, 16), ([5], [200], 0, 64), ([0, 0, 60], [1, 64, 9], 64, 128)])
+def test_causal_rows_do_not_see_later_values(dev, H, Hkv, hd, dtype, L, Q, P, page):
+    """Infinities and NaN among the values (and keys) of later tokens leave the rows before them as they are; the rows
+    that see them get what the softmax makes of them."""
+    x = Paged(L, Q, P, page, H, Hkv, hd, dtype=dtype, causal=True, seed=25)
+    clean = x.check()
+    table = x.s.table.cpu().tolist()
+    start = np.cumsum([0] + Q)
+    G = H // Hkv
+    ok = torch.ones(sum(Q), H, hd, dtype=torch.bool, device="cuda")
+    sums = torch.zeros(sum(Q), H, hd, device="cuda")
+    r, placed = np.random.default_rng(26), set()
+    for b in range(len(L)):
+        for _ in range(4):
+            t = int(r.integers(0, Q[b]))  # a new token's value
+            at, h, f = L[b] + t, int(r.integers(0, Hkv)), int(r.integers(0, hd))
+            v = float(r.choice([np.inf, -np.inf, np.nan]))
+            if (b, t, h, f) in placed:
+                continue
+            placed.add((b, t, h, f))
+            x.vc[table[b][at // page], h, at % page, f] = v
+            rows = slice(int(start[b]) + t, int(start[b + 1]))
+            ok[rows, h * G:(h + 1) * G, f] = False
+            sums[rows, h * G:(h + 1) * G, f] += v
+    out, lse = x.call(lse=True)
+    x.s.dllm_serve_check()
+    out = out.view(sum(Q), H, hd)
+    assert torch.equal(out[ok], clean.view(sum(Q), H, hd)[ok])
+    assert torch.equal(out[~ok].float().nan_to_num(7.0, 8.0, 9.0), sums[~ok].nan_to_num(7.0, 8.0, 9.0))
+    assert bool(torch.isfinite(lse).all())
+    # a key that is not a number: the rows from it on, all features
+    b = int(np.argmax(Q))
+    t = Q[b] // 2
+    at = L[b] + t
+    x.kc[table[b][at // page], 0, at % page, 0] = float("nan")
+    out = x.call().view(sum(Q), H, hd)
+    gone = torch.zeros_like(ok)
+    gone[int(start[b]) + t:int(start[b + 1]), :G] = True
+    assert bool(out[gone].isnan().all()) and torch.equal(out[ok & ~gone], clean.view(sum(Q), H, hd)[ok & ~gone])
+
+
 def test_norm_refuses_rows_past_the_plan(dev):
     """Slots past a plan's rows are an earlier plan's."""
     s = _serve(max_batch=2, max_rows=8, page=16, n_pages=8, max_pages=4, n_heads=4, n_kv_heads=2, head_dim=64)
