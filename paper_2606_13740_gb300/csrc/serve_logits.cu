@@ -428,17 +428,7 @@ __global__ void __launch_bounds__(128) k_merge(const __grid_constant__ dllm_serv
     pdl_wait();
     const int row = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (row >= a.rows) return;
-    if (a.grammar && a.grammar_row[row] >= 0 && a.grammar_row[row] >= a.n_grammar) {
-        if (a.out) {
-            T* z = static_cast<T*>(a.out) + static_cast<size_t>(row) * a.ld_out;
-            for (int v = lane; v < a.vocab; v += 32) Io<T>::put(z + v, -INFINITY);
-        }
-        if (lane) return;
-        if (a.x0) a.x0[row] = -1;
-        if (a.conf) a.conf[row] = 0.0f;
-        if (a.tokconf) a.tokconf[row] = 0.0f;
-        return;
-    }
+    const int g = a.grammar ? a.grammar_row[row] : -1;  // (looked at when the parts are there)
     float m = -INFINITY, s = 0.0f;
     int arg = a.vocab;
     constexpr int kAtOnce = 8;
@@ -463,6 +453,14 @@ __global__ void __launch_bounds__(128) k_merge(const __grid_constant__ dllm_serv
         s = s * (m == mx ? 1.0f : exp_below(m, mx)) + os * (om == mx ? 1.0f : exp_below(om, mx));
         arg = om > m ? oa : om < m ? arg : min(arg, oa);
         m = mx;
+    }
+    if (g >= 0 && g >= a.n_grammar) {
+        if (a.out) {
+            T* z = static_cast<T*>(a.out) + static_cast<size_t>(row) * a.ld_out;
+            for (int v = lane; v < a.vocab; v += 32) Io<T>::put(z + v, -INFINITY);
+        }
+        m = -INFINITY;
+        s = 0.0f;
     }
     if (lane) return;
     const bool some = s != 0.0f;  // (NaN too)
