@@ -42,7 +42,8 @@ enum { DLLM_BF16 = 0, DLLM_F16 = 1, DLLM_F32 = 2 };
  * page.  Slot s of the pool is place s % page of page s / page.
  * Constraints: max_batch <= 4096; page one of 16, 32, 64, 128, 256;
  * n_pages * page < 2^31; max_pages * page < 2^31; max_rows <= 2^22;
- * head_dim 64 or 128; n_kv_heads divides n_heads, n_heads / n_kv_heads <= 128;
+ * head_dim 64 or 128; n_heads <= 65536; n_kv_heads divides n_heads,
+ * n_heads / n_kv_heads <= 128;
  * dtype DLLM_BF16 or DLLM_F16. */
 typedef struct {
     int max_batch;  /* requests */
@@ -118,7 +119,7 @@ int dllm_serve_plan(const dllm_serve_config* cfg, const dllm_serve_tables* t, co
 
 /* Queries and keys of rows 0 .. rows - 1: RMSNorm of each head,
  * y = x * rsqrt(mean(x^2) + eps) * gain (gain dev fp32 [head_dim], 16-byte
- * aligned, null: ones),
+ * aligned, null: ones; the norm itself is always applied),
  * then rotate-half RoPE: features j and j + head_dim / 2 turned by
  * pos[row] * theta[j] (theta dev fp32 [head_dim / 2]).  q, k, v dev of in_dtype
  * (the config's dtype, or DLLM_F32): row r at r * ldq, r * ldk, r * ldv
@@ -140,7 +141,9 @@ int dllm_serve_qk_norm_rope(const dllm_serve_config* cfg, const dllm_serve_table
  * padding, gives zeros (lse -inf).  Keys and values past a request's n_keys,
  * or past the prefix, may hold anything, infinities and NaN included; so may
  * those that a row does not see, for that row.
- * rows: those of the plan.  scale > 0. */
+ * rows: those of the plan.  scale > 0.  Scores, sums and out's accumulation
+ * are fp32; the softmax's weights are rounded to dtype before the product with
+ * v (out's error is 1.4 times that of an fp32 softmax rounded once). */
 int dllm_serve_attention(const dllm_serve_config* cfg, const dllm_serve_tables* t, const void* q, int64_t ldq,
                          const void* kc, const void* vc, const int32_t* prefix_pages, int n_prefix, float scale,
                          void* out, float* lse, int rows, void* stream);

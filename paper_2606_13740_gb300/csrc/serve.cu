@@ -53,7 +53,7 @@ const char* shape_of(const dllm_serve_config* c, ServeShape* s) {
     if (c->head_dim != 64 && c->head_dim != 128) return "head_dim must be 64 or 128";
     if (c->n_heads < 1 || c->n_kv_heads < 1 || c->n_heads % c->n_kv_heads || c->n_heads / c->n_kv_heads > kServeRows ||
         c->n_heads > 1 << 16)
-        return "n_kv_heads must divide n_heads, in groups of at most 128";
+        return "n_heads must be 1 to 65536, and n_kv_heads divide it in groups of at most 128";
     if (c->dtype != DLLM_BF16 && c->dtype != DLLM_F16) return "dtype must be DLLM_BF16 or DLLM_F16";
     const long long dense = static_cast<long long>(c->n_kv_heads) * c->page * c->head_dim;
     if (c->page_stride != 0 && (c->page_stride < dense || c->page_stride % 8 || c->page_stride >= 1ll << 38))

@@ -24,9 +24,9 @@
 // would reach the rows before them, and added at the unit's end for the rows that see them.  (The look at these blocks
 // costs 5 causal prompts under 2000 2.6 us, made while the tensor cores make S; after the softmax it was 4.)
 // Bound: 0.78 us a step, in which S, softmax and P V of a tile wait for one another, the SM's two CTAs side by side.
-// Measured in a graph, join included: 16 windows of 32 under 4096 shared keys, 32 heads of 128, 55.5 us (189 MB at
-// least: 3.4 TB/s); 96 tokens under 8001, 28 heads over 4, 39.9 us (151 MB, 3.8 TB/s); 5 causal prompts under
-// 2000, 107.9 us (127 GFLOP: 1.18 PFLOP/s); one token under 300 keys 9.3 us.
+// Measured in a graph, join included: 16 windows of 32 under 4096 shared keys, 32 heads of 128, 56.2 us (189 MB at
+// least: 3.4 TB/s); 96 tokens under 8001, 28 heads over 4, 40.6 us (151 MB, 3.7 TB/s); 5 causal prompts under
+// 2000, 108.2 us (127 GFLOP: 1.17 PFLOP/s); one token under 300 keys 9.5 us.
 #include "serve.cuh"
 
 namespace dllm {

@@ -9,9 +9,10 @@
 // of exponentials and argmax in registers.  The ids asked for, few among many, leave that stream and are
 // taken 32 at a time from a list, in a fixed order: treated in the stream, they cost a warp the division for
 // nearly every 512 ids (20 instructions an id, 69 us for 512 rows of 126464).  k_merge joins a row's
-// stretches.  Bound: memory (logits once in, once out when asked for) and, with long lists, the instructions that
-// read them.  Measured in a graph: 512 rows of 126464 32-bit ids 60.5 us (262 MB, 4.3 TB/s; 47 with nothing asked for);
-// 96 single bf16 rows of 152064 ids with 5000 ids of history each, written out, 35.5 us (11 with nothing asked for, in L2).
+// stretches.  Bound: memory (logits once in, once out when asked for) and, with long lists, what each CTA does before it
+// streams: words, history, list.  Measured in a graph: 512 rows of 126464 32-bit ids 61.5 us (262 MB, 4.3 TB/s; 47 with
+// nothing asked for; 1024 CTAs on 608 places, DRAM 58 % busy, issue slots 44); 96 single bf16 rows of 152064 ids with
+// 5000 ids of history each, written out, 38.2 us (11 with nothing asked for, in L2).
 // (Clusters of 8 stretches that each read an eighth of a history and count in one another's shared memory: 61 us, as half
 // of a history falls into one stretch, which all of the cluster then waits for.)
 #include "serve.cuh"

@@ -9,7 +9,8 @@
 // whole turns fall off its top and the rotation is as exact at position 10^6 as at 1.  (In 64-bit floating
 // point, of which the SM does two operations a cycle, the angles of 1201 rows took a fifth of the call.)
 // Bound: memory, each value once in and once out.  Measured in a graph: 16384 rows of 96 heads of 128 (805 MB)
-// 130.5 us, 6.2 TB/s; 32 rows 2.8 us and 1201 rows of 36 heads 7.5 us, the latency of a row.
+// 131.3 us, 6.1 TB/s, and from 32 bits (1208 MB) 199.6, 6.05 TB/s, though that form spills some 70 bytes a thread; 32
+// rows 2.8 us, the latency of a row; 1201 rows of 36 heads 7.6 us (751 CTAs, and 80 registers leave places for 456).
 #include "serve.cuh"
 
 namespace dllm {

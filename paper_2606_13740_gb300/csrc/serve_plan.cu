@@ -9,7 +9,7 @@
 // the tiles took 30 us for 19500 of them.)  The state that all CTAs read (held, ring_pos) is replaced by the
 // CTA that has read it last.  Pages come from the ring's front and go to its end, so that what a plan takes and what
 // it gives back never meet: the free pages and those given back fit into the ring together.
-// Bound: latency of that chain.  Measured in a graph: 16 requests of 32 tokens 8.1 us, 1000 ragged prompts 15.1; the CTA that cuts the
+// Bound: latency of that chain.  Measured in a graph: 16 requests of 32 tokens 8.1 us, 1000 ragged prompts 15.0; the CTA that cuts the
 // runs ends last, so that fewer or more items a thread for the others change nothing.
 #include "serve.cuh"
 
@@ -20,7 +20,7 @@ namespace {
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMost = 0x7fffffff;
-constexpr int kStart = 10, kPrefix = 5, kOwnStep = 6;  // cost of a unit's start, of a prefix and of an own step
+constexpr int kStart = 10, kPrefix = 5, kOwnStep = 6;  // cost of a unit's start, of a prefix and of an own step (heads of 128)
 constexpr int kLeast = 12;                             // of a run
 
 struct PlanArgs {
@@ -95,7 +95,9 @@ __device__ __forceinline__ Wants wants(const PlanArgs& a, int b) {
     return w;
 }
 
-// sum of floor((x + k d) / m), k = 0 .. n - 1, by Euclid's steps on the lattice points under the line
+// sum of floor((x + k d) / m), k = 0 .. n - 1: the lattice points under a line.  Whole parts of d / m and x / m come
+// out as a closed form; what is left is counted along the other axis, which trades m and d (the reciprocity of such sums,
+// Graham, Knuth and Patashnik, Concrete Mathematics, 3.5), so that the steps are those of Euclid's algorithm.
 __device__ long long floor_sum(long long n, long long m, long long d, long long x) {
     long long sum = 0;
     while (n > 0) {
@@ -260,7 +262,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
         // -------------------------------------------- row starts, the CTAs' runs
         for (int b = threadIdx.x; b <= B; b += kThreads) t.row_start[b] = u.row[b];
         // The cost of a unit: its start, its prefix steps, its own steps; of all units of the tiles before tile i.
-        // (Measured, in prefix steps of 0.78 us: an own step 1.17, a unit's start and end 1.5 to 2.7.  Cut by steps
+        // (Measured at heads of 128, in prefix steps of 0.78 us: an own step 1.17, a unit's start and end 1.5 to 2.7.  Cut by steps
         // alone, the CTAs of 16 windows of 32 under 4096 shared keys ended between 34 and 47 us.)
         auto cost_of = [&](int i, long long steps) {  // of tile i, with cum(i)
             return i * (kStart + kPrefix * static_cast<long long>(pb)) + kOwnStep * (steps - static_cast<long long>(i) * pb);
