@@ -5,7 +5,7 @@
 #include <cuda_fp16.h>
 
 #include "../../include/dllm.h"
-#include "../../include/dllm_serve.h"
+#include "../../include/dllm_serve_drafts.h"
 #include "common.cuh"
 #include "internal.h"
 
@@ -41,8 +41,10 @@ struct ServeWork {
     int joins;           // units that several CTAs share
     long long total;     // steps of all units
     int shape[6];        // what the list was made for (serve_same_shape)
+    int batch;           // requests of the plan
+    int pad[3];
 };
-static_assert(sizeof(ServeWork) == 64, "the arrays behind it are 16-byte aligned");
+static_assert(sizeof(ServeWork) % 16 == 0, "the arrays behind it are 16-byte aligned");
 
 // Whether a work list was made for this config (calls with another one find its arrays elsewhere, or want larger
 // partials behind it).
@@ -64,6 +66,7 @@ __device__ inline bool serve_same_shape(const ServeShape& s, const ServeWork& w)
 
 struct ServeArrays {
     ServeWork* head;
+    int* shared;          // [kServeMaxBatch]: leading pages of a request that others hold too, of the last fork
     int4* join;           // [joins]: the unit's tile and K/V head, the first and the last CTA that holds a part of it
     int4* cta;            // [kServeCtas][2]: tile, K/V head, step within the unit, number of steps; the tile's entry
     int4* info;           // [max_blocks]: first and last + 1 row of the request, the block's first key, n_keys - rows
@@ -80,6 +83,8 @@ __host__ __device__ inline size_t serve_arrays(const ServeShape& s, void* base, 
     ServeArrays r;
     r.head = reinterpret_cast<ServeWork*>(b + at);
     at += serve_round(sizeof(ServeWork));
+    r.shared = reinterpret_cast<int*>(b + at);
+    at += serve_round(sizeof(int) * kServeMaxBatch);
     r.join = reinterpret_cast<int4*>(b + at);
     at += serve_round(sizeof(int4) * kServeCtas);
     r.cta = reinterpret_cast<int4*>(b + at);
@@ -156,11 +161,40 @@ struct ServeAttnArgs {
     void* out;
     float* lse;
     int rows;
+    const uint32_t* mask;  // [rows][words]: new tokens that a row sees (null: by the plan's causal)
+    int words;
 };
 cudaError_t launch_serve_attention(const ServeShape& s, const dllm_serve_tables& t, const ServeAttnArgs& a, int sms,
                                    cudaStream_t st);
+cudaError_t launch_serve_tree_attention(const ServeShape& s, const dllm_serve_tables& t, const ServeAttnArgs& a, int sms,
+                                        cudaStream_t st);
 size_t serve_partial_bytes(const ServeShape& s);
 size_t serve_logits_bytes(int rows, int vocab);
 cudaError_t launch_serve_logits(const dllm_serve_logits_args& a, int sms, cudaStream_t st);
+cudaError_t launch_serve_tree(const ServeShape& s, const dllm_serve_tables& t, const int* parent, uint32_t* mask, int words,
+                              int rows, int sms, cudaStream_t st);
+struct ServeAcceptArgs {
+    const int *parent, *ids, *x0;
+    int batch, rows, max_len;
+    int *keep, *n, *next;
+};
+cudaError_t launch_serve_accept(const ServeShape& s, const dllm_serve_tables& t, const ServeAcceptArgs& a, cudaStream_t st);
+// The caches of a model's layers.
+constexpr int kServeLayers = 128;
+struct ServeCaches {
+    void *k[kServeLayers], *v[kServeLayers];
+    int n;
+};
+struct ServeCompactArgs {
+    const int *first, *keep, *n;
+    int keep_ld, batch;
+};
+cudaError_t launch_serve_compact(const ServeShape& s, const dllm_serve_tables& t, const ServeCaches& c,
+                                 const ServeCompactArgs& a, int sms, cudaStream_t st);
+size_t serve_fork_bytes(const ServeShape& s);  // of the tables' partials
+cudaError_t launch_serve_fork(const ServeShape& s, const dllm_serve_tables& t, const ServeCaches& c, const int* src,
+                              const int* len, int batch, int sms, cudaStream_t st);
+size_t serve_logprobs_bytes(int rows, int vocab);
+cudaError_t launch_serve_logprobs(const dllm_serve_logprobs_args& a, int sms, cudaStream_t st);
 
 }  // namespace dllm

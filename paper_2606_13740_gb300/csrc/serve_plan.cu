@@ -82,15 +82,18 @@ __device__ __forceinline__ int find(const T* a, int n, T k) {
 struct Wants {
     int rows, held, need;  // new tokens, pages held and wanted
     bool bad, state;       // its lengths make no sense, or its held does not
+    bool shared;           // pages that others hold too would be given back or written to
 };
-__device__ __forceinline__ Wants wants(const PlanArgs& a, int b) {
-    const int L = load_in(a.len + b), q = load_in(a.q_len + b), held = a.t.held[b];
+__device__ __forceinline__ Wants wants(const PlanArgs& a, const int* shared, int b) {
+    const int L = load_in(a.len + b), q = load_in(a.q_len + b), held = a.t.held[b], others = shared[b];
     Wants w;
     w.rows = max(q, 0);
     w.state = held < 0 || held > a.s.max_pages;
     w.held = min(max(held, 0), a.s.max_pages);
     const long long own = static_cast<long long>(L) + q, need = (own + a.s.page - 1) >> a.s.page_log2;
     w.bad = w.state || L < 0 || q < 0 || need > a.s.max_pages || a.prefix_len + own > kMost;
+    w.shared = !w.bad && (need < others || (q > 0 && L >> a.s.page_log2 < others));
+    w.bad |= w.shared;
     w.need = w.bad ? w.held : static_cast<int>(need);
     return w;
 }
@@ -163,7 +166,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
     if (free0 != free_n || head0 != head) bits |= DLLM_SERVE_STATE;
     long long run[3] = {0, 0, 0}, all[3];
     for (int b = b0; b < b1; ++b) {
-        const Wants x = wants(a, b);
+        const Wants x = wants(a, w.shared, b);
         run[0] += x.rows;
         run[1] += max(x.need - x.held, 0);
         run[2] += max(x.held - x.need, 0);
@@ -185,7 +188,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
     };
     long long more[2] = {0, 0}, all_more[2];
     for (int b = b0; b < b1; ++b) {
-        const Wants x = wants(a, b);
+        const Wants x = wants(a, w.shared, b);
         const int grow = max(x.need - x.held, 0), L = load_in(a.len + b);
         u.row[b] = clip(run[0]);
         u.grow[b] = clip(run[1]);
@@ -195,6 +198,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
         run[1] += grow;
         const bool no = x.bad || (grow > 0 && run[1] > free_n);
         if (x.state) bits |= DLLM_SERVE_STATE;
+        else if (x.shared) bits |= DLLM_SERVE_SHARED;
         else if (x.bad) bits |= DLLM_SERVE_LENGTHS;
         else if (no) bits |= DLLM_SERVE_PAGES;
         if (!no && grow > 0) taken = max(taken, static_cast<int>(run[1]));
@@ -320,6 +324,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
             w.head->rows = fits ? rows : 0;
             w.head->total = total;
             w.head->joins = s_joins;
+            w.head->batch = B;
             serve_key(a.s, w.head->shape);
             t.status[1] = s_refused;
             t.status[2] = taken;
@@ -414,6 +419,9 @@ __global__ void k_serve_reset(ServeShape s, dllm_serve_tables t) {
     }
     if (i0 < 4) t.status[i0] = 0;
     if (i0 < 2) t.ring_pos[i0] = i0 ? s.n_pages : 0;
+    ServeArrays w;
+    serve_arrays(s, t.work, &w);
+    for (size_t i = i0; i < kServeMaxBatch; i += n) w.shared[i] = 0;
     if (i0 < sizeof(ServeWork) / 4) t.work[i0] = 0;
 }
 

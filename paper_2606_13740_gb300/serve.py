@@ -1,5 +1,6 @@
-"""Python binding of ``include/dllm_serve.h``: the operators that serve a batch of unequal requests over a
-paged K/V cache, under a prefix that all of them share.
+"""Python binding of ``include/dllm_serve.h`` and ``include/dllm_serve_drafts.h``: the operators that serve a batch of
+unequal requests over a paged K/V cache, under a prefix that all of them share, and those that decode from drafts and
+with several continuations.
 
 Argument marshalling only.  Calls run on torch's current stream and do not wait; what a kernel found wrong
 (lengths, a pool that ran out) is raised by ``Serve.dllm_serve_check``.  The library launches on the current
@@ -14,6 +15,7 @@ from dataclasses import dataclass
 from .dllm import _check, lib
 
 SERVE_TIMEOUT, SERVE_LENGTHS, SERVE_PAGES, SERVE_ROWS, SERVE_PREFIX, SERVE_SLOT, SERVE_STATE = 1, 2, 4, 8, 16, 32, 64
+SERVE_TREE, SERVE_SHARED = 128, 256
 DTYPES = {"bf16": 0, "f16": 1, "f32": 2}
 
 _P, _I, _F, _I64, _SZ = C.c_void_p, C.c_int, C.c_float, C.c_int64, C.c_size_t
@@ -37,6 +39,12 @@ class dllm_serve_logits_args(C.Structure):
                 ("tokconf", _P), ("ws", _P), ("ws_bytes", _SZ)]
 
 
+class dllm_serve_logprobs_args(C.Structure):
+    _fields_ = [("logits", _P), ("ld", _I64), ("dtype", _I), ("rows", _I), ("vocab", _I), ("mask_id", _I), ("tokens", _P),
+                ("n_tokens", _I), ("n_top", _I), ("lp", _P), ("entropy", _P), ("lse", _P), ("top_ids", _P), ("top_lp", _P),
+                ("ws", _P), ("ws_bytes", _SZ)]
+
+
 # name -> (restype, argtypes); every entry point of include/dllm_serve.h
 SIGNATURES = {
     "dllm_serve_layout": (_I, [_P, _P, _P, _P]),
@@ -48,16 +56,26 @@ SIGNATURES = {
     "dllm_serve_logits_bytes": (_I, [_I, _I, _P]),
     "dllm_serve_logits": (_I, [_P, _P]),
 }
+# and of include/dllm_serve_drafts.h
+DRAFT_SIGNATURES = {
+    "dllm_serve_tree": (_I, [_P, _P, _P, _P, _I, _I, _P]),
+    "dllm_serve_tree_attention": (_I, [_P, _P, _P, _I64, _P, _P, _P, _I, _F, _P, _I, _P, _P, _I, _P]),
+    "dllm_serve_accept": (_I, [_P, _P, _P, _P, _P, _I, _I, _I, _P, _P, _P, _P]),
+    "dllm_serve_compact": (_I, [_P, _P, _P, _P, _I, _P, _P, _I, _P, _I, _P]),
+    "dllm_serve_fork": (_I, [_P, _P, _P, _P, _I, _P, _P, _I, _P]),
+    "dllm_serve_logprobs_bytes": (_I, [_I, _I, _P]),
+    "dllm_serve_logprobs": (_I, [_P, _P]),
+}
 
 _lib = None
 
 
 def serve_lib():
-    """The library with this header's entry points typed."""
+    """The library with these headers' entry points typed."""
     global _lib
     if _lib is None:
         L = lib()
-        for name, (res, args) in SIGNATURES.items():
+        for name, (res, args) in {**SIGNATURES, **DRAFT_SIGNATURES}.items():
             fn = getattr(L, name)
             fn.restype = res
             fn.argtypes = args
@@ -124,6 +142,21 @@ def _logits_bytes(rows, vocab):
     return n.value
 
 
+@functools.cache
+def _logprobs_bytes(rows, vocab):
+    n = _SZ()
+    _check(serve_lib().dllm_serve_logprobs_bytes(rows, vocab, C.byref(n)))
+    return n.value
+
+
+class Layers:
+    """The caches of a model's layers, as Serve.layers looks them over."""
+
+    def __init__(self, kc, vc, pointers):
+        self.kc, self.vc, self.n = kc, vc, len(kc)
+        self.k, self.v = ((_P * self.n)(*p) for p in pointers)
+
+
 class Serve:
     """The buffers of one serving batch (a torch tensor), and the calls on them with the ABI's names.  The
     attributes table, held, ring, ring_pos, row_start, n_keys, slot, pos, req and status are int32 views of
@@ -167,7 +200,7 @@ class Serve:
         self.ring, self.ring_pos = view("ring", cfg.n_pages), view("ring_pos", 2)
         self.row_start, self.status = view("row_start", cfg.max_batch + 1), view("status", 4)
         self.slot, self.pos, self.req = (view(n, cfg.max_rows) for n in ("slot", "pos", "req"))
-        self.rows = self.prefix_len = 0
+        self.rows = self.prefix_len = self.batch = 0
         self.dllm_serve_reset()
 
     def _stream(self):
@@ -176,7 +209,7 @@ class Serve:
     def dllm_serve_reset(self):
         """Nothing held, every page free."""
         _check(self._L.dllm_serve_reset(self._cp, self._tp, self._stream()))
-        self.rows = self.prefix_len = 0
+        self.rows = self.prefix_len = self.batch = 0
 
     def dllm_serve_plan(self, length, q_len, rows, prefix_len=0, causal=False):
         """length, q_len: int32 CUDA tensors [batch], own positions cached and new tokens; rows: rows of the step's
@@ -189,7 +222,7 @@ class Serve:
                                      prefix_len, causal, self._stream())
         if rc:
             _check(rc)
-        self.rows, self.prefix_len = rows, prefix_len
+        self.rows, self.prefix_len, self.batch = rows, prefix_len, length.numel()
 
     def _row_stride(self, name, x, heads, dtype):
         """Elements from row to row of x: [rows][heads * head_dim] or [rows][heads][head_dim], rows dense."""
@@ -244,6 +277,17 @@ class Serve:
     def dllm_serve_attention(self, q, kc, vc, prefix_pages=None, scale=None, lse=False, out=None):
         """q [rows][n_heads][head_dim] of the plan's rows -> [rows][n_heads * head_dim] (with lse: and the
         logarithms of the softmax sums, fp32 [rows][n_heads])."""
+        return self._attend(q, kc, vc, None, prefix_pages, scale, lse, out)
+
+    def dllm_serve_tree_attention(self, q, kc, vc, mask, prefix_pages=None, scale=None, lse=False, out=None):
+        """dllm_serve_attention with bits: mask int32 [rows][words], bit j % 32 of word j // 32 for the request's new token
+        j; the keys cached before the plan, and the prefix, are seen all the same."""
+        if len(mask.shape) != 2:
+            raise ValueError(f"mask must be [rows][words], not {tuple(mask.shape)}")
+        return self._attend(q, kc, vc, (self._words("mask", mask, (q.shape[0], mask.shape[1])), mask.shape[1]), prefix_pages,
+                            scale, lse, out)
+
+    def _attend(self, q, kc, vc, mask, prefix_pages, scale, lse, out):
         rows, n_prefix, pages = q.shape[0], 0, None
         ldq = self._row_stride("q", q, self._H, self._dt)
         if rows != self.rows:
@@ -261,12 +305,76 @@ class Serve:
               or out.get_device() != self._index):
             raise ValueError("out must be contiguous, of q's rows, type and device")
         ls = self._empty((rows, self._H), dtype=self._f32, device=self.device) if lse else None
-        rc = self._L.dllm_serve_attention(self._cp, self._tp, q.data_ptr(), ldq, self._cache("kc", kc), self._cache("vc", vc),
-                                          pages, n_prefix, self._scale if scale is None else scale, out.data_ptr(),
-                                          None if ls is None else ls.data_ptr(), rows, self._stream())
+        call = self._L.dllm_serve_attention if mask is None else self._L.dllm_serve_tree_attention
+        rc = call(self._cp, self._tp, q.data_ptr(), ldq, self._cache("kc", kc), self._cache("vc", vc), pages, n_prefix,
+                  self._scale if scale is None else scale, *(mask or ()), out.data_ptr(),
+                  None if ls is None else ls.data_ptr(), rows, self._stream())
         if rc:
             _check(rc)
         return (out, ls) if lse else out
+
+    def _words(self, name, x, shape):
+        """Pointer of a contiguous int32 tensor of a shape on the handle's device."""
+        if x.dtype != self._i32 or x.shape != shape or x.get_device() != self._index or not x.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous int32 tensor {tuple(shape)} on cuda:{self._index}, not {x.dtype} "
+                             f"{tuple(x.shape)} on {x.device}")
+        return x.data_ptr()
+
+    def dllm_serve_tree(self, parent, bits, mask=None):
+        """parent int32 [rows] of the plan's rows: which new token of its request each one follows (an earlier one; -1: the
+        cached ones) -> mask int32 [rows][ceil(bits / 32)] of those that a row sees, itself among them; pos becomes the
+        tree's positions.  bits: as many as the largest tree has tokens, at least."""
+        rows, words = self.rows, -(-bits // 32)
+        at = self._words("parent", parent, (rows,))
+        if mask is None:
+            mask = self._empty((rows, words), dtype=self._i32, device=self.device)
+        rc = self._L.dllm_serve_tree(self._cp, self._tp, at, self._words("mask", mask, (rows, words)), words, rows, self._stream())
+        if rc:
+            _check(rc)
+        return mask
+
+    def dllm_serve_accept(self, parent, ids, x0, batch, max_len):
+        """parent, ids (the tokens) and x0 (what follows each of them, as decided) int32 of the plan's rows -> (keep, n,
+        next): the path of each request's tree that the decisions bear out, int32 [batch][max_len] (-1 behind it), its
+        length, and the decision at its end."""
+        rows = self.rows
+        at = [self._words(name, x, (rows,)) for name, x in (("parent", parent), ("ids", ids), ("x0", x0))]
+        keep = self._empty((batch, max_len), dtype=self._i32, device=self.device)
+        n = self._empty((batch,), dtype=self._i32, device=self.device)
+        nxt = self._empty((batch,), dtype=self._i32, device=self.device)
+        rc = self._L.dllm_serve_accept(self._cp, self._tp, *at, batch, rows, max_len, keep.data_ptr(), n.data_ptr(),
+                                       nxt.data_ptr(), self._stream())
+        if rc:
+            _check(rc)
+        return keep, n, nxt
+
+    def layers(self, kc, vc):
+        """The caches of all layers, for dllm_serve_compact and dllm_serve_fork: two sequences of tensors, or tensors
+        with a first dimension more."""
+        kc, vc = list(kc), list(vc)
+        if len(kc) != len(vc):
+            raise ValueError(f"{len(kc)} caches of keys, {len(vc)} of values")
+        return Layers(kc, vc, [[self._cache(name, x) for x in xs] for name, xs in (("kc", kc), ("vc", vc))])
+
+    def dllm_serve_compact(self, layers, first, keep, n):
+        """Own position first[b] + keep[b][i] goes to first[b] + i, for i < n[b], in all layers (of Serve.layers); keep
+        int32 [batch][any] ascends."""
+        batch, ld = keep.shape
+        rc = self._L.dllm_serve_compact(self._cp, self._tp, layers.k, layers.v, layers.n, self._words("first", first, (batch,)),
+                                        self._words("keep", keep, (batch, ld)), ld, self._words("n", n, (batch,)), batch,
+                                        self._stream())
+        if rc:
+            _check(rc)
+
+    def dllm_serve_fork(self, layers, src, length):
+        """Request b continues what src[b] held up to length[b] own positions (int32 [batch]): full pages are shared, the
+        last one is copied in all layers (of Serve.layers) unless nobody else holds it.  length 0 ends a request."""
+        if len(src.shape) != 1:
+            raise ValueError("src must be [batch]")
+        rc = self._L.dllm_serve_fork(self._cp, self._tp, layers.k, layers.v, layers.n, self._words("src", src, src.shape),
+                                     self._words("length", length, src.shape), src.numel(), self._stream())
+        if rc:
+            _check(rc)
 
     def dllm_serve_check(self):
         """Waits for the stream; raises DllmError for what the kernels found wrong since the last check."""
@@ -335,3 +443,43 @@ def dllm_serve_logits(logits, mask_id=-1, req=None, hist=None, hist_len=None, re
     if rc:
         _check(rc)
     return x0, conf, None if cur is None else tokconf
+
+
+def dllm_serve_logprobs(logits, tokens=None, mask_id=-1, top=0, ws=None):
+    """Under softmax(logits) over all ids but mask_id, logits [rows][vocab] (fp32, bf16 or f16): (lp, entropy, top_ids,
+    top_lp, lse), the log probabilities of tokens (int32 [rows][any]), the entropy, the `top` likeliest ids (ties: lowest
+    id) with theirs, and the logarithm of the softmax sum.  lp is None without tokens, top_ids and top_lp without top."""
+    import torch
+
+    shape, st = logits.shape, logits.stride()
+    if len(shape) != 2 or not logits.is_cuda or (shape[1] > 1 and st[1] != 1):
+        raise ValueError("logits must be a CUDA tensor [rows][vocab] with dense rows")
+    rows, vocab = shape
+    i32, f32, dev, index = torch.int32, torch.float32, logits.device, logits.get_device()
+    stream = _stream_on(index)
+    n_tokens = 0
+    if tokens is not None:
+        if (tokens.dtype != i32 or len(tokens.shape) != 2 or tokens.shape[0] != rows or tokens.get_device() != index
+                or not tokens.is_contiguous()):
+            raise ValueError(f"tokens must be a contiguous int32 tensor [{rows}][any] on {dev}, not {tokens.dtype} "
+                             f"{tuple(tokens.shape)} on {tokens.device}")
+        n_tokens = tokens.shape[1]
+    if not 0 <= top <= 32:
+        raise ValueError(f"top must be 0 to 32, not {top}")
+    if ws is None:
+        ws = torch.empty(_logprobs_bytes(rows, vocab), dtype=torch.uint8, device=dev)
+    elif ws.get_device() != index or not ws.is_contiguous():
+        raise ValueError(f"ws must be contiguous on {dev}")
+    lp = torch.empty((rows, n_tokens), dtype=f32, device=dev) if tokens is not None else None
+    entropy, lse = torch.empty((2, rows), dtype=f32, device=dev).unbind(0)
+    top_ids = torch.empty((rows, top), dtype=i32, device=dev) if top else None
+    top_lp = torch.empty((rows, top), dtype=f32, device=dev) if top else None
+    a = dllm_serve_logprobs_args(
+        logits.data_ptr(), st[0] if rows > 1 else max(st[0], vocab), _names().get(logits.dtype, -1), rows, vocab, mask_id,
+        tokens.data_ptr() if n_tokens else None, n_tokens, top, lp.data_ptr() if n_tokens else None, entropy.data_ptr(),
+        lse.data_ptr(), top_ids.data_ptr() if top else None, top_lp.data_ptr() if top else None, ws.data_ptr(),
+        ws.numel() * ws.element_size())
+    rc = serve_lib().dllm_serve_logprobs(C.byref(a), stream)
+    if rc:
+        _check(rc)
+    return lp, entropy, top_ids, top_lp, lse
