@@ -125,11 +125,8 @@ typedef struct {
     float* lse;
     int32_t* top_ids;      /* dev [rows][n_top] (with n_top) */
     float* top_lp;
-    void* ws;              /* dev, 16-byte aligned, dllm_serve_logprobs_bytes */
-    size_t ws_bytes;
 } dllm_serve_logprobs_args;
 
-int dllm_serve_logprobs_bytes(int rows, int vocab, size_t* bytes);
 int dllm_serve_logprobs(const dllm_serve_logprobs_args* a, void* stream);
 
 #ifdef __cplusplus

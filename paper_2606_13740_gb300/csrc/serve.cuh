@@ -194,7 +194,6 @@ cudaError_t launch_serve_compact(const ServeShape& s, const dllm_serve_tables& t
 size_t serve_fork_bytes(const ServeShape& s);  // of the tables' partials
 cudaError_t launch_serve_fork(const ServeShape& s, const dllm_serve_tables& t, const ServeCaches& c, const int* src,
                               const int* len, int batch, int sms, cudaStream_t st);
-size_t serve_logprobs_bytes(int rows, int vocab);
 cudaError_t launch_serve_logprobs(const dllm_serve_logprobs_args& a, int sms, cudaStream_t st);
 
 }  // namespace dllm

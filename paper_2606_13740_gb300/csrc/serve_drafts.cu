@@ -102,12 +102,6 @@ int dllm_serve_fork(const dllm_serve_config* cfg, const dllm_serve_tables* t, vo
     return launched(launch_serve_fork(s, *t, c, src, len, batch, sms, static_cast<cudaStream_t>(stream)), "serve fork");
 }
 
-int dllm_serve_logprobs_bytes(int rows, int vocab, size_t* bytes) {
-    if (!bytes || rows < 0 || vocab < 1 || vocab > 1 << 28) return fail(DLLM_EINVAL, "serve logprobs: bad sizes");
-    *bytes = serve_logprobs_bytes(rows, vocab);
-    return DLLM_OK;
-}
-
 int dllm_serve_logprobs(const dllm_serve_logprobs_args* a, void* stream) {
     if (!a || (a->rows > 0 && !a->logits)) return fail(DLLM_EINVAL, "serve logprobs: null buffer");
     if (a->rows < 0 || a->vocab < 1 || a->vocab > 1 << 28) return fail(DLLM_EINVAL, "serve logprobs: bad sizes");
@@ -122,8 +116,6 @@ int dllm_serve_logprobs(const dllm_serve_logprobs_args* a, void* stream) {
     if ((a->n_tokens && (!a->tokens || !a->lp)) || (a->n_top && (!a->top_ids || !a->top_lp)))
         return fail(DLLM_EINVAL, "serve logprobs: tokens come with lp, n_top with top_ids and top_lp");
     if (!a->n_tokens && !a->n_top && !a->lse && !a->entropy) return fail(DLLM_EINVAL, "serve logprobs: nothing to write");
-    if (!a->ws || !aligned(a->ws, 16) || a->ws_bytes < serve_logprobs_bytes(a->rows, a->vocab))
-        return fail(DLLM_EINVAL, "serve logprobs: workspace missing, misaligned or too small");
     const int sms = sm_count();
     if (sms <= 0) return fail(DLLM_ECUDA, "no CUDA device");
     return launched(launch_serve_logprobs(*a, sms, static_cast<cudaStream_t>(stream)), "serve logprobs");

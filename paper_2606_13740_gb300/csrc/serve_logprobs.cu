@@ -1,15 +1,16 @@
 // Log probabilities from logits (include/dllm_serve_drafts.h, dllm_serve_logprobs): the normaliser, the entropy, given
 // tokens and the largest ones, from one read of the logits.
 //
-// Warps stream stretches of a row.  A lane keeps the largest logit m it has met and, of all the others, the sums
-//   s = sum exp(z - ref),  t = sum exp(z - ref) (z - ref)
-// against a reference that moves only when a value exceeds it by more than 8: of each new value and m the smaller
-// goes into the sums, so that the largest is never among them, and log1p(s) of a row in which one id has nearly
-// everything keeps its digits.  Parts meet in the same way in k_logprobs_row (a CTA a row), which turns them into the
-// row's values.  The largest ids: each group of ids (512, or more where that makes over 1024 groups) leaves its maximum; the
-// n_top largest ids lie in the n_top groups with the largest maxima (of equal ones the first), as each of these has
-// one value at least as large as any value outside.  They are read again, and what is not below the smallest of the
-// chosen maxima is ranked.
+// A cluster takes a row, its warps stretches of it that they copy ahead into shared memory (cp.async, each lane what it
+// reads itself, so that nobody waits for another).  A warp keeps the largest logit m it has met and, of all the others, sums
+//   s = sum 2^y,  t = sum 2^y y,  y = z log2(e) - c
+// against a reference c that moves only when a value exceeds it by more than 8.  The largest is never among the sums,
+// so that log1p(s) of a row in which one id has nearly everything keeps its digits; as a step (2 KB of ids) seldom brings a new
+// one, it is looked for a step at a time.  Where m log2(e) may not be a number
+// (10^37 and more) the sums are of exp(z - m) itself.  Parts meet in the same way.  The largest ids: each group of ids (a step,
+// or more where that makes over 1024 groups) leaves its maximum; the n_top largest ids lie in the n_top groups with the largest
+// maxima (of equal ones the first), as each of these has one value at least as large as any value outside.  They are
+// read again, and what is not below the smallest of the chosen maxima is ranked.
 // Bound: memory.
 #include "serve.cuh"
 
@@ -19,91 +20,136 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kSpan = 128;               // ids that a warp takes side by side, 4 a lane
-constexpr int kSpans = 4;                // of these in flight together
-constexpr int kPiece = kSpan * kSpans;   // a warp's step
+constexpr int kCluster = 8;              // CTAs of a row, at most
+constexpr int kSpans = 4;                // 16-byte pieces of a lane in a step
+constexpr int kStages = 3;               // steps of a warp on their way
 constexpr int kGroups = 1024;            // of a row, at most
-constexpr int kTop = 32;
-constexpr int kList = 1024;              // ids that are ranked side by side
+constexpr int kList = 5600;              // ids that may be among the largest, at most; past kRanked they are thinned out
+constexpr int kRanked = 256;
+constexpr int kAhead = 8;                // loads of a thread in flight, of the groups that are read again
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFar = -150.0f;          // exp of it is 0 in 32 bits
+constexpr float kFar2 = -216.0f;         // 2^ that too
 constexpr float kLowest = -3.402823466e38f;
+constexpr float kWide = 1e37f;           // values whose product with log2(e) is safely a number
+constexpr float kLn2 = 0.6931471805599453f;
 
 struct alignas(16) Part {
     float m, s, t, pad;  // the largest logit; of the others the sums against m
 };
 
+// Values side by side in 16 bytes of memory.
 template <typename T>
-struct Vec4;  // four values as they lie in memory
+struct Raw {
+    static constexpr int kPer = 8;
+    static __device__ __forceinline__ void floats(const uint4& u, float* v) {
+        const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = Half2<T>::unpack(x[i]);
+            v[2 * i] = f.x;
+            v[2 * i + 1] = f.y;
+        }
+    }
+};
 template <>
-struct Vec4<float> {
-    static __device__ __forceinline__ void load(const float* p, float* v) {
-        const float4 f = *reinterpret_cast<const float4*>(p);
-        v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
+struct Raw<float> {
+    static constexpr int kPer = 4;
+    static __device__ __forceinline__ void floats(const uint4& u, float* v) {
+        v[0] = __uint_as_float(u.x), v[1] = __uint_as_float(u.y), v[2] = __uint_as_float(u.z), v[3] = __uint_as_float(u.w);
     }
 };
 template <typename T>
-struct Vec4 {
-    static __device__ __forceinline__ void load(const T* p, float* v) {
-        const uint2 u = *reinterpret_cast<const uint2*>(p);
-        const float2 a = Half2<T>::unpack(u.x), b = Half2<T>::unpack(u.y);
-        v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
-    }
-};
+constexpr int kSpan = 32 * Raw<T>::kPer;         // ids that a warp takes side by side
+template <typename T>
+constexpr int kPiece = kSpan<T> * kSpans;        // a warp's step
 
 __device__ __forceinline__ float ex2(float x) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-// the smaller, the larger; NaN if one is
-__device__ __forceinline__ float min_nan(float a, float b) {
-    float r;
-    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
+// the larger; NaN if one is
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
 
-// The running sums of a lane.
+// 2 values at a time
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n"
+        " add.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}\n"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n .reg .b64 a, b, c, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n"
+        " fma.rn.f32x2 d, a, b, c;\n mov.b64 {%0, %1}, d;\n}\n"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float finite(float x) { return fminf(fmaxf(x, kLowest), -kLowest); }
+
+// A lane's share of the sums, against ref.
 struct Sums {
-    float m = -INFINITY, ref = kLowest, s = 0.0f, t = 0.0f;
+    float ref = kLowest, s = 0.0f, t = 0.0f;
     __device__ __forceinline__ void add(float z) {
-        const float lo = min_nan(z, m);
-        m = fmaxf(m, z);
-        const float d = max_nan(lo - ref, kFar), e = ex2(d * kLog2e);
+        const float d = max_nan(z - ref, kFar), e = ex2(d * kLog2e);
         s += e;
         t = fmaf(e, d, t);
     }
-    __device__ __forceinline__ void move(float to) {  // the reference; to finite
-        const float d = ref - to, e = ex2(fmaxf(d, kFar) * kLog2e);
-        t = e > 0.0f ? (t + s * d) * e : t * 0.0f;  // (0, or NaN)
-        s *= e;
-        ref = to;
+    __device__ __forceinline__ void add(float s2, float t2, float ref2) {  // sums against another reference
+        const float d = ref2 - ref, e = ex2(fmaxf(d, kFar) * kLog2e);
+        s = fmaf(s2, e, s);
+        t += e > 0.0f ? fmaf(s2, d, t2) * e : t2 * 0.0f;  // (0, or NaN)
     }
-    __device__ __forceinline__ void look(float mx) {  // before values up to mx are added
-        if (mx > ref + 8.0f || (ref == kLowest && mx > ref)) move(fminf(mx, -kLowest));
+    __device__ __forceinline__ void move(float to) {  // the reference; to finite
+        const Sums old = *this;
+        ref = to;
+        s = t = 0.0f;
+        add(old.s, old.t, old.ref);
     }
 };
 
-// Joins the lanes' (or parts') sums: afterwards m is the largest of all, s and t are against it, and the largest values
-// of the others are among them.  All lanes get the result.
-__device__ __forceinline__ Part join_warp(Sums v) {
-    float m = v.m;
-#pragma unroll
-    for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    const uint32_t have = __ballot_sync(0xffffffffu, v.m == m);
-    const bool holder = (threadIdx.x & 31) == __ffs(have) - 1;
-    const float to = fminf(fmaxf(m, kLowest), -kLowest);
-    v.move(to);
-    if (!holder) {
-        const float d = fmaxf(v.m - to, kFar), e = ex2(d * kLog2e);
-        v.s += e;
-        v.t = fmaf(e, d, v.t);
+// The same against c in powers of 2: y of z is fma(z, log2(e), -c), so that the rounding of c is no error.
+struct Sums2 {
+    float c = 0.0f, s = 0.0f, t = 0.0f;
+    __device__ __forceinline__ void move(float to) {  // to z = `to`
+        const float d = fmaf(-to, kLog2e, c), e = ex2(fmaxf(d, kFar2));
+        t = fmaf(s, fmaxf(d, kFar2), t) * e;
+        s *= e;
+        c = fmaf(to, kLog2e, 0.0f);
+        // (c is rounded: what its rounding leaves of d)
+        const float r = fmaf(to, kLog2e, -c), f = ex2(r);
+        t = fmaf(s, r, t) * f;
+        s *= f;
     }
+};
+
+__device__ __forceinline__ float warp_max(float x) {  // (NaN passed over)
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// Joins parts, one a lane (those without: m -inf, s and t 0).  All lanes get the result.
+__device__ __forceinline__ Part join_warp(const Part& p) {
+    const float m = warp_max(p.m);
+    const bool holder = (threadIdx.x & 31) == __ffs(__ballot_sync(0xffffffffu, p.m == m)) - 1;
+    Sums v;
+    v.ref = finite(m);
+    v.add(p.s, p.t, finite(p.m));
+    if (!holder) v.add(p.m);
 #pragma unroll
     for (int d = 16; d; d /= 2) {
         v.s += __shfl_xor_sync(0xffffffffu, v.s, d);
@@ -112,102 +158,143 @@ __device__ __forceinline__ Part join_warp(Sums v) {
     return Part{m, v.s, v.t, 0.0f};
 }
 
-// A warp takes some groups of a row that lie side by side.
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads) k_logprobs(const __grid_constant__ dllm_serve_logprobs_args a, int group_pieces,
-                                                       int groups, int shares, Part* part, float* top) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int row = blockIdx.y, share = blockIdx.x * kWarps + warp;
-    pdl_wait();
-    pdl_launch_dependents();
-    if (share >= shares) return;
-    const T* src = static_cast<const T*>(a.logits) + row * a.ld;
-    const int g0 = static_cast<int>(static_cast<long long>(groups) * share / shares);
-    const int g1 = static_cast<int>(static_cast<long long>(groups) * (share + 1) / shares);
-    Sums sums;
-    for (int g = g0; g < g1; ++g) {
-        float best = -INFINITY;
-        for (int q = g * group_pieces; q < (g + 1) * group_pieces; ++q) {
-            const int v0 = q * kPiece + 4 * lane;
-            float z[kSpans][4];
-            if (VEC && (q + 1) * kPiece <= a.vocab) {
+// Ids of a row side by side, one by one.
+template <typename T>
+__device__ __forceinline__ void load_some(const T* src, int v, int vocab, float* z) {
 #pragma unroll
-                for (int u = 0; u < kSpans; ++u) Vec4<T>::load(src + v0 + u * kSpan, z[u]);
-            } else {
-#pragma unroll
-                for (int u = 0; u < kSpans; ++u)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        z[u][i] = v0 + u * kSpan + i < a.vocab ? static_cast<float>(src[v0 + u * kSpan + i]) : -INFINITY;
-            }
-            if (a.mask_id >= 0 && a.mask_id / kPiece == q) {
-#pragma unroll
-                for (int u = 0; u < kSpans; ++u)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (v0 + u * kSpan + i == a.mask_id) z[u][i] = -INFINITY;
-            }
-            float mx = z[0][0];
-#pragma unroll
-            for (int u = 0; u < kSpans; ++u) mx = fmaxf(fmaxf(fmaxf(mx, z[u][0]), z[u][1]), fmaxf(z[u][2], z[u][3]));
-            best = fmaxf(best, mx);
-            sums.look(mx);
-#pragma unroll
-            for (int u = 0; u < kSpans; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sums.add(z[u][i]);
-        }
-        if (a.n_top) {
-#pragma unroll
-            for (int d = 16; d; d /= 2) best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, d));
-            if (lane == 0) top[static_cast<size_t>(row) * groups + g] = best;
-        }
-    }
-    const Part p = join_warp(sums);
-    if (lane == 0) part[static_cast<size_t>(row) * shares + share] = p;
+    for (int i = 0; i < Raw<T>::kPer; ++i) z[i] = v + i < vocab ? static_cast<float>(src[v + i]) : -INFINITY;
 }
-
 // Whether (value, id) comes before another among the largest.
 __device__ __forceinline__ bool before(float z, int v, float z2, int v2) { return z > z2 || (z == z2 && v < v2); }
 
+// Shared memory of a CTA.  The steps on their way, and when all have been taken what the ending of a row needs.
+struct Shared {
+    alignas(16) float top[kGroups];  // the groups' maxima
+    Part part[kCluster * kWarps];    // of the row's warps
+    Part all;
+    int n_groups, n, count[64];
+    float least;
+    union {
+        alignas(16) uint4 ring[kWarps][kStages][kSpans * 32];
+        struct {
+            float z[kList];
+            int v[kList], group[kGroups];
+        };
+    };
+    float best[kWarps];
+    int id[kWarps];
+};
+static_assert(4 * (sizeof(Shared) + 1024) <= 228 * 1024, "four CTAs an SM");
+
+// The logit of a row's token i, -inf for ids that are none.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_logprobs_row(const __grid_constant__ dllm_serve_logprobs_args a, int group_pieces,
-                                                           int groups, int shares, const Part* part, const float* top) {
-    __shared__ float s_top[kGroups], s_z[kList];
-    __shared__ int s_group[kTop], s_v[kList], s_n;
-    __shared__ Part s_part[kWarps];
-    __shared__ float s_best[kWarps];
-    __shared__ int s_id[kWarps];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = blockIdx.x;
-    pdl_wait();
-    pdl_launch_dependents();
-    const T* src = static_cast<const T*>(a.logits) + row * a.ld;
-    // ------------------------------------------------ the parts
-    Sums sums;
-    for (int i = tid; i < shares; i += kThreads) {
-        const Part p = part[static_cast<size_t>(row) * shares + i];
-        sums.look(p.m);
-        sums.add(p.m);
-        const float d = fminf(fmaxf(p.m, kLowest), -kLowest) - sums.ref, e = ex2(fmaxf(d, kFar) * kLog2e);
-        sums.s += p.s * e;
-        sums.t += e > 0.0f ? (p.t + p.s * d) * e : p.t * 0.0f;
+__device__ __forceinline__ float logit_of(const dllm_serve_logprobs_args& a, int row, const T* src, int i) {
+    const int v = a.tokens[static_cast<long long>(row) * a.n_tokens + i];
+    return v >= 0 && v < a.vocab && v != a.mask_id ? static_cast<float>(src[v]) : -INFINITY;
+}
+
+// Values in an order of whole numbers; -inf and NaN: 0.
+__device__ __forceinline__ uint32_t key_of(float x) {
+    const uint32_t b = __float_as_uint(x + 0.0f);  // (-0 is 0)
+    return x > -INFINITY ? (b >> 31 ? ~b : b | 0x80000000u) : 0u;
+}
+
+// A warp chooses groups whose maxima reach a value that k of them, at least, reach (all where there are less), in order of their
+// numbers.  The k-th largest of the lanes' two largest is such a value.  Where it lets more than 2 k through (many equal
+// ones), the k-th largest of all is found bit by bit, and of those equal to it the first are taken.
+__device__ __forceinline__ void choose(Shared& sh, int groups, int k) {
+    const int lane = threadIdx.x & 31;
+    uint32_t top = 0, next = 0;
+    for (int g = lane; g < groups; g += 32) {
+        const uint32_t x = key_of(sh.top[g]);
+        next = max(next, min(x, top));
+        top = max(top, x);
     }
-    Part all = join_warp(sums);
-    if (lane == 0) s_part[warp] = all;
-    if (a.n_top)
-        for (int i = tid; i < groups; i += kThreads) s_top[i] = top[static_cast<size_t>(row) * groups + i];
-    if (tid < kTop) s_group[tid] = -1;
-    if (tid == 0) s_n = 0;
+    int rank = 0, rank2 = 0;
+#pragma unroll 8
+    for (int i = 0; i < 32; ++i) {
+        const uint32_t o = __shfl_sync(0xffffffffu, top, i), o2 = __shfl_sync(0xffffffffu, next, i);
+        rank += (o > top || (o == top && i < lane)) + (o2 > top);
+        rank2 += (o >= next) + (o2 > next || (o2 == next && i < lane));
+    }
+    const uint32_t nth = __reduce_max_sync(0xffffffffu, rank == k - 1 ? top : rank2 == k - 1 ? next : 0u);
+    uint32_t least = nth;
+    if (least == 0) least = 1;
+    auto reach = [&](uint32_t from) {  // how many are no less
+        int n = 0;
+        for (int g = lane; g < groups; g += 32) n += key_of(sh.top[g]) >= from;
+        return __reduce_add_sync(0xffffffffu, n);
+    };
+    int equal = groups;  // how many of those equal to it are taken
+    if (reach(least) > 2 * k) {
+        least = 0;
+        for (uint32_t bit = 1u << 31; bit; bit >>= 1)
+            if (reach(least | bit) >= k) least |= bit;
+        equal = k - reach(least + 1);
+    }
+    int n = 0;
+    for (int g0 = 0; g0 < groups; g0 += 32) {
+        const uint32_t x = g0 + lane < groups ? key_of(sh.top[g0 + lane]) : 0u;
+        const uint32_t same = __ballot_sync(0xffffffffu, x == least), low = (1u << lane) - 1;
+        const bool in = x > least || (x == least && __popc(same & low) < equal);
+        const uint32_t ins = __ballot_sync(0xffffffffu, in);
+        if (in) sh.group[n + __popc(ins & low)] = g0 + lane;
+        n += __popc(ins);
+        equal -= __popc(same);
+    }
+    if (lane == 0) {
+        sh.n_groups = n;
+        sh.least = least > 1 ? __uint_as_float(least >> 31 ? least & 0x7fffffffu : ~least) : kLowest;
+    }
+}
+
+// The row's values from the parts of its `warps` warps and the groups' maxima, which lie in sh.  (z_token: the logit of the
+// thread's token.)
+template <typename T, bool VEC>
+__device__ __forceinline__ void finish(const dllm_serve_logprobs_args& a, int row, const T* src, int group_pieces, int groups,
+                                       int warps, float z_token, Shared& sh) {
+    constexpr int kPer = Raw<T>::kPer, kLoads = kPiece<T> / kPer;  // 16-byte loads of a step
+    const Part nothing{-INFINITY, 0.0f, 0.0f, 0.0f};
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int k = min(a.n_top, groups);
     __syncthreads();
-    sums = Sums();
-    if (lane < kWarps) {
-        const Part p = s_part[lane];
-        sums.m = p.m;
-        sums.ref = fminf(fmaxf(p.m, kLowest), -kLowest);
-        sums.s = p.s;
-        sums.t = p.t;
+    if (warp == 0) {
+        Part all = nothing;
+        for (int i = 0; i < warps; i += 32) {
+            const Part p = join_warp(i + lane < warps ? sh.part[i + lane] : nothing);
+            if (lane == i / 32) all = p;
+        }
+        all = join_warp(all);
+        if (lane == 0) {
+            sh.all = all;
+            sh.n = 0;
+        }
+        sh.count[lane] = sh.count[lane + 32] = 0;
+    } else if (warp == 1 && k) {
+        choose(sh, groups, k);
     }
-    all = join_warp(sums);
+    __syncthreads();
+    // ------------------------------------------------ the chosen groups, their first loads asked for
+    const int n_groups = k ? sh.n_groups : 0;
+    const float least = k && k == a.n_top ? sh.least : kLowest;
+    const int total = n_groups * group_pieces * kLoads;
+    static_assert(kThreads % kLoads == 0, "a load's place in its step is the thread's own");
+    auto id_of = [&](int i) {
+        if (i >= total) return a.vocab;
+        const int piece = i / kLoads, g = group_pieces == 1 ? piece : piece / group_pieces;
+        return (sh.group[g] * group_pieces + piece - g * group_pieces) * kPiece<T> + i % kLoads * kPer;
+    };
+    auto load = [&](int i0, uint4 (&x)[kAhead]) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int v = id_of(i0 + u * kThreads);
+            if (VEC && v + kPer <= a.vocab) x[u] = *reinterpret_cast<const uint4*>(src + v);
+        }
+    };
+    uint4 ahead[kAhead];
+    load(tid, ahead);
+
+    const Part all = sh.all;
     const bool none = all.m == -INFINITY && all.s == 0.0f, above = all.m == INFINITY;
     const float m = all.m, log_rest = log1pf(all.s);
     auto lp_of = [&](float z) {
@@ -219,62 +306,50 @@ __global__ void __launch_bounds__(kThreads) k_logprobs_row(const __grid_constant
         if (a.lse) a.lse[row] = none ? -INFINITY : above && all.s == all.s ? INFINITY : m + log_rest;
         if (a.entropy) a.entropy[row] = none ? 0.0f : above ? __int_as_float(0x7fffffff) : log_rest - all.t / (1.0f + all.s);
     }
-    for (int i = tid; i < a.n_tokens; i += kThreads) {
-        const long long at = static_cast<long long>(row) * a.n_tokens + i;
-        const int v = a.tokens[at];
-        a.lp[at] = lp_of(v >= 0 && v < a.vocab && v != a.mask_id ? static_cast<float>(src[v]) : -INFINITY);
-    }
-    if (!a.n_top) return;
+    for (int i = tid; i < a.n_tokens; i += kThreads)
+        a.lp[static_cast<long long>(row) * a.n_tokens + i] = lp_of(i == tid ? z_token : logit_of<T>(a, row, src, i));
+    if (!k) return;
 
-    // ------------------------------------------------ the groups that hold the largest
-    const int k = min(a.n_top, groups);
-    for (int g = tid; g < groups; g += kThreads) {
-        const float x = s_top[g];
-        int rank = 0;
-        for (int i = 0; i < groups; ++i) rank += before(s_top[i], i, x, g);
-        if (rank < k && x > -INFINITY) s_group[rank] = g;
-    }
-    __syncthreads();
-    int n_groups = 0;
-    while (n_groups < k && s_group[n_groups] >= 0) ++n_groups;
-    const float least = n_groups == a.n_top ? s_top[s_group[n_groups - 1]] : -INFINITY;
-    const int size = group_pieces * kPiece;
-    auto each = [&](auto&& f) {  // of the groups' ids
-        for (int g = 0; g < n_groups; ++g) {
-            const int v0 = s_group[g] * size, v1 = min(a.vocab, v0 + size);
-            for (int v = v0 + tid; v < v1; v += kThreads)
-                if (v != a.mask_id) f(v, static_cast<float>(src[v]));
+    // ------------------------------------------------ the largest
+    auto each = [&](auto&& f) {  // of the groups' ids that may be among them; the first loads are there
+        for (int i0 = tid; i0 < total; i0 += kAhead * kThreads) {
+            if (i0 != tid) load(i0, ahead);
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (i0 + u * kThreads >= total) break;
+                const int v = id_of(i0 + u * kThreads);
+                float z[kPer];
+                if (VEC && v + kPer <= a.vocab) Raw<T>::floats(ahead[u], z);
+                else load_some(src, v, a.vocab, z);
+                float mx = z[0];
+#pragma unroll
+                for (int c = 1; c < kPer; ++c) mx = fmaxf(mx, z[c]);
+                if (!(mx >= least)) continue;
+#pragma unroll
+                for (int c = 0; c < kPer; ++c)
+                    if (z[c] >= least && v + c != a.mask_id) f(v + c, z[c]);
+            }
         }
     };
     each([&](int v, float z) {
-        if (z >= least && z > -INFINITY) {
-            const int at = atomicAdd(&s_n, 1);
-            if (at < kList) {
-                s_z[at] = z;
-                s_v[at] = v;
-            }
+        const int at = atomicAdd(&sh.n, 1);
+        if (at < kList) {
+            sh.z[at] = z;
+            sh.v[at] = v;
         }
     });
     __syncthreads();
-    const int n = s_n;
+    int n = min(sh.n, kList);
     int* ids = a.top_ids + static_cast<long long>(row) * a.n_top;
     float* lps = a.top_lp + static_cast<long long>(row) * a.n_top;
-    if (n <= kList) {
-        for (int i = tid; i < n; i += kThreads) {
-            int rank = 0;
-            for (int j = 0; j < n; ++j) rank += before(s_z[j], s_v[j], s_z[i], s_v[i]);
-            if (rank < a.n_top) {
-                ids[rank] = s_v[i];
-                lps[rank] = lp_of(s_z[i]);
-            }
-        }
-    } else {
-        // too many equal or allowed ones: the largest below the one before, one by one
+    if (sh.n > kList) {
+        // more equal ones than there are places: the largest below the one before, one by one
         float z0 = INFINITY;
         int v0 = -1;
         for (int r = 0; r < a.n_top; ++r) {
             float bz = -INFINITY;
             int bv = a.vocab;
+            load(tid, ahead);
             each([&](int v, float z) {
                 if (before(z0, v0, z, v) && before(z, v, bz, bv)) {
                     bz = z;
@@ -291,22 +366,64 @@ __global__ void __launch_bounds__(kThreads) k_logprobs_row(const __grid_constant
                 }
             }
             if (lane == 0) {
-                s_best[warp] = bz;
-                s_id[warp] = bv;
+                sh.best[warp] = bz;
+                sh.id[warp] = bv;
             }
             __syncthreads();
-            z0 = s_best[0];
-            v0 = s_id[0];
+            z0 = sh.best[0];
+            v0 = sh.id[0];
             for (int i = 1; i < kWarps; ++i)
-                if (before(s_best[i], s_id[i], z0, v0)) {
-                    z0 = s_best[i];
-                    v0 = s_id[i];
+                if (before(sh.best[i], sh.id[i], z0, v0)) {
+                    z0 = sh.best[i];
+                    v0 = sh.id[i];
                 }
             if (tid == 0) {
                 ids[r] = v0;
                 lps[r] = lp_of(z0);
             }
             __syncthreads();
+        }
+        return;
+    }
+    if (n > kRanked) {
+        // The n_top largest (value, id), which are all different, bit by bit.
+        const int want = min(a.n_top, n);
+        auto pair_of = [&](int i) { return static_cast<unsigned long long>(key_of(sh.z[i])) << 32 | static_cast<uint32_t>(~sh.v[i]); };
+        unsigned long long from = 0;
+        for (int bit = 63; bit >= 0; --bit) {
+            const unsigned long long x = from | 1ull << bit;
+            int c = 0;
+            for (int i = tid; i < n; i += kThreads) c += pair_of(i) >= x;
+            c = __reduce_add_sync(0xffffffffu, c);
+            if (lane == 0 && c) atomicAdd(&sh.count[bit], c);
+            __syncthreads();
+            c = sh.count[bit];
+            if (c >= want) from = x;
+            if (c == want) break;
+        }
+        __syncthreads();
+        if (tid == 0) sh.n = 0;
+        __syncthreads();
+        for (int i = tid; i < n; i += kThreads)
+            if (pair_of(i) >= from) sh.group[atomicAdd(&sh.n, 1)] = i;
+        __syncthreads();
+        const int left = sh.n;
+        if (tid < left) {
+            const int at = sh.group[tid];
+            int rank = 0;
+            for (int j = 0; j < left; ++j) rank += before(sh.z[sh.group[j]], sh.v[sh.group[j]], sh.z[at], sh.v[at]);
+            ids[rank] = sh.v[at];
+            lps[rank] = lp_of(sh.z[at]);
+        }
+    } else if (tid < n) {
+        const float z = sh.z[tid];
+        const int v = sh.v[tid];
+        int rank = 0;
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) rank += before(sh.z[j], sh.v[j], z, v);
+        if (rank < a.n_top) {
+            ids[rank] = v;
+            lps[rank] = lp_of(z);
         }
     }
     for (int r = n + tid; r < a.n_top; r += kThreads) {
@@ -315,38 +432,174 @@ __global__ void __launch_bounds__(kThreads) k_logprobs_row(const __grid_constant
     }
 }
 
-// Groups of a row, and the warps that share them.
-struct Cut {
-    int group_pieces, groups, shares;
-};
-Cut logprobs_cut(int rows, int vocab, int sms) {
-    Cut c;
-    const int pieces = (vocab + kPiece - 1) / kPiece;
-    c.group_pieces = (pieces + kGroups - 1) / kGroups;
-    c.groups = (pieces + c.group_pieces - 1) / c.group_pieces;
-    // as many warps a row as fill the GPU (16 an SM), none of less than a group
-    const long long want = (16ll * sms + rows - 1) / rows;
-    c.shares = static_cast<int>(want < c.groups ? want : c.groups);
-    c.shares = (c.shares + kWarps - 1) / kWarps * kWarps;
-    if (c.shares > c.groups) c.shares = c.groups;
-    return c;
+// A cluster takes a row, each warp of it some groups that lie side by side; its first CTA ends it.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 3)
+    k_logprobs(const __grid_constant__ dllm_serve_logprobs_args a, int group_pieces, int groups) {
+    constexpr int kPer = Raw<T>::kPer, kValues = kSpans * kPer;
+    extern __shared__ __align__(16) uint8_t smem[];
+    Shared& sh = *reinterpret_cast<Shared*>(smem);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int row = blockIdx.y, share = blockIdx.x * kWarps + warp, shares = gridDim.x * kWarps;
+    if (gridDim.x > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;");  // (the first CTA is there)
+    const int g0 = static_cast<int>(static_cast<long long>(groups) * share / shares);
+    const int g1 = static_cast<int>(static_cast<long long>(groups) * (share + 1) / shares);
+    const int q1 = min(g1 * group_pieces, (a.vocab + kPiece<T> - 1) / kPiece<T>), qw = VEC ? min(q1, a.vocab / kPiece<T>) : 0;
+    int q = g0 * group_pieces, asked = q, stage = 0, to = 0;
+    pdl_wait();
+    pdl_launch_dependents();
+    const T* src = static_cast<const T*>(a.logits) + row * a.ld;
+    uint4* const mine = sh.ring[warp][0] + lane;
+    const T* ps = src + static_cast<size_t>(q) * kPiece<T> + lane * kPer;
+    auto ask = [&] {  // for the next whole step (a group of copies in any case, to count)
+        if (asked < qw) {
+#pragma unroll
+            for (int u = 0; u < kSpans; ++u) cp_async16(mine + to * (kSpans * 32) + u * 32, ps + u * kSpan<T>);
+        }
+        cp_async_commit();
+        ++asked;
+        ps += kPiece<T>;
+        to = to + 1 == kStages ? 0 : to + 1;
+    };
+#pragma unroll
+    for (int i = 0; i < kStages; ++i) ask();
+    const float z_token = blockIdx.x == 0 && static_cast<int>(threadIdx.x) < a.n_tokens ? logit_of<T>(a, row, src, threadIdx.x) : 0.0f;
+    Shared* first = &sh;  // the first CTA's
+    if (gridDim.x > 1) {
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+        uint64_t at;
+        asm("mapa.u64 %0, %1, 0;" : "=l"(at) : "l"(&sh));
+        first = reinterpret_cast<Shared*>(at);
+    }
+    float m = -INFINITY, best = -INFINITY;  // the warp's; the group's
+    Sums2 sums;                             // while -10^37 < m < 10^37
+    Sums wide;                              // else
+    const int mask_piece = a.mask_id >= 0 ? a.mask_id / kPiece<T> : -1;
+    int left = group_pieces;  // steps of the group
+    for (int g = g0; q < q1; ++q) {
+        uint4* at = mine + stage * (kSpans * 32);
+        cp_async_wait<kStages - 1>();
+        if (q >= qw) {  // one by one
+#pragma unroll 1
+            for (int u = 0; u < kSpans; ++u) {
+                const int v = q * kPiece<T> + u * kSpan<T> + kPer * lane;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    reinterpret_cast<T*>(at + u * 32)[i] = v + i < a.vocab ? src[v + i] : static_cast<T>(-INFINITY);
+            }
+        }
+        if (q == mask_piece) {
+            const int in = a.mask_id % kPiece<T>, span = in / kSpan<T>, of = in % kSpan<T>;
+            if (of / kPer == lane) reinterpret_cast<T*>(at + span * 32)[of % kPer] = static_cast<T>(-INFINITY);
+        }
+        asm volatile("" ::: "memory");  // (stored as values, loaded as 16 bytes)
+        float z[kValues];
+#pragma unroll
+        for (int u = 0; u < kSpans; ++u) Raw<T>::floats(at[u * 32], z + u * kPer);
+        float mx = z[0];
+#pragma unroll
+        for (int i = 1; i + 1 < kValues; i += 2) mx = max3(mx, z[i], z[i + 1]);
+        mx = fmaxf(mx, z[kValues - 1]);
+        const float wm = warp_max(mx), old = m;
+        const bool more = wm > m;
+        if (more) {  // the new m stays out, the old one comes in its place
+            if (lane == __ffs(__ballot_sync(0xffffffffu, mx == wm)) - 1) {
+                float seek = wm;
+#pragma unroll
+                for (int i = 0; i < kValues; ++i) {
+                    const bool hit = z[i] == seek;
+                    z[i] = hit ? old : z[i];
+                    seek = hit ? __int_as_float(0x7fffffff) : seek;
+                }
+            }
+            __syncwarp();
+            m = wm;
+            if (fabsf(m) < kWide) {
+                if (!(fabsf(old) < kWide)) {  // (what there was is nothing beside it, unless it is NaN)
+                    sums.s = sums.t = wide.s * 0.0f + wide.t * 0.0f;
+                    sums.c = m * kLog2e;
+                } else if (fmaf(m, kLog2e, -sums.c) > 8.0f) {
+                    sums.move(m);
+                }
+            } else {
+                if (fabsf(old) < kWide) wide.s = wide.t = sums.s * 0.0f + sums.t * 0.0f;
+                wide.move(finite(m));
+            }
+        }
+        if (fabsf(m) < kWide) {
+            // (clamped, so that -inf gives 0 times a number)
+            const float2 nc = make_float2(-sums.c, -sums.c), l2 = make_float2(kLog2e, kLog2e);
+            float2 s2 = make_float2(0.0f, 0.0f), t2 = s2;
+#pragma unroll
+            for (int i = 0; i < kValues; i += 2) {
+                float2 y = fma2(make_float2(z[i], z[i + 1]), l2, nc), e;
+                y.x = max_nan(y.x, kFar2);
+                y.y = max_nan(y.y, kFar2);
+                e.x = ex2(y.x);
+                e.y = ex2(y.y);
+                s2 = add2(s2, e);
+                t2 = fma2(e, y, t2);
+            }
+            sums.s += s2.x + s2.y;
+            sums.t += t2.x + t2.y;
+        } else if (m == -INFINITY) {
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < kValues; ++i) odd |= z[i] != z[i];
+            if (odd) wide.s = wide.t = __int_as_float(0x7fffffff);
+        } else {
+            bool out = more && lane == __ffs(__ballot_sync(0xffffffffu, mx == wm)) - 1;  // (the step's one new m)
+            if (out) wide.add(old);
+#pragma unroll 1
+            for (int i = 0; i < kValues; ++i) {
+                const float x = static_cast<float>(reinterpret_cast<const T*>(at + i / kPer * 32)[i % kPer]);
+                if (out && x == wm) out = false;
+                else wide.add(x);
+            }
+        }
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+        ask();
+        best = fmaxf(best, wm);
+        if (--left == 0 || q + 1 == q1) {
+            if (lane == 0 && a.n_top) first->top[g] = best;
+            best = -INFINITY;
+            left = group_pieces;
+            ++g;
+        }
+    }
+    cp_async_wait<0>();
+    // the lanes' sums, against m
+    if (fabsf(m) < kWide) {
+        const float d = fmaf(-m, kLog2e, sums.c), e = ex2(d);
+        wide.s = sums.s * e;
+        wide.t = fmaf(sums.s, d, sums.t) * e * kLn2;
+    } else {
+        wide.move(finite(m));
+    }
+#pragma unroll
+    for (int d = 16; d; d /= 2) {
+        wide.s += __shfl_xor_sync(0xffffffffu, wide.s, d);
+        wide.t += __shfl_xor_sync(0xffffffffu, wide.t, d);
+    }
+    if (lane == 0) first->part[share] = Part{m, wide.s, wide.t, 0.0f};
+    if (gridDim.x > 1) {
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (blockIdx.x) return;
+    }
+    finish<T, VEC>(a, row, src, group_pieces, groups, shares, z_token, sh);
 }
-
-constexpr int kRows = 65535;  // of a launch
-size_t most_of(int rows, int vocab) {  // groups of a launch, at most
-    const size_t pieces = (static_cast<size_t>(vocab) + kPiece - 1) / kPiece;
-    return (rows < kRows ? rows : kRows) * (pieces < kGroups ? pieces : kGroups);
-}
-size_t part_bytes(int rows, int vocab) { return serve_round(sizeof(Part) * most_of(rows, vocab)); }
 
 template <typename T>
 cudaError_t go(const dllm_serve_logprobs_args& a, int sms, cudaStream_t st) {
-    // (a grid has 65535 rows of blocks at most)
-    const Cut c = logprobs_cut(a.rows < kRows ? a.rows : kRows, a.vocab, sms);
-    Part* part = static_cast<Part*>(a.ws);
-    float* top = reinterpret_cast<float*>(static_cast<char*>(a.ws) + part_bytes(a.rows, a.vocab));
-    const bool vec = reinterpret_cast<uintptr_t>(a.logits) % (4 * sizeof(T)) == 0 && a.ld % 4 == 0;
+    constexpr int kRows = 65535;  // of a launch: a grid has no more rows of blocks
+    const int pieces = (a.vocab + kPiece<T> - 1) / kPiece<T>, group_pieces = (pieces + kGroups - 1) / kGroups;
+    const int groups = (pieces + group_pieces - 1) / group_pieces;
+    const bool vec = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 && a.ld % Raw<T>::kPer == 0;
     const auto kernel = vec ? k_logprobs<T, true> : k_logprobs<T, false>;
+    cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         static_cast<int>(sizeof(Shared)));
+    if (e != cudaSuccess) return e;
     for (int r0 = 0; r0 < a.rows; r0 += kRows) {
         dllm_serve_logprobs_args b = a;
         b.rows = a.rows - r0 < kRows ? a.rows - r0 : kRows;
@@ -357,20 +610,29 @@ cudaError_t go(const dllm_serve_logprobs_args& a, int sms, cudaStream_t st) {
         if (a.lse) b.lse = a.lse + r0;
         if (a.top_ids) b.top_ids = a.top_ids + static_cast<long long>(r0) * a.n_top;
         if (a.top_lp) b.top_lp = a.top_lp + static_cast<long long>(r0) * a.n_top;
-        cudaError_t e = serve_launch(kernel, dim3((c.shares + kWarps - 1) / kWarps, b.rows), kThreads, 0, st, b, c.group_pieces,
-                                     c.groups, c.shares, part, top);
-        if (e == cudaSuccess)
-            e = serve_launch(k_logprobs_row<T>, dim3(b.rows), kThreads, 0, st, b, c.group_pieces, c.groups, c.shares, part, top);
+        // CTAs of a row: as many as make six an SM (of which four run at a time), none with less than a group a warp
+        int ctas = 1;
+        while (ctas < kCluster && static_cast<long long>(ctas) * b.rows < 6ll * sms && ctas * kWarps < groups) ctas *= 2;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3(ctas, b.rows);
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = sizeof(Shared);
+        cfg.stream = st;
+        cudaLaunchAttribute at[2];
+        at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[0].val.programmaticStreamSerializationAllowed = 1;
+        at[1].id = cudaLaunchAttributeClusterDimension;
+        at[1].val.clusterDim.x = ctas;
+        at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 2;
+        e = cudaLaunchKernelEx(&cfg, kernel, b, group_pieces, groups);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
 }
 
 }  // namespace
-
-size_t serve_logprobs_bytes(int rows, int vocab) {
-    return part_bytes(rows, vocab) + serve_round(sizeof(float) * most_of(rows, vocab));
-}
 
 cudaError_t launch_serve_logprobs(const dllm_serve_logprobs_args& a, int sms, cudaStream_t st) {
     return a.dtype == DLLM_F32    ? go<float>(a, sms, st)

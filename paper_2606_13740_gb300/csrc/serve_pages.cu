@@ -10,60 +10,71 @@ namespace {
 constexpr int kMoveThreads = 256;
 constexpr int kMoveWarps = kMoveThreads / 32;
 
-// A warp takes a request, a layer's K or V, and a head: places in ascending order, 32 at a time, all of them loaded
-// before the first is stored.  A place moves down or stays, so what is stored lies below all that is yet to be loaded.
-template <int HD>
-__global__ void __launch_bounds__(kMoveThreads) k_serve_compact(const __grid_constant__ ServeShape s,
-                                                                const __grid_constant__ dllm_serve_tables t,
-                                                                const __grid_constant__ ServeCaches c,
-                                                                const __grid_constant__ ServeCompactArgs a) {
+// A request's column is a layer's K or V and a head.  W warps take a column: its places in ascending order, ROWS of
+// each warp at a time, all of them loaded before the first is stored.  A place moves down or stays, so what is stored lies below
+// all that is yet to be loaded.  A list that ascends from 0 begins with the places that stay.
+template <int HD, int W, int ROWS>
+__global__ void __launch_bounds__(kMoveThreads, 3)
+    k_serve_compact(const __grid_constant__ ServeShape s, const __grid_constant__ dllm_serve_tables t,
+                    const __grid_constant__ ServeCaches c, const __grid_constant__ ServeCompactArgs a) {
     constexpr int kLanes = HD / 8, kAtOnce = 32 / kLanes;  // lanes of a row of 16-byte pieces, rows of a warp's load
+    constexpr int kLoads = ROWS / kAtOnce, kStep = W * ROWS;
+    __shared__ int s_stay[kMoveWarps];
     ServeArrays w;
     serve_arrays(s, t.work, &w);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int me = W == 1 ? lane : static_cast<int>(threadIdx.x);  // of the W warps' threads
     const int columns = 2 * c.n * s.Hkv;
     const long long units = static_cast<long long>(a.batch) * columns;
+    auto any = [&](bool v) { return W == 1 ? __any_sync(0xffffffffu, v) != 0 : __syncthreads_or(v) != 0; };
+    auto barrier = [&] {
+        if (W == 1) __syncwarp();
+        else __syncthreads();
+    };
+    static_assert(W == 1 || W == kMoveWarps, "a warp or a CTA");
     pdl_wait();
     pdl_launch_dependents();
-    for (long long unit = static_cast<long long>(blockIdx.x) * kMoveWarps + warp; unit < units;
-         unit += static_cast<long long>(gridDim.x) * kMoveWarps) {
+    for (long long unit = W == 1 ? static_cast<long long>(blockIdx.x) * kMoveWarps + warp : blockIdx.x; unit < units;
+         unit += static_cast<long long>(gridDim.x) * (kMoveWarps / W)) {
         const int b = static_cast<int>(unit / columns), col = static_cast<int>(unit % columns);
-        const int n = a.n[b], first = a.first[b], held = t.held[b];
+        const int n = a.n[b], first = a.first[b], held = t.held[b], shared = w.shared[b];
         if (n == 0) continue;
         const int* keep = a.keep + static_cast<long long>(b) * a.keep_ld;
         const int* table = t.table + static_cast<size_t>(b) * s.max_pages;
         const long long end = static_cast<long long>(min(max(held, 0), s.max_pages)) << s.page_log2;  // places there are
-        // the list ascends, its places are there and in the pool; the first that moves
+        // the list ascends, its places are there and in the pool; how many of them stay
         bool bad = n < 0 || n > a.keep_ld || first < 0;
-        int from = n, bits = 0;
+        int from = 0, bits = 0;
         if (!bad) {
-            int last = -1;
-            for (int i0 = 0; i0 < n; i0 += 32) {
-                const int i = i0 + lane, k = i < n ? keep[i] : 0x7fffffff;
-                int before = __shfl_up_sync(0xffffffffu, k, 1);
-                if (lane == 0) before = last;
-                last = __shfl_sync(0xffffffffu, k, 31);
-                if (i < n) {
-                    bad |= k <= before || k < 0 || first + static_cast<long long>(k) >= end;
-                    if (k != i) from = min(from, i);
-                }
+#pragma unroll 4
+            for (int i = me; i < n; i += 32 * W) {
+                const int k = keep[i], below = i ? keep[i - 1] : -1;
+                bad |= k <= below || first + static_cast<long long>(k) >= end;
+                from += k == i;
             }
-            from = __reduce_min_sync(0xffffffffu, from);
         }
-        if (__any_sync(0xffffffffu, bad)) {
+        from = __reduce_add_sync(0xffffffffu, from);
+        if (W > 1 && lane == 0) s_stay[warp] = from;
+        if (any(bad)) {
             bits = DLLM_SERVE_TREE;
-        } else if (from == n) {
-            continue;
-        } else if ((first + from) >> s.page_log2 < w.shared[b]) {
-            bits = DLLM_SERVE_SHARED;
         } else {
+            if (W > 1) {
+                from = 0;
+                for (int i = 0; i < W; ++i) from += s_stay[i];
+            }
+            if (from == n) {
+                barrier();
+                continue;
+            }
             bool out = false;  // a page that is not of the pool
             const int p1 = (first + keep[n - 1]) >> s.page_log2;
-            for (int p = ((first + from) >> s.page_log2) + lane; p <= p1; p += 32) out |= table[p] < 0 || table[p] >= s.n_pages;
-            if (__any_sync(0xffffffffu, out)) bits = DLLM_SERVE_STATE;
+            for (int p = ((first + from) >> s.page_log2) + me; p <= p1; p += 32 * W) out |= table[p] < 0 || table[p] >= s.n_pages;
+            if (any(out)) bits = DLLM_SERVE_STATE;
+            if ((first + from) >> s.page_log2 < shared) bits = DLLM_SERVE_SHARED;
         }
         if (bits) {
-            if (lane == 0 && col == 0) atomicOr(t.status, bits);
+            if (me == 0 && col == 0) atomicOr(t.status, bits);
+            barrier();
             continue;
         }
         uint4* cache = static_cast<uint4*>(col & 1 ? c.v[(col >> 1) / s.Hkv] : c.k[(col >> 1) / s.Hkv]) +
@@ -71,27 +82,35 @@ __global__ void __launch_bounds__(kMoveThreads) k_serve_compact(const __grid_con
         auto row = [&](int place) {  // of the cache, in 16-byte pieces
             return static_cast<long long>(table[place >> s.page_log2]) * (s.page_stride / 8) + (place & (s.page - 1)) * kLanes;
         };
-        for (int i0 = from; i0 < n; i0 += 32) {
-            const int i = i0 + lane;
-            long long src = 0, dst = 0;
-            if (i < n) {
+        // rows of this lane's place in a step (the warp's places side by side)
+        auto rows_of = [&](int i, long long& src, long long& dst) {
+            if (lane < ROWS && i < n) {
                 src = row(first + keep[i]);
                 dst = row(first + i);
             }
-            uint4 x[32 / kAtOnce];
+        };
+        const int mine = (W == 1 ? 0 : warp) * ROWS, nth = lane / kLanes;
+        long long src = 0, dst = 0, src2 = 0, dst2 = 0;
+        rows_of(from + mine + lane, src, dst);
+        for (int i0 = from; i0 < n; i0 += kStep) {
+            const int left = n - i0 - mine;  // of this warp
+            uint4 x[kLoads];
 #pragma unroll
-            for (int k = 0; k < 32 / kAtOnce; ++k) {
-                const long long at = __shfl_sync(0xffffffffu, src, k * kAtOnce + lane / kLanes);
-                if (i0 + k * kAtOnce + lane / kLanes < n) x[k] = cache[at];
+            for (int k = 0; k < kLoads; ++k) {
+                const long long at = __shfl_sync(0xffffffffu, src, k * kAtOnce + nth);
+                if (k * kAtOnce + nth < left) x[k] = cache[at];
             }
-            __syncwarp();
+            rows_of(i0 + kStep + mine + lane, src2, dst2);
+            barrier();
 #pragma unroll
-            for (int k = 0; k < 32 / kAtOnce; ++k) {
-                const long long at = __shfl_sync(0xffffffffu, dst, k * kAtOnce + lane / kLanes);
-                if (i0 + k * kAtOnce + lane / kLanes < n) cache[at] = x[k];
+            for (int k = 0; k < kLoads; ++k) {
+                const long long at = __shfl_sync(0xffffffffu, dst, k * kAtOnce + nth);
+                if (k * kAtOnce + nth < left) cache[at] = x[k];
             }
-            __syncwarp();
+            src = src2;
+            dst = dst2;
         }
+        barrier();
     }
 }
 
@@ -99,6 +118,13 @@ __global__ void __launch_bounds__(kMoveThreads) k_serve_compact(const __grid_con
 constexpr int kForkThreads = 1024;
 constexpr int kForkWarps = kForkThreads / 32;
 constexpr int kForkCtas = 8;  // a cluster
+// One CTA with all of it in shared memory, for so many requests, pages of the pool, and of the rows.
+constexpr int kSmallBatch = 1024, kSmallPages = 12288, kSmallStage = 16384;
+size_t fork_smem(const ServeShape& s, bool small) {
+    return sizeof(int) * (5 * static_cast<size_t>(s.max_batch) + (small ? 2 * static_cast<size_t>(s.n_pages) + kSmallStage : 0));
+}
+constexpr size_t kForkSmem[2] = {sizeof(int) * 5 * kServeMaxBatch,
+                                 sizeof(int) * (5 * kSmallBatch + 2 * kSmallPages + kSmallStage)};  // the most of any call
 
 // The bookkeeping's workspace.
 constexpr int kOld = 1 << 30, kKept = 1 << 29, kCount = kKept - 1;
@@ -164,54 +190,74 @@ __device__ __forceinline__ int block_before(int v, int* buf, int* sum) {
 }
 
 // The tables.  One cluster: every CTA looks at all requests, the rows and the pages are shared out, marks go through L2
-// between cluster barriers.  Nothing that others read is changed before it is known that the fork can be carried out.
+// between cluster barriers; or (SMALL) one CTA, marks in shared memory.  Nothing that others read is changed before it is
+// known that the fork can be carried out.
+template <bool SMALL>
 __global__ void __launch_bounds__(kForkThreads) k_serve_fork(const __grid_constant__ ServeShape s,
                                                              const __grid_constant__ dllm_serve_tables t, const int* src,
-                                                             const int* len, int batch) {
-    __shared__ int s_src[kServeMaxBatch], s_last[kServeMaxBatch];  // the request continued; the last page, if partly filled
+                                                             const int* len, int batch, int row_lanes) {
+    extern __shared__ int smem[];
     __shared__ int s_scan[kForkWarps];
-    const int rank = cluster_rank(), ctas = cluster_size(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int lg = s.page_log2, page = s.page, M = s.max_pages;
+    const int B = s.max_batch, M = s.max_pages, lg = s.page_log2, page = s.page, tid = threadIdx.x;
+    // of the requests: the one continued, its length, pages held before; the last page, if partly filled; pages shared
+    int *s_src = smem, *s_len = s_src + B, *s_held = s_len + B, *s_last = s_held + B, *s_shared = s_last + B;
+    const int rank = SMALL ? 0 : cluster_rank(), ctas = SMALL ? 1 : cluster_size();
     ServeArrays w;
     serve_arrays(s, t.work, &w);
     ForkArrays f;
     fork_arrays(s, t.partials, &f);
+    int* const mark = SMALL ? smem + 5 * B : f.mark;
+    int* const writer = SMALL ? smem + 5 * B + s.n_pages : f.writer;
+    int* const stage = SMALL ? smem + 5 * B + 2 * s.n_pages : f.stage;
+    auto barrier = [] {
+        if (SMALL) __syncthreads();
+        else cluster_barrier();
+    };
+    const int p0 = static_cast<int>(static_cast<long long>(s.n_pages) * rank / ctas);
+    const int p1 = static_cast<int>(static_cast<long long>(s.n_pages) * (rank + 1) / ctas);
+    if (SMALL) {
+        for (int p = tid; p < s.n_pages; p += kForkThreads) mark[p] = 0;
+    }
     pdl_wait();
     pdl_launch_dependents();
 
     // ------------------------------------------------ what is asked for
     const int head0 = t.ring_pos[0], free0 = t.ring_pos[1];
+    int bits = 0;
+    for (int b = tid; b < B; b += kForkThreads) {
+        const int held = t.held[b], from = b < batch ? src[b] : b, n = b < batch ? len[b] : 0;
+        const bool bad = from < 0 || from >= B || n < 0;
+        if (held < 0 || held > M) bits |= DLLM_SERVE_STATE;
+        if (bad) bits |= DLLM_SERVE_LENGTHS;
+        s_held[b] = min(max(held, 0), M);
+        s_src[b] = bad ? 0 : from;
+        s_len[b] = bad ? 0 : n;
+        s_shared[b] = 0;
+    }
     const int free_n = min(max(free0, 0), s.n_pages);
-    const int head = static_cast<int>(static_cast<unsigned>(max(head0, 0)) % static_cast<unsigned>(s.n_pages));
-    int bits = free0 != free_n || head0 != head ? DLLM_SERVE_STATE : 0;
-    auto held_of = [&](int b) { return min(max(t.held[b], 0), M); };
-    for (int b = tid; b < s.max_batch; b += kForkThreads)
-        if (t.held[b] < 0 || t.held[b] > M) bits |= DLLM_SERVE_STATE;
+    const unsigned head = static_cast<unsigned>(max(head0, 0)) % static_cast<unsigned>(s.n_pages);
+    if (free0 != free_n || head0 != static_cast<int>(head)) bits |= DLLM_SERVE_STATE;
+    auto free_page = [&](int k) { return t.ring[(head + k) % static_cast<unsigned>(s.n_pages)]; };
+    const int ring0 = tid < min(batch, free_n) ? free_page(tid) : 0;  // (asked for ahead of its use)
+    if (!SMALL) {
+        for (int p = p0 + tid; p < p1; p += kForkThreads) mark[p] = 0;
+    }
+    if (rank == 0 && tid < 2) f.head[tid] = 0;
+    __syncthreads();
     for (int b = tid; b < batch; b += kForkThreads) {
-        int from = src[b], last = -1;
-        const int n = len[b];
-        if (from < 0 || from >= s.max_batch || n < 0) {
+        const int n = s_len[b], from = s_src[b];
+        int last = -1;
+        if ((static_cast<long long>(n) + page - 1) >> lg > s_held[from]) {
             bits |= DLLM_SERVE_LENGTHS;
-            from = 0;
-        } else {
-            const int need = static_cast<int>((static_cast<long long>(n) + page - 1) >> lg);
-            if (need > held_of(from)) {
-                bits |= DLLM_SERVE_LENGTHS;
-            } else if (n & (page - 1)) {
-                last = t.table[static_cast<size_t>(from) * M + (n >> lg)];
-                if (last < 0 || last >= s.n_pages) bits |= DLLM_SERVE_STATE;
-                else if (rank == 0) f.writer[last] = 0;
-            }
+        } else if (n & (page - 1)) {
+            last = t.table[static_cast<size_t>(from) * M + (n >> lg)];
+            if (last < 0 || last >= s.n_pages) bits |= DLLM_SERVE_STATE;
+            else if (rank == 0) writer[last] = 0;
         }
-        s_src[b] = from;
         s_last[b] = last;
     }
-    const int p0 = static_cast<int>(static_cast<long long>(s.n_pages) * rank / ctas);
-    const int p1 = static_cast<int>(static_cast<long long>(s.n_pages) * (rank + 1) / ctas);
-    for (int p = p0 + tid; p < p1; p += kForkThreads) f.mark[p] = 0;
-    if (rank == 0 && tid < 2) f.head[tid] = 0;
-    const bool shape_bad = __syncthreads_or(bits) != 0;
-    cluster_barrier();
+    const bool wrong = __syncthreads_or(bits) != 0;
+    barrier();
     auto refuse = [&](int why) {
         if (rank == 0) {
             if (why) atomicOr(t.status, why);
@@ -221,114 +267,123 @@ __global__ void __launch_bounds__(kForkThreads) k_serve_fork(const __grid_consta
             }
         }
     };
-    if (shape_bad) return refuse(bits);
+    if (wrong) return refuse(bits);
 
-    // ------------------------------------------------ who holds what
+    // ------------------------------------------------ who holds what; row_lanes threads a row
+    const int sub = tid % row_lanes, row0 = rank * (kForkThreads / row_lanes) + tid / row_lanes;
+    const int rows = ctas * (kForkThreads / row_lanes);
     bool out = false;
-    for (int r = rank * kForkWarps + warp; r < s.max_batch; r += ctas * kForkWarps) {
-        const int held = held_of(r);
+    for (int r = row0; r < B; r += rows) {
+        const int held = s_held[r], full = s_len[r] >> lg;
         const int* row = t.table + static_cast<size_t>(r) * M;
-        for (int i = lane; i < held; i += 32) {
-            const int p = row[i];
-            if (p < 0 || p >= s.n_pages) out = true;
-            else if (r < batch) atomicOr(f.mark + p, kOld);
-            else atomicAdd(f.mark + p, 1);
-        }
-        if (r >= batch) continue;
-        const int full = len[r] >> lg;
         const int* from = t.table + static_cast<size_t>(s_src[r]) * M;
-        for (int i = lane; i < full; i += 32) {
-            const int p = from[i];
-            f.stage[static_cast<size_t>(r) * M + i] = p;
-            if (p < 0 || p >= s.n_pages) out = true;
-            else atomicAdd(f.mark + p, 1);
+        const bool more = r >= batch;  // a row that stays
+        for (int i = sub; i < max(held, full); i += row_lanes) {
+            const int p = i < held ? row[i] : 0, q = i < full ? from[i] : 0;
+            if (p < 0 || p >= s.n_pages || q < 0 || q >= s.n_pages) {
+                out = true;
+                continue;
+            }
+            if (i < held) {
+                if (more) atomicAdd(mark + p, 1);
+                else atomicOr(mark + p, kOld);
+            }
+            if (i < full) {
+                atomicAdd(mark + q, 1);
+                stage[static_cast<size_t>(r) * M + i] = q;
+            }
         }
     }
     if (rank == 0) {
         for (int b = tid; b < batch; b += kForkThreads)
-            if (s_last[b] >= 0) atomicMax(f.writer + s_last[b], s.max_batch - b);
+            if (s_last[b] >= 0) atomicMax(writer + s_last[b], B - b);
     }
-    if (out) f.head[1] = 1;
-    cluster_barrier();
-    if (f.head[1]) return refuse(tid == 0 ? DLLM_SERVE_STATE : 0);
+    if (tid < min(batch, free_n) && (ring0 < 0 || ring0 >= s.n_pages)) out = true;
+    for (int k = kForkThreads + tid; k < min(batch, free_n); k += kForkThreads) out |= free_page(k) < 0 || free_page(k) >= s.n_pages;
+    if (SMALL) {
+        out = __syncthreads_or(out);
+    } else {
+        if (out) f.head[1] = 1;
+        barrier();
+        out = f.head[1];
+    }
+    if (out) return refuse(tid == 0 ? DLLM_SERVE_STATE : 0);
 
     // ------------------------------------------------ the last pages: kept, or copied
     const int per = (batch + kForkThreads - 1) / kForkThreads;
     const int b0 = min(batch, tid * per), b1 = min(batch, b0 + per);
     auto copied = [&](int b) {
         const int p = s_last[b];
-        return p >= 0 && ((f.mark[p] & kCount) > 0 || f.writer[p] != s.max_batch - b);
+        return p >= 0 && ((mark[p] & kCount) > 0 || writer[p] != B - b);
     };
     int mine = 0, taken;
     for (int b = b0; b < b1; ++b) mine += copied(b);
     int nth = block_before(mine, s_scan, &taken);
     if (taken > free_n) return refuse(tid == 0 ? DLLM_SERVE_PAGES : 0);
-    auto free_page = [&](int k) { return t.ring[(static_cast<unsigned>(head) + k) % static_cast<unsigned>(s.n_pages)]; };
-    for (int k = tid; k < taken; k += kForkThreads) out |= free_page(k) < 0 || free_page(k) >= s.n_pages;
-    if (__syncthreads_or(out)) return refuse(tid == 0 ? DLLM_SERVE_STATE : 0);
     for (int b = b0; b < b1; ++b) {
         const int p = s_last[b];
         if (p < 0) continue;
         if (copied(b)) {
             const int to = free_page(nth);
-            if (rank == 0) f.job[nth] = make_int4(p, to, len[b] & (page - 1), 0);
+            if (rank == 0) f.job[nth] = make_int4(p, to, s_len[b] & (page - 1), 0);
             s_last[b] = to;
             ++nth;
         } else if (rank == 0) {
-            atomicOr(f.mark + p, kKept);
+            atomicOr(mark + p, kKept);
         }
     }
-    cluster_barrier();  // (and the state is read)
+    barrier();  // (and the state is read)
 
     // ------------------------------------------------ the rows
-    for (int r = rank * kForkWarps + warp; r < s.max_batch; r += ctas * kForkWarps) {
+    for (int r = row0; r < B; r += rows) {
         int* row = t.table + static_cast<size_t>(r) * M;
-        const int held = held_of(r), n = r < batch ? len[r] : 0, full = r < batch ? n >> lg : held;
-        const int need = r < batch ? static_cast<int>((static_cast<long long>(n) + page - 1) >> lg) : held;
+        const bool more = r >= batch;
+        const int held = s_held[r], n = s_len[r], full = more ? held : n >> lg, need = more ? held : (n >> lg) + ((n & (page - 1)) != 0);
         int shared = 0;
-        for (int i = lane; i < max(need, r < batch ? held : 0); i += 32) {
+        for (int i = sub; i < max(need, held); i += row_lanes) {
             if (i < full) {
-                const int p = r < batch ? f.stage[static_cast<size_t>(r) * M + i] : row[i];
-                if ((f.mark[p] & kCount) > 1) shared = i + 1;
-                if (r < batch) row[i] = p;
+                const int p = more ? row[i] : stage[static_cast<size_t>(r) * M + i];
+                if ((mark[p] & kCount) > 1) shared = i + 1;
+                if (!more) row[i] = p;
             } else {
                 row[i] = i < need ? s_last[r] : -1;
             }
         }
-        shared = __reduce_max_sync(0xffffffffu, shared);
-        __syncwarp();
-        if (lane == 0) {
-            w.shared[r] = shared;
-            if (r < batch) {
-                t.held[r] = need;
-                t.n_keys[r] = n;
-            }
+        if (shared) atomicMax(s_shared + r, shared);
+        if (sub == 0 && !more) {
+            t.held[r] = need;
+            t.n_keys[r] = n;
         }
     }
 
     // ------------------------------------------------ the ring
     int n_back = 0;
-    for (int p = p0 + tid; p < p1; p += kForkThreads) n_back += (f.mark[p] & (kCount | kKept | kOld)) == kOld;
-    int given;
+    for (int p = p0 + tid; p < p1; p += kForkThreads) n_back += (mark[p] & (kCount | kKept | kOld)) == kOld;
+    int given, all = 0, at = free_n;
     block_before(n_back, s_scan, &given);
-    if (tid == 0) f.head[2 + rank] = given;
-    cluster_barrier();
-    int at = free_n, all = 0;
-    for (int c = 0; c < ctas; ++c) {
-        if (c < rank) at += f.head[2 + c];
-        all += f.head[2 + c];
+    for (int r = row0; r < B; r += rows)
+        if (sub == 0) w.shared[r] = s_shared[r];
+    if (SMALL) {
+        all = given;
+    } else {
+        if (tid == 0) f.head[2 + rank] = given;
+        barrier();
+        for (int c = 0; c < ctas; ++c) {
+            if (c < rank) at += f.head[2 + c];
+            all += f.head[2 + c];
+        }
     }
-    for (int q = p0; q < p1; q += kForkThreads) {
+    for (int q = p0; q < p1 && given; q += kForkThreads) {
         const int p = q + tid;
-        const bool back = p < p1 && (f.mark[p] & (kCount | kKept | kOld)) == kOld;
+        const bool back = p < p1 && (mark[p] & (kCount | kKept | kOld)) == kOld;
         int here;
         const int before = block_before(back, s_scan, &here);
-        if (back) t.ring[(static_cast<unsigned>(head) + at + before) % static_cast<unsigned>(s.n_pages)] = p;
+        if (back) t.ring[(head + at + before) % static_cast<unsigned>(s.n_pages)] = p;
         at += here;
     }
     if (rank == 0 && tid == 0) {
         f.head[0] = taken;
-        t.ring_pos[0] = static_cast<int>((static_cast<unsigned>(head) + taken) % static_cast<unsigned>(s.n_pages));
+        t.ring_pos[0] = static_cast<int>((head + taken) % static_cast<unsigned>(s.n_pages));
         t.ring_pos[1] = min(free_n - taken + all, s.n_pages);
         t.status[1] = 0;
         t.status[2] = taken;
@@ -372,20 +427,33 @@ __global__ void __launch_bounds__(kMoveThreads) k_serve_copy(const __grid_consta
 
 cudaError_t launch_serve_compact(const ServeShape& s, const dllm_serve_tables& t, const ServeCaches& c,
                                  const ServeCompactArgs& a, int sms, cudaStream_t st) {
-    const long long units = 2ll * c.n * s.Hkv * a.batch, ctas = (units + kMoveWarps - 1) / kMoveWarps;
-    const dim3 grid(static_cast<unsigned>(ctas < 8ll * sms ? ctas : 8ll * sms));
-    return s.hd == 128 ? serve_launch(k_serve_compact<128>, grid, kMoveThreads, 0, st, s, t, c, a)
-                       : serve_launch(k_serve_compact<64>, grid, kMoveThreads, 0, st, s, t, c, a);
+    // short lists (an accepted path) a warp a column, others a CTA
+    const bool small = a.keep_ld <= 64;
+    const long long units = 2ll * c.n * s.Hkv * a.batch, ctas = small ? (units + kMoveWarps - 1) / kMoveWarps : units;
+    const dim3 grid(static_cast<unsigned>(ctas < 64ll * sms ? ctas : 64ll * sms));
+    if (small)
+        return s.hd == 128 ? serve_launch(k_serve_compact<128, 1, 16>, grid, kMoveThreads, 0, st, s, t, c, a)
+                           : serve_launch(k_serve_compact<64, 1, 32>, grid, kMoveThreads, 0, st, s, t, c, a);
+    return s.hd == 128 ? serve_launch(k_serve_compact<128, kMoveWarps, 16>, grid, kMoveThreads, 0, st, s, t, c, a)
+                       : serve_launch(k_serve_compact<64, kMoveWarps, 32>, grid, kMoveThreads, 0, st, s, t, c, a);
 }
 
 size_t serve_fork_bytes(const ServeShape& s) { return fork_arrays(s, nullptr, nullptr); }
 
 cudaError_t launch_serve_fork(const ServeShape& s, const dllm_serve_tables& t, const ServeCaches& c, const int* src,
                               const int* len, int batch, int sms, cudaStream_t st) {
+    const bool small = s.max_batch <= kSmallBatch && s.n_pages <= kSmallPages && static_cast<long long>(batch) * s.max_pages <= kSmallStage;
+    const auto kernel = small ? k_serve_fork<true> : k_serve_fork<false>;
+    // (always the most of any call, so that host threads do not lower it between another's asking and launch)
+    cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         static_cast<int>(kForkSmem[small]));
+    if (e != cudaSuccess) return e;
+    int row_lanes = 1;  // threads a row: as many as it may hold pages, up to a warp
+    while (row_lanes < 32 && row_lanes < s.max_pages) row_lanes *= 2;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = cfg.blockDim = dim3(1);
-    cfg.gridDim.x = kForkCtas;
-    cfg.blockDim.x = kForkThreads;
+    cfg.gridDim = dim3(small ? 1 : kForkCtas);
+    cfg.blockDim = dim3(kForkThreads);
+    cfg.dynamicSmemBytes = fork_smem(s, small);
     cfg.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -394,8 +462,8 @@ cudaError_t launch_serve_fork(const ServeShape& s, const dllm_serve_tables& t, c
     at[1].val.clusterDim.x = cfg.gridDim.x;
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 2;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, k_serve_fork, s, t, src, len, batch);
+    cfg.numAttrs = small ? 1 : 2;
+    e = cudaLaunchKernelEx(&cfg, kernel, s, t, src, len, batch, row_lanes);
     if (e != cudaSuccess) return e;
     const long long units = 2ll * c.n * s.Hkv * batch, ctas = (units + kMoveWarps - 1) / kMoveWarps;
     return serve_launch(k_serve_copy, dim3(static_cast<unsigned>(ctas < 8ll * sms ? ctas : 8ll * sms)), kMoveThreads, 0, st, s, t, c);

@@ -41,8 +41,7 @@ class dllm_serve_logits_args(C.Structure):
 
 class dllm_serve_logprobs_args(C.Structure):
     _fields_ = [("logits", _P), ("ld", _I64), ("dtype", _I), ("rows", _I), ("vocab", _I), ("mask_id", _I), ("tokens", _P),
-                ("n_tokens", _I), ("n_top", _I), ("lp", _P), ("entropy", _P), ("lse", _P), ("top_ids", _P), ("top_lp", _P),
-                ("ws", _P), ("ws_bytes", _SZ)]
+                ("n_tokens", _I), ("n_top", _I), ("lp", _P), ("entropy", _P), ("lse", _P), ("top_ids", _P), ("top_lp", _P)]
 
 
 # name -> (restype, argtypes); every entry point of include/dllm_serve.h
@@ -63,7 +62,6 @@ DRAFT_SIGNATURES = {
     "dllm_serve_accept": (_I, [_P, _P, _P, _P, _P, _I, _I, _I, _P, _P, _P, _P]),
     "dllm_serve_compact": (_I, [_P, _P, _P, _P, _I, _P, _P, _I, _P, _I, _P]),
     "dllm_serve_fork": (_I, [_P, _P, _P, _P, _I, _P, _P, _I, _P]),
-    "dllm_serve_logprobs_bytes": (_I, [_I, _I, _P]),
     "dllm_serve_logprobs": (_I, [_P, _P]),
 }
 
@@ -139,13 +137,6 @@ def _stream_on(index):
 def _logits_bytes(rows, vocab):
     n = _SZ()
     _check(serve_lib().dllm_serve_logits_bytes(rows, vocab, C.byref(n)))
-    return n.value
-
-
-@functools.cache
-def _logprobs_bytes(rows, vocab):
-    n = _SZ()
-    _check(serve_lib().dllm_serve_logprobs_bytes(rows, vocab, C.byref(n)))
     return n.value
 
 
@@ -445,7 +436,7 @@ def dllm_serve_logits(logits, mask_id=-1, req=None, hist=None, hist_len=None, re
     return x0, conf, None if cur is None else tokconf
 
 
-def dllm_serve_logprobs(logits, tokens=None, mask_id=-1, top=0, ws=None):
+def dllm_serve_logprobs(logits, tokens=None, mask_id=-1, top=0):
     """Under softmax(logits) over all ids but mask_id, logits [rows][vocab] (fp32, bf16 or f16): (lp, entropy, top_ids,
     top_lp, lse), the log probabilities of tokens (int32 [rows][any]), the entropy, the `top` likeliest ids (ties: lowest
     id) with theirs, and the logarithm of the softmax sum.  lp is None without tokens, top_ids and top_lp without top."""
@@ -466,19 +457,14 @@ def dllm_serve_logprobs(logits, tokens=None, mask_id=-1, top=0, ws=None):
         n_tokens = tokens.shape[1]
     if not 0 <= top <= 32:
         raise ValueError(f"top must be 0 to 32, not {top}")
-    if ws is None:
-        ws = torch.empty(_logprobs_bytes(rows, vocab), dtype=torch.uint8, device=dev)
-    elif ws.get_device() != index or not ws.is_contiguous():
-        raise ValueError(f"ws must be contiguous on {dev}")
     lp = torch.empty((rows, n_tokens), dtype=f32, device=dev) if tokens is not None else None
-    entropy, lse = torch.empty((2, rows), dtype=f32, device=dev).unbind(0)
+    entropy, lse = torch.empty(rows, dtype=f32, device=dev), torch.empty(rows, dtype=f32, device=dev)
     top_ids = torch.empty((rows, top), dtype=i32, device=dev) if top else None
     top_lp = torch.empty((rows, top), dtype=f32, device=dev) if top else None
     a = dllm_serve_logprobs_args(
         logits.data_ptr(), st[0] if rows > 1 else max(st[0], vocab), _names().get(logits.dtype, -1), rows, vocab, mask_id,
         tokens.data_ptr() if n_tokens else None, n_tokens, top, lp.data_ptr() if n_tokens else None, entropy.data_ptr(),
-        lse.data_ptr(), top_ids.data_ptr() if top else None, top_lp.data_ptr() if top else None, ws.data_ptr(),
-        ws.numel() * ws.element_size())
+        lse.data_ptr(), top_ids.data_ptr() if top else None, top_lp.data_ptr() if top else None)
     rc = serve_lib().dllm_serve_logprobs(C.byref(a), stream)
     if rc:
         _check(rc)

@@ -641,7 +641,6 @@ def test_a_step_in_a_graph_on_another_stream(dev):
     a, b = setup(), setup()
     want = [x.clone() for x in step(a)]
     a["s"].dllm_serve_check()
-    serve._logprobs_bytes(sum(Q), 900)
     side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):

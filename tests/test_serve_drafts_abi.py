@@ -113,15 +113,10 @@ def test_calls_refuse_bad_arguments(L):
 
 def test_logprobs_refuse_bad_arguments(L):
     from paper_2606_13740_gb300 import serve
-    n = C.c_size_t()
-    assert L.dllm_serve_logprobs_bytes(4, 1000, C.byref(n)) == 0 and n.value > 0
-    assert L.dllm_serve_logprobs_bytes(-1, 1000, C.byref(n)) == -1 and L.dllm_serve_logprobs_bytes(1, 0, C.byref(n)) == -1
-    assert L.dllm_serve_logprobs_bytes(1, (1 << 28) + 1, C.byref(n)) == -1 and L.dllm_serve_logprobs_bytes(1, 1000, None) == -1
-
     def call(**over):
         a = serve.dllm_serve_logprobs_args()
         good = dict(logits=P, ld=1000, dtype=2, rows=4, vocab=1000, mask_id=999, tokens=P, n_tokens=1, n_top=3, lp=P, entropy=P, lse=P,
-                    top_ids=P, top_lp=P, ws=P, ws_bytes=n.value)
+                    top_ids=P, top_lp=P)
         for k, v in {**good, **over}.items():
             setattr(a, k, v)
         return L.dllm_serve_logprobs(C.byref(a), None)
@@ -129,10 +124,10 @@ def test_logprobs_refuse_bad_arguments(L):
     for bad in (dict(logits=None), dict(rows=-1), dict(vocab=0), dict(ld=999), dict(dtype=3), dict(mask_id=1000), dict(mask_id=-2),
                 dict(logits=P + 2), dict(logits=P + 1, dtype=0), dict(tokens=None), dict(lp=None), dict(top_ids=None),
                 dict(top_lp=None), dict(n_tokens=-1), dict(n_tokens=(1 << 20) + 1), dict(n_top=-1), dict(n_top=33),
-                dict(n_top=0, n_tokens=0, lse=None, entropy=None), dict(ws=None), dict(ws=P + 8), dict(ws_bytes=n.value - 1),
+                dict(n_top=0, n_tokens=0, lse=None, entropy=None),
                 *(dict([(k, P + 2)]) for k in ("tokens", "lp", "entropy", "lse", "top_ids", "top_lp"))):
         assert call(**bad) == -1, bad
-    assert L.dllm_serve_logprobs(None, None) == -1 and call(rows=0, logits=None, ws=None) == 0
+    assert L.dllm_serve_logprobs(None, None) == -1 and call(rows=0, logits=None) == 0
 
 
 @pytest.fixture
@@ -147,7 +142,6 @@ def serve(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     monkeypatch.setattr(serve, "_stream_of", lambda: lambda index: 0)
     monkeypatch.setattr(serve, "_lib", SimpleNamespace(**{n: launch for n in serve.DRAFT_SIGNATURES}))
-    monkeypatch.setattr(serve, "_logprobs_bytes", lambda rows, vocab: 16)
     return serve
 
 
@@ -199,12 +193,12 @@ def test_tensors_lie_on_the_current_device(serve, monkeypatch):
     monkeypatch.setattr(torch, "empty", lambda shape, dtype, device: SimpleNamespace(
         data_ptr=lambda: P, numel=lambda: P, element_size=lambda: 1, unbind=lambda d: (_f32(0, 4), _f32(0, 4))))
 
-    def logprobs(z=0, tokens=0, ws=0, top=2, shape=(4, 2)):
-        serve.dllm_serve_logprobs(_f32(z, 4, 100), _i32(tokens, *shape), 99, top, ws=_on(ws, torch.zeros(64, dtype=torch.uint8)))
+    def logprobs(z=0, tokens=0, top=2, shape=(4, 2)):
+        serve.dllm_serve_logprobs(_f32(z, 4, 100), _i32(tokens, *shape), 99, top)
 
     with pytest.raises(AssertionError, match="launched"):
         logprobs()
-    for bad in (dict(z=1), dict(z=-1), dict(tokens=1), dict(tokens=-1), dict(ws=1), dict(top=33), dict(top=-1), dict(shape=(3, 2)),
+    for bad in (dict(z=1), dict(z=-1), dict(tokens=1), dict(tokens=-1), dict(top=33), dict(top=-1), dict(shape=(3, 2)),
                 dict(shape=(4,))):
         with pytest.raises(ValueError):
             logprobs(**bad)
