@@ -10,107 +10,175 @@ namespace {
 constexpr int kMoveThreads = 256;
 constexpr int kMoveWarps = kMoveThreads / 32;
 
-// A request's column is a layer's K or V and a head.  W warps take a column: its places in ascending order, ROWS of
-// each warp at a time, all of them loaded before the first is stored.  A place moves down or stays, so what is stored lies below
-// all that is yet to be loaded.  A list that ascends from 0 begins with the places that stay.
-template <int HD, int W, int ROWS>
+// A request's column is a layer's K or V and a head.  Its places are moved in ascending order, a step of them at a
+// time, all of a step loaded before the first is stored.  A place moves down or stays, so what is stored lies below all that
+// is yet to be loaded, and loads may run ahead.  A list that ascends from 0 begins with the places that stay.
+struct Column {
+    const int* keep;
+    const int* table;
+    uint4* cache;  // of the lane's 16 bytes
+    int n, first, from;
+};
+
+// What request b asks for.  Threads: a warp's or a CTA's (THREADS of them, me one of them).  False: nothing to move.
+template <int HD, int THREADS>
+__device__ __forceinline__ bool column_of(const ServeShape& s, const dllm_serve_tables& t, const ServeCaches& c,
+                                          const ServeCompactArgs& a, const int* shared_pages, int b, int col, int me, int* s_stay,
+                                          Column* out) {
+    constexpr int kLanes = HD / 8;
+    constexpr bool kWarp = THREADS == 32;
+    auto any = [&](bool v) { return kWarp ? __any_sync(0xffffffffu, v) != 0 : __syncthreads_or(v) != 0; };
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int n = a.n[b], first = a.first[b], held = t.held[b], shared = shared_pages[b];
+    if (n == 0) return false;
+    const int* keep = a.keep + static_cast<long long>(b) * a.keep_ld;
+    const int* table = t.table + static_cast<size_t>(b) * s.max_pages;
+    const long long end = static_cast<long long>(min(max(held, 0), s.max_pages)) << s.page_log2;  // places there are
+    // the list ascends, its places are there and in the pool; how many of them stay
+    bool bad = n < 0 || n > a.keep_ld || first < 0;
+    int from = 0, bits = 0;
+    if (!bad) {
+#pragma unroll 4
+        for (int i = me; i < n; i += THREADS) {
+            const int k = keep[i], below = i ? keep[i - 1] : -1;
+            bad |= k <= below || first + static_cast<long long>(k) >= end;
+            from += k == i;
+        }
+    }
+    from = __reduce_add_sync(0xffffffffu, from);
+    if (!kWarp && lane == 0) s_stay[warp] = from;
+    if (any(bad)) {
+        bits = DLLM_SERVE_TREE;
+    } else {
+        if (!kWarp) {
+            from = 0;
+            for (int i = 0; i < THREADS / 32; ++i) from += s_stay[i];
+        }
+        if (from == n) return false;
+        bool out_of = false;  // a page that is not of the pool
+        const int p1 = (first + keep[n - 1]) >> s.page_log2;
+        for (int p = ((first + from) >> s.page_log2) + me; p <= p1; p += THREADS) out_of |= table[p] < 0 || table[p] >= s.n_pages;
+        if (any(out_of)) bits = DLLM_SERVE_STATE;
+        if ((first + from) >> s.page_log2 < shared) bits = DLLM_SERVE_SHARED;
+    }
+    if (bits) {
+        if (me == 0 && col == 0) atomicOr(t.status, bits);
+        return false;
+    }
+    out->keep = keep;
+    out->table = table;
+    out->n = n;
+    out->first = first;
+    out->from = from;
+    out->cache = static_cast<uint4*>(col & 1 ? c.v[(col >> 1) / s.Hkv] : c.k[(col >> 1) / s.Hkv]) +
+                 static_cast<long long>((col >> 1) % s.Hkv) * s.page * kLanes + lane % kLanes;
+    return true;
+}
+// A place's row of the cache, in 16-byte pieces.
+template <int HD>
+__device__ __forceinline__ long long row_of(const ServeShape& s, const Column& u, int place) {
+    return static_cast<long long>(u.table[place >> s.page_log2]) * (s.page_stride / 8) + (place & (s.page - 1)) * (HD / 8);
+}
+
+// Short lists (an accepted path): a warp a column.
+template <int HD>
 __global__ void __launch_bounds__(kMoveThreads, 3)
     k_serve_compact(const __grid_constant__ ServeShape s, const __grid_constant__ dllm_serve_tables t,
                     const __grid_constant__ ServeCaches c, const __grid_constant__ ServeCompactArgs a) {
     constexpr int kLanes = HD / 8, kAtOnce = 32 / kLanes;  // lanes of a row of 16-byte pieces, rows of a warp's load
-    constexpr int kLoads = ROWS / kAtOnce, kStep = W * ROWS;
-    __shared__ int s_stay[kMoveWarps];
+    constexpr int kLoads = 8, kStep = kLoads * kAtOnce;
     ServeArrays w;
     serve_arrays(s, t.work, &w);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int me = W == 1 ? lane : static_cast<int>(threadIdx.x);  // of the W warps' threads
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nth = lane / kLanes;
     const int columns = 2 * c.n * s.Hkv;
     const long long units = static_cast<long long>(a.batch) * columns;
-    auto any = [&](bool v) { return W == 1 ? __any_sync(0xffffffffu, v) != 0 : __syncthreads_or(v) != 0; };
-    auto barrier = [&] {
-        if (W == 1) __syncwarp();
-        else __syncthreads();
-    };
-    static_assert(W == 1 || W == kMoveWarps, "a warp or a CTA");
     pdl_wait();
     pdl_launch_dependents();
-    for (long long unit = W == 1 ? static_cast<long long>(blockIdx.x) * kMoveWarps + warp : blockIdx.x; unit < units;
-         unit += static_cast<long long>(gridDim.x) * (kMoveWarps / W)) {
-        const int b = static_cast<int>(unit / columns), col = static_cast<int>(unit % columns);
-        const int n = a.n[b], first = a.first[b], held = t.held[b], shared = w.shared[b];
-        if (n == 0) continue;
-        const int* keep = a.keep + static_cast<long long>(b) * a.keep_ld;
-        const int* table = t.table + static_cast<size_t>(b) * s.max_pages;
-        const long long end = static_cast<long long>(min(max(held, 0), s.max_pages)) << s.page_log2;  // places there are
-        // the list ascends, its places are there and in the pool; how many of them stay
-        bool bad = n < 0 || n > a.keep_ld || first < 0;
-        int from = 0, bits = 0;
-        if (!bad) {
-#pragma unroll 4
-            for (int i = me; i < n; i += 32 * W) {
-                const int k = keep[i], below = i ? keep[i - 1] : -1;
-                bad |= k <= below || first + static_cast<long long>(k) >= end;
-                from += k == i;
-            }
-        }
-        from = __reduce_add_sync(0xffffffffu, from);
-        if (W > 1 && lane == 0) s_stay[warp] = from;
-        if (any(bad)) {
-            bits = DLLM_SERVE_TREE;
-        } else {
-            if (W > 1) {
-                from = 0;
-                for (int i = 0; i < W; ++i) from += s_stay[i];
-            }
-            if (from == n) {
-                barrier();
-                continue;
-            }
-            bool out = false;  // a page that is not of the pool
-            const int p1 = (first + keep[n - 1]) >> s.page_log2;
-            for (int p = ((first + from) >> s.page_log2) + me; p <= p1; p += 32 * W) out |= table[p] < 0 || table[p] >= s.n_pages;
-            if (any(out)) bits = DLLM_SERVE_STATE;
-            if ((first + from) >> s.page_log2 < shared) bits = DLLM_SERVE_SHARED;
-        }
-        if (bits) {
-            if (me == 0 && col == 0) atomicOr(t.status, bits);
-            barrier();
+    for (long long unit = static_cast<long long>(blockIdx.x) * kMoveWarps + warp; unit < units;
+         unit += static_cast<long long>(gridDim.x) * kMoveWarps) {
+        Column u;
+        if (!column_of<HD, 32>(s, t, c, a, w.shared, static_cast<int>(unit / columns), static_cast<int>(unit % columns), lane, nullptr, &u))
             continue;
-        }
-        uint4* cache = static_cast<uint4*>(col & 1 ? c.v[(col >> 1) / s.Hkv] : c.k[(col >> 1) / s.Hkv]) +
-                       static_cast<long long>((col >> 1) % s.Hkv) * s.page * kLanes + lane % kLanes;
-        auto row = [&](int place) {  // of the cache, in 16-byte pieces
-            return static_cast<long long>(table[place >> s.page_log2]) * (s.page_stride / 8) + (place & (s.page - 1)) * kLanes;
-        };
-        // rows of this lane's place in a step (the warp's places side by side)
-        auto rows_of = [&](int i, long long& src, long long& dst) {
-            if (lane < ROWS && i < n) {
-                src = row(first + keep[i]);
-                dst = row(first + i);
+        for (int i0 = u.from; i0 < u.n; i0 += kStep) {
+            long long src = 0, dst = 0;
+            if (lane < kStep && i0 + lane < u.n) {
+                src = row_of<HD>(s, u, u.first + u.keep[i0 + lane]);
+                dst = row_of<HD>(s, u, u.first + i0 + lane);
             }
-        };
-        const int mine = (W == 1 ? 0 : warp) * ROWS, nth = lane / kLanes;
-        long long src = 0, dst = 0, src2 = 0, dst2 = 0;
-        rows_of(from + mine + lane, src, dst);
-        for (int i0 = from; i0 < n; i0 += kStep) {
-            const int left = n - i0 - mine;  // of this warp
             uint4 x[kLoads];
 #pragma unroll
             for (int k = 0; k < kLoads; ++k) {
                 const long long at = __shfl_sync(0xffffffffu, src, k * kAtOnce + nth);
-                if (k * kAtOnce + nth < left) x[k] = cache[at];
+                if (i0 + k * kAtOnce + nth < u.n) x[k] = u.cache[at];
             }
-            rows_of(i0 + kStep + mine + lane, src2, dst2);
-            barrier();
+            __syncwarp();
 #pragma unroll
             for (int k = 0; k < kLoads; ++k) {
                 const long long at = __shfl_sync(0xffffffffu, dst, k * kAtOnce + nth);
-                if (k * kAtOnce + nth < left) cache[at] = x[k];
+                if (i0 + k * kAtOnce + nth < u.n) u.cache[at] = x[k];
             }
-            src = src2;
-            dst = dst2;
+            __syncwarp();
         }
-        barrier();
+    }
+}
+
+// Long lists: a CTA a column, steps copied ahead into shared memory, each lane what it stores itself.
+constexpr int kMoveStages = 3, kMoveLoads = 8;
+constexpr int kMoveSmem = kMoveStages * kMoveWarps * kMoveLoads * 32 * 16;
+template <int HD>
+__global__ void __launch_bounds__(kMoveThreads, 2)
+    k_serve_compact_long(const __grid_constant__ ServeShape s, const __grid_constant__ dllm_serve_tables t,
+                         const __grid_constant__ ServeCaches c, const __grid_constant__ ServeCompactArgs a) {
+    constexpr int kLanes = HD / 8, kAtOnce = 32 / kLanes;
+    constexpr int kRows = kMoveLoads * kAtOnce, kStep = kRows * kMoveWarps;  // of a warp, of a CTA
+    extern __shared__ __align__(16) uint4 ring[];
+    __shared__ int s_stay[kMoveWarps];
+    ServeArrays w;
+    serve_arrays(s, t.work, &w);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nth = lane / kLanes;
+    const int columns = 2 * c.n * s.Hkv;
+    const long long units = static_cast<long long>(a.batch) * columns;
+    uint4* const mine = ring + warp * (kMoveLoads * 32) + lane;
+    pdl_wait();
+    pdl_launch_dependents();
+    for (long long unit = blockIdx.x; unit < units; unit += gridDim.x) {
+        Column u;
+        if (column_of<HD, kMoveThreads>(s, t, c, a, w.shared, static_cast<int>(unit / columns), static_cast<int>(unit % columns),
+                                        threadIdx.x, s_stay, &u)) {
+            const int begin = u.from + warp * kRows;
+            long long src = 0;
+            auto look = [&](int i0) {  // the rows that a step's places come from, a lane a place
+                if (lane < kRows && i0 + lane < u.n) src = row_of<HD>(s, u, u.first + u.keep[i0 + lane]);
+            };
+            auto ask = [&](int i0, int stage) {  // a step's copies, and the rows of the step after it
+#pragma unroll
+                for (int k = 0; k < kMoveLoads; ++k) {
+                    const long long at = __shfl_sync(0xffffffffu, src, k * kAtOnce + nth);
+                    if (i0 + k * kAtOnce + nth < u.n) cp_async16(mine + (stage * kMoveWarps * kMoveLoads + k) * 32, u.cache + at);
+                }
+                cp_async_commit();
+                look(i0 + kStep);
+            };
+            look(begin);
+#pragma unroll
+            for (int k = 0; k < kMoveStages; ++k) ask(begin + k * kStep, k);
+            int stage = 0;
+            for (int i0 = begin; i0 - begin < u.n - u.from; i0 += kStep) {
+                long long dst = 0;
+                if (lane < kRows && i0 + lane < u.n) dst = row_of<HD>(s, u, u.first + i0 + lane);
+                cp_async_wait<kMoveStages - 1>();
+                __syncthreads();  // all warps have the step
+#pragma unroll
+                for (int k = 0; k < kMoveLoads; ++k) {
+                    const long long at = __shfl_sync(0xffffffffu, dst, k * kAtOnce + nth);
+                    if (i0 + k * kAtOnce + nth < u.n) u.cache[at] = mine[(stage * kMoveWarps * kMoveLoads + k) * 32];
+                }
+                ask(i0 + kMoveStages * kStep, stage);
+                stage = stage + 1 == kMoveStages ? 0 : stage + 1;
+            }
+            cp_async_wait<0>();
+        }
+        __syncthreads();
     }
 }
 
@@ -427,15 +495,16 @@ __global__ void __launch_bounds__(kMoveThreads) k_serve_copy(const __grid_consta
 
 cudaError_t launch_serve_compact(const ServeShape& s, const dllm_serve_tables& t, const ServeCaches& c,
                                  const ServeCompactArgs& a, int sms, cudaStream_t st) {
-    // short lists (an accepted path) a warp a column, others a CTA
     const bool small = a.keep_ld <= 64;
     const long long units = 2ll * c.n * s.Hkv * a.batch, ctas = small ? (units + kMoveWarps - 1) / kMoveWarps : units;
     const dim3 grid(static_cast<unsigned>(ctas < 64ll * sms ? ctas : 64ll * sms));
     if (small)
-        return s.hd == 128 ? serve_launch(k_serve_compact<128, 1, 16>, grid, kMoveThreads, 0, st, s, t, c, a)
-                           : serve_launch(k_serve_compact<64, 1, 32>, grid, kMoveThreads, 0, st, s, t, c, a);
-    return s.hd == 128 ? serve_launch(k_serve_compact<128, kMoveWarps, 16>, grid, kMoveThreads, 0, st, s, t, c, a)
-                       : serve_launch(k_serve_compact<64, kMoveWarps, 32>, grid, kMoveThreads, 0, st, s, t, c, a);
+        return s.hd == 128 ? serve_launch(k_serve_compact<128>, grid, kMoveThreads, 0, st, s, t, c, a)
+                           : serve_launch(k_serve_compact<64>, grid, kMoveThreads, 0, st, s, t, c, a);
+    const auto kernel = s.hd == 128 ? k_serve_compact_long<128> : k_serve_compact_long<64>;
+    const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, kMoveSmem);
+    if (e != cudaSuccess) return e;
+    return serve_launch(kernel, grid, kMoveThreads, kMoveSmem, st, s, t, c, a);
 }
 
 size_t serve_fork_bytes(const ServeShape& s) { return fork_arrays(s, nullptr, nullptr); }
