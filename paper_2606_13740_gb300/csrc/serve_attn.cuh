@@ -166,6 +166,12 @@ __device__ __forceinline__ uint64_t seen_bits(const uint32_t* m, int words, int 
     }
     return (static_cast<uint64_t>(word(1)) << 32 | word(0)) << -d | ((1ull << -d) - 1);
 }
+// Whether a live row of a block (f: its info, valid: its keys) may see less than all of it, in the tile from token tok0 on.
+template <bool TREE>
+__device__ __forceinline__ bool sees_partly(const int4& f, int valid, int tok0, int causal) {
+    if (TREE && f.w < f.z + valid) return true;  // new tokens among its keys
+    return causal && f.w + max(tok0, f.x) - f.x + 1 - f.z < valid;
+}
 // The first n of 64 bits.
 __device__ __forceinline__ uint64_t low_bits(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
 
@@ -277,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     pdl_launch_dependents();
     const bool same = serve_same_shape(s, *w.head);  // else the plan of another config, or none
     const int rows = same ? min(w.head->rows, a.rows) : 0, ctas = same ? w.head->ctas : 0;
-    const int prefix_blocks = w.head->prefix_blocks, prefix_len = w.head->prefix_len;
+    const int prefix_blocks = w.head->prefix_blocks, prefix_len = w.head->prefix_len, causal = w.head->causal;
     if (!same && w.head->ctas && threadIdx.x == 0 && cta == 0) atomicOr(t.status, DLLM_SERVE_STATE);
     // rows that are padding
     for (long long i = static_cast<long long>(rows) * s.H * (HD / 8) + static_cast<long long>(cta) * kThreads + threadIdx.x;
@@ -301,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         // ------------------------------------------------ loads
         const bool leader = elect_one(), is_k = warp == 4;
         const CUtensorMap* tm = is_k ? &maps.k : &maps.v;
-        const uint64_t once = policy_evict_first(), often = policy_evict_last();
+        const uint64_t once = policy_evict_first(), often = policy_evict_last(), again = policy_evict_normal();
         const int lg = s.page_log2, page = s.page, boxes = page < kServeBlock ? kServeBlock >> lg : 1;
         const int n_prefix = min(a.n_prefix, (prefix_len + page - 1) >> lg);
         if (static_cast<long long>(a.n_prefix) * page < prefix_len && cta == 0 && is_k && leader)
@@ -336,6 +342,12 @@ __global__ void __launch_bounds__(kThreads, 2)
             }
             return p;
         };
+        // whether a step's keys are those of a request that has rows in other tiles too
+        auto shared_of = [&](int step) {
+            if (step < prefix_blocks) return false;
+            const int4 f = w.info[at.own0 + step - prefix_blocks];
+            return f.x < at.tile * s.tile_tokens || f.y > (at.tile + 1) * s.tile_tokens;
+        };
         int j = 0, seg = 0;
         bool ok = true;
         do {
@@ -351,11 +363,20 @@ __global__ void __launch_bounds__(kThreads, 2)
                 ++seg;
             }
             int4 cur, nxt = make_int4(-1, 0, -1, -1);
-            if (lane < at.n) nxt = pages_of(at.step + lane);
+            bool more = false;
+            uint32_t reread = 0;
+            if (lane < at.n) {
+                nxt = pages_of(at.step + lane);
+                more = shared_of(at.step + lane);
+            }
             for (int i = 0; i < at.n; ++i) {
                 if ((i & 31) == 0) {
                     cur = nxt;
-                    if (i + 32 + lane < at.n) nxt = pages_of(at.step + i + 32 + lane);
+                    reread = __ballot_sync(0xffffffffu, more);
+                    if (i + 32 + lane < at.n) {
+                        nxt = pages_of(at.step + i + 32 + lane);
+                        more = shared_of(at.step + i + 32 + lane);
+                    }
                 }
                 const int p0 = __shfl_sync(0xffffffffu, cur.x, i & 31), p1 = __shfl_sync(0xffffffffu, cur.y, i & 31);
                 const int p2 = __shfl_sync(0xffffffffu, cur.z, i & 31), p3 = __shfl_sync(0xffffffffu, cur.w, i & 31);
@@ -365,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                     break;
                 }
                 if (leader) {
-                    const uint64_t pol = at.step + i < prefix_blocks ? often : once;
+                    const uint64_t pol = at.step + i < prefix_blocks ? often : reread >> (i & 31) & 1u ? again : once;
                     uint8_t* dst = ring + st * kKV;
                     const int y = at.hk * page;
                     mbar_arrive_expect_tx(&full[st], kKV);
@@ -438,30 +459,75 @@ __global__ void __launch_bounds__(kThreads, 2)
             const uint64_t vd = sw128(smem_u32(sV), kHalfKV, 1024);
             do {
                 if (at.left <= 0) break;
-                // first and last + 1 live lane of a step
+                // of a step: first and last + 1 live lane, keys that there are, whether rows see less than those
                 const int tok0 = at.tile * s.tile_tokens;
                 auto live_of = [&](int step) {
-                    int2 r = make_int2(0, kServeRows);
-                    if (step >= prefix_blocks) {
+                    int lo = 0, hi = kServeRows, valid = kServeBlock;
+                    bool partly = false;
+                    if (step < prefix_blocks) {
+                        valid = min(valid, prefix_len - step * kServeBlock);
+                    } else {
                         const int4 f = w.info[at.own0 + step - prefix_blocks];
-                        r.x = max(f.x - tok0, 0) * s.G;
-                        r.y = min(f.y - tok0, s.tile_tokens) * s.G;
+                        lo = max(f.x - tok0, 0) * s.G;
+                        hi = min(f.y - tok0, s.tile_tokens) * s.G;
+                        valid = max(min(valid, f.w + f.y - f.x - f.z), 0);
+                        partly = sees_partly<TREE>(f, valid, tok0, causal);
                     }
-                    return r;
+                    return lo | hi << 8 | valid << 16 | static_cast<int>(partly) << 24;
                 };
-                int2 cur, nxt = make_int2(0, 0);
+                int cur, nxt = 0;
                 if (lane < at.n) nxt = live_of(at.step + lane);
                 for (int i = 0; i < at.n; ++i, ++j) {
                     if ((i & 31) == 0) {
                         cur = nxt;
                         if (i + 32 + lane < at.n) nxt = live_of(at.step + i + 32 + lane);
                     }
-                    const int lo = __shfl_sync(0xffffffffu, cur.x, i & 31), hi = __shfl_sync(0xffffffffu, cur.y, i & 31);
+                    const int x = __shfl_sync(0xffffffffu, cur, i & 31);
+                    const int lo = x & 255, hi = x >> 8 & 255, valid = x >> 16 & 255;
                     const uint4 off = make_uint4(~bit_run(lo, hi), ~bit_run(lo - 32, hi - 32), ~bit_run(lo - 64, hi - 64),
                                                  ~bit_run(lo - 96, hi - 96));
                     const int st = j % NB, sb = j % 2;
-                    ok = wait_all(&vfull[st], static_cast<uint32_t>((j / NB) & 1)) &&
-                         wait_all(&pfull[sb], static_cast<uint32_t>((j / 2) & 1));
+                    ok = wait_all(&vfull[st], static_cast<uint32_t>((j / NB) & 1));
+                    if (!ok) break;
+                    if (valid < kServeBlock || x >> 24) {
+                        // While the softmax is at work: the values of keys that are not there become 0; so do infinities
+                        // and NaN that some row must not see (its P is 0, but they would come through the MMA all
+                        // the same), which the rows that see them get at the unit's end.
+                        uint4* v4 = reinterpret_cast<uint4*>(sV + st * kKV);
+                        if (x >> 24) {
+                            uint32_t odd = 0;
+                            auto bits = [](uint32_t u) { return odd_halves<T>(u); };
+#pragma unroll 4
+                            for (int k = lane; k < valid * 8; k += 32) {
+#pragma unroll
+                                for (int h = 0; h < kParts; ++h) {
+                                    const uint4 y = v4[h * (kHalfKV / 16) + k];
+                                    odd |= bits(y.x) | bits(y.y) | bits(y.z) | bits(y.w);
+                                }
+                            }
+                            if (odd) {
+#pragma unroll 1
+                                for (int k = lane; k < valid * 8; k += 32) {
+                                    for (int h = 0; h < kParts; ++h) {
+                                        uint4& y = v4[h * (kHalfKV / 16) + k];
+                                        y.x &= ~((bits(y.x) >> 15) * 0xffffu);
+                                        y.y &= ~((bits(y.y) >> 15) * 0xffffu);
+                                        y.z &= ~((bits(y.z) >> 15) * 0xffffu);
+                                        y.w &= ~((bits(y.w) >> 15) * 0xffffu);
+                                    }
+                                }
+                                *const_cast<volatile int*>(&sy.odd) = 1;
+                            }
+                        }
+                        for (int k = valid * 8 + lane; k < kServeBlock * 8; k += 32) {
+#pragma unroll
+                            for (int h = 0; h < kParts; ++h) v4[h * (kHalfKV / 16) + k] = make_uint4(0, 0, 0, 0);
+                        }
+                        __threadfence_block();
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                    }
+                    ok = wait_all(&pfull[sb], static_cast<uint32_t>((j / 2) & 1));
                     if (!ok) break;
                     tc_fence_after();
                     if (leader) {
@@ -492,14 +558,9 @@ __global__ void __launch_bounds__(kThreads, 2)
         const uint32_t lane_off = static_cast<uint32_t>(warp * 32) << 16;
         const uint32_t t_o = tmem + lane_off, t_s = tmem + 128 + lane_off;
         const float sl2 = a.scale * 1.4426950408889634f;
-        const int causal = w.head->causal, full_blocks = prefix_len / kServeBlock;
+        const int full_blocks = prefix_len / kServeBlock;
         auto wait = [&](uint64_t* bar, uint32_t parity) {
             return __all_sync(0xffffffffu, mbar_wait(bar, parity, &s_abort, t.status)) != 0;
-        };
-        // whether a live row of a block may see less than all of it (f: its info)
-        auto unseen = [&](const int4& f, int valid) {
-            if (TREE && f.w < f.z + valid) return true;  // new tokens among its keys
-            return causal && f.w + max(at.tile * s.tile_tokens, f.x) - f.x + 1 - f.z < valid;
         };
         int j = 0;
         bool ok = true;
@@ -508,6 +569,8 @@ __global__ void __launch_bounds__(kThreads, 2)
             const int tok = at.tile * s.tile_tokens + tok_off;
             const bool there = tok_off < s.tile_tokens && tok < rows;
             float m = -INFINITY, l = 0.0f;
+            // of the request whose own keys are at hand: keys from the step's block on, its new tokens, which of them the row is
+            int n_left = 0, q_rows = 0, nth = 0;
             {
                 uint32_t zero[32];
 #pragma unroll
@@ -520,20 +583,26 @@ __global__ void __launch_bounds__(kThreads, 2)
                 // Keys of the block that there are, and that this row sees.  A row that is not live (of another
                 // request) computes on, unmasked, and keeps its m and l: its lane of O is not written.
                 int valid = kServeBlock, seen = kServeBlock;
-                bool live = true, masked = false, some = true, any_live = true, partly = false;
+                bool live = true, masked = false, some = true, any_live = true;
                 uint64_t bits = ~0ull;  // TREE: those keys
                 if (step >= full_blocks) {
                     if (step < prefix_blocks) {
                         valid = seen = prefix_len - step * kServeBlock;
                     } else {
-                        const int4 f = w.info[at.own0 + step - prefix_blocks];
-                        valid = min(kServeBlock, f.w + f.y - f.x - f.z);
-                        live = there && tok >= f.x && tok < f.y;
-                        seen = causal ? min(valid, f.w + tok - f.x + 1 - f.z) : valid;
-                        partly = unseen(f, valid);
-                        if constexpr (TREE) {
-                            if (live && f.w < f.z + valid) bits = seen_bits(a.mask + static_cast<size_t>(tok) * a.words, a.words, f.z - f.w);
+                        if (n_left <= 0) {  // (a request's blocks follow one another)
+                            const int4 f = w.info[at.own0 + step - prefix_blocks];
+                            q_rows = f.y - f.x;
+                            nth = tok - f.x;
+                            n_left = f.w + q_rows - f.z;
                         }
+                        valid = min(kServeBlock, n_left);
+                        live = there && static_cast<unsigned>(nth) < static_cast<unsigned>(q_rows);
+                        seen = causal ? min(valid, n_left - q_rows + nth + 1) : valid;
+                        if constexpr (TREE) {
+                            if (live && q_rows - n_left + valid > 0)
+                                bits = seen_bits(a.mask + static_cast<size_t>(tok) * a.words, a.words, q_rows - n_left);
+                        }
+                        n_left -= kServeBlock;
                     }
                     if constexpr (TREE) {
                         bits &= low_bits(seen);
@@ -542,38 +611,6 @@ __global__ void __launch_bounds__(kThreads, 2)
                     masked = __any_sync(0xffffffffu, live && seen < kServeBlock);
                     some = __any_sync(0xffffffffu, live && seen > 0);
                     any_live = __any_sync(0xffffffffu, live);
-                }
-                if (partly) {
-                    // Values that some row must not see: its P is 0, but an infinity or NaN would come through the MMA
-                    // all the same.  They are taken out (while S is made), and put to the rows that see them at the end.
-                    const int st = j % NB;
-                    ok = wait(&vfull[st], static_cast<uint32_t>((j / NB) & 1));
-                    if (!ok) break;
-                    uint4* v4 = reinterpret_cast<uint4*>(sV + st * kKV) + r;
-                    uint32_t odd = 0;
-#pragma unroll
-                    for (int k = 0; k < kServeBlock * 8; k += 128) {
-                        if (k + r >= valid * 8) break;
-#pragma unroll
-                        for (int h = 0; h < kParts; ++h) {
-                            const uint4 x = v4[h * (kHalfKV / 16) + k];
-                            odd |= odd_halves<T>(x.x) | odd_halves<T>(x.y) | odd_halves<T>(x.z) | odd_halves<T>(x.w);
-                        }
-                    }
-                    if (odd) {
-#pragma unroll 1
-                        for (int k = 0; k + r < valid * 8; k += 128) {
-                            for (int h = 0; h < kParts; ++h) {
-                                uint4& x = v4[h * (kHalfKV / 16) + k];
-                                x.x &= ~((odd_halves<T>(x.x) >> 15) * 0xffffu);
-                                x.y &= ~((odd_halves<T>(x.y) >> 15) * 0xffffu);
-                                x.z &= ~((odd_halves<T>(x.z) >> 15) * 0xffffu);
-                                x.w &= ~((odd_halves<T>(x.w) >> 15) * 0xffffu);
-                            }
-                        }
-                        *const_cast<volatile int*>(&sy.odd) = 1;
-                        fence_proxy_async_smem();
-                    }
                 }
                 ok = wait(&sfull[sb], static_cast<uint32_t>((j / 2) & 1));
                 if (!ok) break;
@@ -650,18 +687,6 @@ __global__ void __launch_bounds__(kThreads, 2)
                     for (int k = 0; k < 32; ++k) zero[k] = 0u;
                     tmem_st_32u(ts, zero);
                 }
-                if (valid < kServeBlock) {
-                    // the values of keys that are not there
-                    const int st = j % NB;
-                    ok = wait(&vfull[st], static_cast<uint32_t>((j / NB) & 1));
-                    if (!ok) break;
-                    uint4* v4 = reinterpret_cast<uint4*>(sV + st * kKV);
-                    for (int k = max(valid, 0) * 8 + r; k < kServeBlock * 8; k += 128) {
-#pragma unroll
-                        for (int h = 0; h < kParts; ++h) v4[h * (kHalfKV / 16) + k] = make_uint4(0, 0, 0, 0);
-                    }
-                    fence_proxy_async_smem();
-                }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&pfull[sb]);
@@ -684,7 +709,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                     for (int step = max(at.step, prefix_blocks); step < at.step + at.n; ++step) {
                         const int4 f = w.info[at.own0 + step - prefix_blocks], pg = w.pages[at.own0 + step - prefix_blocks];
                         const int valid = min(kServeBlock, f.w + f.y - f.x - f.z);
-                        if (!there || tok < f.x || tok >= f.y || !unseen(f, valid)) continue;
+                        if (!there || tok < f.x || tok >= f.y || !sees_partly<TREE>(f, valid, at.tile * s.tile_tokens, causal)) continue;
                         const int seen = causal ? min(valid, f.w + tok - f.x + 1 - f.z) : valid;
                         uint64_t bits = ~0ull;
                         if constexpr (TREE) bits = seen_bits(a.mask + static_cast<size_t>(tok) * a.words, a.words, f.z - f.w);

@@ -261,7 +261,7 @@ __device__ __forceinline__ int block_before(int v, int* buf, int* sum) {
 // between cluster barriers; or (SMALL) one CTA, marks in shared memory.  Nothing that others read is changed before it is
 // known that the fork can be carried out.
 template <bool SMALL>
-__global__ void __launch_bounds__(kForkThreads) k_serve_fork(const __grid_constant__ ServeShape s,
+__global__ void __launch_bounds__(kForkThreads, 1) k_serve_fork(const __grid_constant__ ServeShape s,
                                                              const __grid_constant__ dllm_serve_tables t, const int* src,
                                                              const int* len, int batch, int row_lanes) {
     extern __shared__ int smem[];
@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(kForkThreads) k_serve_fork(const __grid_consta
     const int p0 = static_cast<int>(static_cast<long long>(s.n_pages) * rank / ctas);
     const int p1 = static_cast<int>(static_cast<long long>(s.n_pages) * (rank + 1) / ctas);
     if (SMALL) {
-        for (int p = tid; p < s.n_pages; p += kForkThreads) mark[p] = 0;
+        for (int p = tid; p < s.n_pages; p += kForkThreads) mark[p] = writer[p] = 0;
     }
     pdl_wait();
     pdl_launch_dependents();
@@ -308,10 +308,12 @@ __global__ void __launch_bounds__(kForkThreads) k_serve_fork(const __grid_consta
     auto free_page = [&](int k) { return t.ring[(head + k) % static_cast<unsigned>(s.n_pages)]; };
     const int ring0 = tid < min(batch, free_n) ? free_page(tid) : 0;  // (asked for ahead of its use)
     if (!SMALL) {
-        for (int p = p0 + tid; p < p1; p += kForkThreads) mark[p] = 0;
+        for (int p = p0 + tid; p < p1; p += kForkThreads) mark[p] = writer[p] = 0;
     }
     if (rank == 0 && tid < 2) f.head[tid] = 0;
-    __syncthreads();
+    barrier();
+
+    // ------------------------------------------------ who holds what; row_lanes threads a row
     for (int b = tid; b < batch; b += kForkThreads) {
         const int n = s_len[b], from = s_src[b];
         int last = -1;
@@ -320,29 +322,15 @@ __global__ void __launch_bounds__(kForkThreads) k_serve_fork(const __grid_consta
         } else if (n & (page - 1)) {
             last = t.table[static_cast<size_t>(from) * M + (n >> lg)];
             if (last < 0 || last >= s.n_pages) bits |= DLLM_SERVE_STATE;
-            else if (rank == 0) writer[last] = 0;
+            else if (rank == 0) atomicMax(writer + last, B - b);
         }
         s_last[b] = last;
     }
-    const bool wrong = __syncthreads_or(bits) != 0;
-    barrier();
-    auto refuse = [&](int why) {
-        if (rank == 0) {
-            if (why) atomicOr(t.status, why);
-            if (tid == 0) {
-                t.status[1] = batch;
-                t.status[2] = t.status[3] = 0;
-            }
-        }
-    };
-    if (wrong) return refuse(bits);
-
-    // ------------------------------------------------ who holds what; row_lanes threads a row
     const int sub = tid % row_lanes, row0 = rank * (kForkThreads / row_lanes) + tid / row_lanes;
     const int rows = ctas * (kForkThreads / row_lanes);
     bool out = false;
     for (int r = row0; r < B; r += rows) {
-        const int held = s_held[r], full = s_len[r] >> lg;
+        const int held = s_held[r], full = min(s_len[r] >> lg, s_held[s_src[r]]);
         const int* row = t.table + static_cast<size_t>(r) * M;
         const int* from = t.table + static_cast<size_t>(s_src[r]) * M;
         const bool more = r >= batch;  // a row that stays
@@ -362,20 +350,23 @@ __global__ void __launch_bounds__(kForkThreads) k_serve_fork(const __grid_consta
             }
         }
     }
-    if (rank == 0) {
-        for (int b = tid; b < batch; b += kForkThreads)
-            if (s_last[b] >= 0) atomicMax(writer + s_last[b], B - b);
-    }
     if (tid < min(batch, free_n) && (ring0 < 0 || ring0 >= s.n_pages)) out = true;
     for (int k = kForkThreads + tid; k < min(batch, free_n); k += kForkThreads) out |= free_page(k) < 0 || free_page(k) >= s.n_pages;
-    if (SMALL) {
-        out = __syncthreads_or(out);
-    } else {
-        if (out) f.head[1] = 1;
+    if (out) bits |= DLLM_SERVE_STATE;
+    bool wrong = __syncthreads_or(bits) != 0;
+    if (!SMALL) {
+        if (wrong) f.head[1] = 1;
         barrier();
-        out = f.head[1];
+        wrong = f.head[1];
     }
-    if (out) return refuse(tid == 0 ? DLLM_SERVE_STATE : 0);
+    auto refuse = [&](int why) {
+        if (why) atomicOr(t.status, why);
+        if (rank == 0 && tid == 0) {
+            t.status[1] = batch;
+            t.status[2] = t.status[3] = 0;
+        }
+    };
+    if (wrong) return refuse(bits);
 
     // ------------------------------------------------ the last pages: kept, or copied
     const int per = (batch + kForkThreads - 1) / kForkThreads;
@@ -387,7 +378,7 @@ __global__ void __launch_bounds__(kForkThreads) k_serve_fork(const __grid_consta
     int mine = 0, taken;
     for (int b = b0; b < b1; ++b) mine += copied(b);
     int nth = block_before(mine, s_scan, &taken);
-    if (taken > free_n) return refuse(tid == 0 ? DLLM_SERVE_PAGES : 0);
+    if (taken > free_n) return refuse(rank == 0 && tid == 0 ? DLLM_SERVE_PAGES : 0);
     for (int b = b0; b < b1; ++b) {
         const int p = s_last[b];
         if (p < 0) continue;
