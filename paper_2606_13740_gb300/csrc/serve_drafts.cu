@@ -79,7 +79,7 @@ int dllm_serve_compact(const dllm_serve_config* cfg, const dllm_serve_tables* t,
     ServeShape s;
     ServeCaches c;
     if (const char* why = shape_of(cfg, &s)) return fail(DLLM_EINVAL, "serve config: %s", why);
-    if (!whole(t) || !first || !keep || !n || !words(first, keep, n)) return fail(DLLM_EINVAL, "serve compact: null or misaligned buffer");
+    if (!whole(t) || !first || (keep_ld > 0 && !keep) || !n || !words(first, keep, n)) return fail(DLLM_EINVAL, "serve compact: null or misaligned buffer");
     if (const char* why = caches_of(kc, vc, n_layers, &c)) return fail(DLLM_EINVAL, "serve compact: %s", why);
     if (batch < 1 || batch > s.max_batch) return fail(DLLM_EINVAL, "serve compact: batch must be 1 to max_batch");
     if (keep_ld < 0) return fail(DLLM_EINVAL, "serve compact: negative keep_ld");

@@ -177,6 +177,23 @@ def test_tree_attention_with_every_bit_is_attention(dev):
     x.check()
 
 
+def test_tree_attention_of_a_long_chain_is_causal_attention(dev):
+    """A chain of 2100 tokens: by the bits alone, and after a causal plan bit for bit what the plan alone gives."""
+    def chain(x):
+        at, rows = 0, []
+        for q in x.Q:
+            rows += [_words((2 << t) - 1, x.words) for t in range(q)]
+        x.mask = _i32(rows)
+        return x
+
+    a = chain(Tree([100, 7], [2100, 65], 70, 64, 8, 2, 128, form="all", seed=21, causal=True))
+    b = chain(Tree([100, 7], [2100, 65], 70, 64, 8, 2, 128, form="all", seed=21))
+    want = Paged.call(a)
+    assert torch.equal(a.call(), want)
+    # the same sums in blocks cut otherwise: a rounding of P and one of the output each, of values of size 1 or so
+    assert float((b.call().double() - want.double()).norm() / want.double().norm()) <= 2 * 1.2 * U["bf16"]
+
+
 @pytest.mark.parametrize("dtype,spread", [("f16", 1.0), ("bf16", 12.0), ("f16", 12.0), ("bf16", 0.0)])
 def test_tree_attention_types_and_spreads(dev, dtype, spread):
     Tree([900, 31, 0, 2000], [1, 32, 100, 7], 1500, 32, 28, 4, 128, dtype=dtype, seed=5, spread=spread).check()
@@ -309,6 +326,24 @@ def test_compact_moves_what_is_kept(dev, hd, dtype, stride, page):
         x.s.dllm_serve_check()
         x.same(want)
     assert x.s.table.cpu().tolist() == table
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_compact_of_short_lists(dev, hd):
+    """Lists of up to 64 places, in steps of one warp; more requests than are asked for; no requests that move."""
+    r = random.Random(hd)
+    L = [r.randint(0, 90) for _ in range(37)]
+    x = Caches(L, 16, hd=hd, layers=3, Hkv=1, seed=3)
+    table = x.s.table.cpu().tolist()
+    for most in (1, 16, 17, 64):
+        keep = [sorted(r.sample(range(n), min(n, r.choice([0, 1, most, r.randint(0, most)])))) for n in L[:30]]
+        want = _compacted(x, x.copy(), table, [0] * 30, keep)
+        x.s.dllm_serve_compact(x.layers, _i32([0] * 30), _i32([k + [-1] * (most - len(k)) for k in keep]), _i32([len(k) for k in keep]))
+        x.s.dllm_serve_check()
+        x.same(want)
+    x.s.dllm_serve_compact(x.layers, _i32([0] * 30), torch.zeros(30, 0, device="cuda", dtype=torch.int32), _i32([0] * 30))
+    x.s.dllm_serve_check()
+    x.same(want)
 
 
 def test_compact_leaves_out_what_makes_no_sense(dev):
@@ -522,7 +557,7 @@ def _check_logprobs(z, tokens, mask, top):
 @pytest.mark.parametrize("N,V,top,tokens,mask", [
     (1, 1, 1, 1, -1), (3, 2, 5, 2, 1), (2, 31, 32, 3, 30), (5, 511, 7, 1, -1), (4, 512, 0, 0, 0), (3, 513, 32, 9, 512),
     (1, 126464, 5, 1, 126463), (33, 5000, 20, 2, 4999), (700, 1024, 32, 1, 1023), (2, 152064, 32, 300, 152063),
-    (2, 600001, 32, 1, 17),  # groups of two steps
+    (2, 600001, 32, 1, 17), (1, 2300000, 20, 2, -1),  # groups of several steps
 ])
 def test_logprobs_match_64_bits(dev, dtype, N, V, top, tokens, mask):
     g = torch.Generator(device="cuda").manual_seed(N + V)
@@ -582,6 +617,30 @@ def test_logprobs_of_extremes(dev):
     assert bool(torch.isfinite(lse[5])) and bool(torch.isfinite(entropy[5])) and lp[5, 4] == -INF
     assert bool((lp[[0, 1, 2, 3, 5, 6, 7]][:, [2, 3, 4]] == -INF).all())
     assert lse[6] == -3 and entropy[6] == 0 and lp[6, 5] == 0 and ids[6].tolist() == [2000, -1, -1] and top_lp[6, 0] == 0
+
+
+def test_logprobs_of_masks_of_the_lowest_value(dev):
+    """Ids that a program has set to the type's lowest value, in runs and alone, and values past 10^37."""
+    g = torch.Generator(device="cuda").manual_seed(6)
+    V = 20000
+    for dtype in ("f32", "bf16", "f16"):
+        z = torch.randn(8, V, device="cuda", generator=g).to(DT[dtype])
+        low = torch.finfo(DT[dtype]).min
+        z[0, :V // 2] = low
+        z[1, V // 3:] = low
+        z[2, torch.rand(V, device="cuda", generator=g) < 0.9] = low
+        z[3] = low
+        z[3, 17] = low / 2
+        z[4, ::512] = -INF
+        z[4, 600:7000] = -INF
+        if dtype != "f16":
+            z[5] = (torch.randn(V, device="cuda", generator=g) * 3e37).to(DT[dtype])
+            z[6, 5000:] = -2e38
+            z[6, 9000] = 3e37
+            z[7] = -1e37 - 1e36 * torch.rand(V, device="cuda", generator=g).to(DT[dtype]).abs()
+        best = z[:, :V - 1].argmax(1, keepdim=True).to(torch.int32)
+        _check_logprobs(z, best, V - 1, 1)
+        _check_logprobs(z[:3], best[:3], V - 1, 32)
 
 
 def test_logprobs_ties_go_to_the_lowest_id(dev):
