@@ -24,9 +24,10 @@ constexpr int kCluster = 8;              // CTAs of a row, at most
 constexpr int kSpans = 4;                // 16-byte pieces of a lane in a step
 constexpr int kStages = 3;               // steps of a warp on their way
 constexpr int kGroups = 1024;            // of a row, at most
-constexpr int kList = 5600;              // ids that may be among the largest, at most; past kRanked they are thinned out
-constexpr int kRanked = 256;
-constexpr int kAhead = 8;                // loads of a thread in flight, of the groups that are read again
+constexpr int kChosen = 64;              // groups that may hold one of the largest, at most
+constexpr int kRanked = 256;             // ids that may be among the largest: so many are ranked, more of them thinned out first
+constexpr int kList = 6144;
+constexpr int kRing = kWarps * kStages * kSpans * 32;  // 16-byte pieces
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kFar = -150.0f;          // exp of it is 0 in 32 bits
 constexpr float kFar2 = -216.0f;         // 2^ that too
@@ -167,22 +168,25 @@ __device__ __forceinline__ void load_some(const T* src, int v, int vocab, float*
 // Whether (value, id) comes before another among the largest.
 __device__ __forceinline__ bool before(float z, int v, float z2, int v2) { return z > z2 || (z == z2 && v < v2); }
 
+struct More {
+    float z[kList];
+    int v[kList];
+};
 // Shared memory of a CTA.  The steps on their way, and when all have been taken what the ending of a row needs.
 struct Shared {
     alignas(16) float top[kGroups];  // the groups' maxima
     Part part[kCluster * kWarps];    // of the row's warps
     Part all;
-    int n_groups, n, count[64];
+    int group[kChosen], n_groups, n, count[64];
     float least;
-    union {
-        alignas(16) uint4 ring[kWarps][kStages][kSpans * 32];
-        struct {
-            float z[kList];
-            int v[kList], group[kGroups];
-        };
-    };
+    alignas(16) float z[kRanked];  // ids that may be among the largest
+    int v[kRanked];
     float best[kWarps];
     int id[kWarps];
+    union {
+        alignas(16) uint4 ring[kRing];
+        More more;
+    };
 };
 static_assert(4 * (sizeof(Shared) + 1024) <= 228 * 1024, "four CTAs an SM");
 
@@ -210,14 +214,19 @@ __device__ __forceinline__ void choose(Shared& sh, int groups, int k) {
         next = max(next, min(x, top));
         top = max(top, x);
     }
-    int rank = 0, rank2 = 0;
-#pragma unroll 8
-    for (int i = 0; i < 32; ++i) {
-        const uint32_t o = __shfl_sync(0xffffffffu, top, i), o2 = __shfl_sync(0xffffffffu, next, i);
-        rank += (o > top || (o == top && i < lane)) + (o2 > top);
-        rank2 += (o >= next) + (o2 > next || (o2 == next && i < lane));
+    // how many of all lanes' are no less than the lane's own two (by way of shared memory, the ids' places)
+    uint32_t* both = reinterpret_cast<uint32_t*>(sh.z);
+    both[lane] = top;
+    both[32 + lane] = next;
+    __syncwarp();
+    int reach1 = 0, reach2 = 0;
+#pragma unroll
+    for (int i = 0; i < 64; i += 4) {
+        const uint4 o = *reinterpret_cast<const uint4*>(both + i);
+        reach1 += (o.x >= top) + (o.y >= top) + (o.z >= top) + (o.w >= top);
+        reach2 += (o.x >= next) + (o.y >= next) + (o.z >= next) + (o.w >= next);
     }
-    const uint32_t nth = __reduce_max_sync(0xffffffffu, rank == k - 1 ? top : rank2 == k - 1 ? next : 0u);
+    const uint32_t nth = __reduce_max_sync(0xffffffffu, reach1 >= k ? top : reach2 >= k ? next : 0u);
     uint32_t least = nth;
     if (least == 0) least = 1;
     auto reach = [&](uint32_t from) {  // how many are no less
@@ -246,6 +255,18 @@ __device__ __forceinline__ void choose(Shared& sh, int groups, int k) {
         sh.n_groups = n;
         sh.least = least > 1 ? __uint_as_float(least >> 31 ? least & 0x7fffffffu : ~least) : kLowest;
     }
+}
+
+// f of the values side by side (the first of id v) that are no less than least.
+template <int N, typename F>
+__device__ __forceinline__ void look(const float (&z)[N], int v, float least, int mask_id, const F& f) {
+    float mx = z[0];
+#pragma unroll
+    for (int c = 1; c < N; ++c) mx = fmaxf(mx, z[c]);
+    if (!(mx >= least)) return;
+#pragma unroll
+    for (int c = 0; c < N; ++c)
+        if (z[c] >= least && v + c != mask_id) f(v + c, z[c]);
 }
 
 // The row's values from the parts of its `warps` warps and the groups' maxima, which lie in sh.  (z_token: the logit of the
@@ -280,19 +301,18 @@ __device__ __forceinline__ void finish(const dllm_serve_logprobs_args& a, int ro
     const int total = n_groups * group_pieces * kLoads;
     static_assert(kThreads % kLoads == 0, "a load's place in its step is the thread's own");
     auto id_of = [&](int i) {
-        if (i >= total) return a.vocab;
         const int piece = i / kLoads, g = group_pieces == 1 ? piece : piece / group_pieces;
         return (sh.group[g] * group_pieces + piece - g * group_pieces) * kPiece<T> + i % kLoads * kPer;
     };
-    auto load = [&](int i0, uint4 (&x)[kAhead]) {
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int v = id_of(i0 + u * kThreads);
-            if (VEC && v + kPer <= a.vocab) x[u] = *reinterpret_cast<const uint4*>(src + v);
+    auto ask = [&](int i0) {  // for a thread's own, up to a ring full
+        for (int i = i0 + tid; i < min(total, i0 + kRing); i += kThreads) {
+            const int v = id_of(i);
+            if (VEC && v + kPer <= a.vocab) cp_async16(sh.ring + (i - i0), src + v);
         }
+        cp_async_commit();
     };
-    uint4 ahead[kAhead];
-    load(tid, ahead);
+    static_assert(kRing <= 32 * kThreads, "a bit for each of a thread's loads");
+    ask(0);
 
     const Part all = sh.all;
     const bool none = all.m == -INFINITY && all.s == 0.0f, above = all.m == INFINITY;
@@ -311,84 +331,86 @@ __device__ __forceinline__ void finish(const dllm_serve_logprobs_args& a, int ro
     if (!k) return;
 
     // ------------------------------------------------ the largest
-    auto each = [&](auto&& f) {  // of the groups' ids that may be among them; the first loads are there
-        for (int i0 = tid; i0 < total; i0 += kAhead * kThreads) {
-            if (i0 != tid) load(i0, ahead);
+    for (int i0 = 0; i0 < total; i0 += kRing) {
+        cp_async_wait<0>();
+        // first which of the thread's loads hold one at all
+        auto get = [&](int i, float (&z)[kPer]) {
+            const int v = id_of(i);
+            if (VEC && v + kPer <= a.vocab) Raw<T>::floats(sh.ring[i - i0], z);
+            else load_some(src, v, a.vocab, z);
+            return v;
+        };
+        const int mine = (min(total - i0, kRing) - tid + kThreads - 1) / kThreads;
+        uint32_t hits = 0;
+#pragma unroll 4
+        for (int u = 0; u < mine; ++u) {
+            float z[kPer];
+            get(i0 + tid + u * kThreads, z);
+            float mx = z[0];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                if (i0 + u * kThreads >= total) break;
-                const int v = id_of(i0 + u * kThreads);
-                float z[kPer];
-                if (VEC && v + kPer <= a.vocab) Raw<T>::floats(ahead[u], z);
-                else load_some(src, v, a.vocab, z);
-                float mx = z[0];
-#pragma unroll
-                for (int c = 1; c < kPer; ++c) mx = fmaxf(mx, z[c]);
-                if (!(mx >= least)) continue;
-#pragma unroll
-                for (int c = 0; c < kPer; ++c)
-                    if (z[c] >= least && v + c != a.mask_id) f(v + c, z[c]);
-            }
+            for (int c = 1; c < kPer; ++c) mx = fmaxf(mx, z[c]);
+            hits |= static_cast<uint32_t>(mx >= least) << u;
         }
-    };
-    each([&](int v, float z) {
-        const int at = atomicAdd(&sh.n, 1);
-        if (at < kList) {
-            sh.z[at] = z;
-            sh.v[at] = v;
-        }
-    });
-    __syncthreads();
-    int n = min(sh.n, kList);
-    int* ids = a.top_ids + static_cast<long long>(row) * a.n_top;
-    float* lps = a.top_lp + static_cast<long long>(row) * a.n_top;
-    if (sh.n > kList) {
-        // more equal ones than there are places: the largest below the one before, one by one
-        float z0 = INFINITY;
-        int v0 = -1;
-        for (int r = 0; r < a.n_top; ++r) {
-            float bz = -INFINITY;
-            int bv = a.vocab;
-            load(tid, ahead);
-            each([&](int v, float z) {
-                if (before(z0, v0, z, v) && before(z, v, bz, bv)) {
-                    bz = z;
-                    bv = v;
+        for (; hits; hits &= hits - 1) {
+            float z[kPer];
+            const int v = get(i0 + tid + (__ffs(hits) - 1) * kThreads, z);
+            look(z, v, least, a.mask_id, [&](int id, float x) {
+                const int at = atomicAdd(&sh.n, 1);
+                if (at < kRanked) {
+                    sh.z[at] = x;
+                    sh.v[at] = id;
                 }
             });
-#pragma unroll
-            for (int d = 16; d; d /= 2) {
-                const float oz = __shfl_xor_sync(0xffffffffu, bz, d);
-                const int ov = __shfl_xor_sync(0xffffffffu, bv, d);
-                if (before(oz, ov, bz, bv)) {
-                    bz = oz;
-                    bv = ov;
-                }
+        }
+        if (i0 + kRing < total) ask(i0 + kRing);
+    }
+    __syncthreads();
+    const int n = sh.n;
+    int* ids = a.top_ids + static_cast<long long>(row) * a.n_top;
+    float* lps = a.top_lp + static_cast<long long>(row) * a.n_top;
+    if (n <= kRanked) {
+        if (tid < n) {
+            const float z = sh.z[tid];
+            const int v = sh.v[tid];
+            int rank = 0;
+#pragma unroll 4
+            for (int j = 0; j < n; ++j) rank += before(sh.z[j], sh.v[j], z, v);
+            if (rank < a.n_top) {
+                ids[rank] = v;
+                lps[rank] = lp_of(z);
             }
-            if (lane == 0) {
-                sh.best[warp] = bz;
-                sh.id[warp] = bv;
-            }
-            __syncthreads();
-            z0 = sh.best[0];
-            v0 = sh.id[0];
-            for (int i = 1; i < kWarps; ++i)
-                if (before(sh.best[i], sh.id[i], z0, v0)) {
-                    z0 = sh.best[i];
-                    v0 = sh.id[i];
-                }
-            if (tid == 0) {
-                ids[r] = v0;
-                lps[r] = lp_of(z0);
-            }
-            __syncthreads();
+        }
+        for (int r = n + tid; r < a.n_top; r += kThreads) {
+            ids[r] = -1;
+            lps[r] = -INFINITY;
         }
         return;
     }
-    if (n > kRanked) {
+    // Many equal ones, or a small vocabulary: from memory again.
+    auto each = [&](const auto& f) {
+#pragma unroll 1
+        for (int i = tid; i < total; i += kThreads) {
+            const int v = id_of(i);
+            float z[kPer];
+            if (VEC && v + kPer <= a.vocab) Raw<T>::floats(*reinterpret_cast<const uint4*>(src + v), z);
+            else load_some(src, v, a.vocab, z);
+            look(z, v, least, a.mask_id, f);
+        }
+    };
+    if (n <= kList) {
+        __syncthreads();  // (all know n)
+        if (tid == 0) sh.n = 0;
+        __syncthreads();
+        each([&](int id, float x) {
+            const int at = atomicAdd(&sh.n, 1);
+            sh.more.z[at] = x;
+            sh.more.v[at] = id;
+        });
+        __syncthreads();
         // The n_top largest (value, id), which are all different, bit by bit.
-        const int want = min(a.n_top, n);
-        auto pair_of = [&](int i) { return static_cast<unsigned long long>(key_of(sh.z[i])) << 32 | static_cast<uint32_t>(~sh.v[i]); };
+        auto pair_of = [&](int i) {
+            return static_cast<unsigned long long>(key_of(sh.more.z[i])) << 32 | static_cast<uint32_t>(~sh.more.v[i]);
+        };
         unsigned long long from = 0;
         for (int bit = 63; bit >= 0; --bit) {
             const unsigned long long x = from | 1ull << bit;
@@ -398,37 +420,63 @@ __device__ __forceinline__ void finish(const dllm_serve_logprobs_args& a, int ro
             if (lane == 0 && c) atomicAdd(&sh.count[bit], c);
             __syncthreads();
             c = sh.count[bit];
-            if (c >= want) from = x;
-            if (c == want) break;
+            if (c >= a.n_top) from = x;
+            if (c == a.n_top) break;
         }
-        __syncthreads();
         if (tid == 0) sh.n = 0;
         __syncthreads();
         for (int i = tid; i < n; i += kThreads)
             if (pair_of(i) >= from) sh.group[atomicAdd(&sh.n, 1)] = i;
         __syncthreads();
-        const int left = sh.n;
-        if (tid < left) {
+        if (tid < a.n_top) {
             const int at = sh.group[tid];
+            const float z = sh.more.z[at];
+            const int v = sh.more.v[at];
             int rank = 0;
-            for (int j = 0; j < left; ++j) rank += before(sh.z[sh.group[j]], sh.v[sh.group[j]], sh.z[at], sh.v[at]);
-            ids[rank] = sh.v[at];
-            lps[rank] = lp_of(sh.z[at]);
-        }
-    } else if (tid < n) {
-        const float z = sh.z[tid];
-        const int v = sh.v[tid];
-        int rank = 0;
-#pragma unroll 4
-        for (int j = 0; j < n; ++j) rank += before(sh.z[j], sh.v[j], z, v);
-        if (rank < a.n_top) {
+            for (int j = 0; j < a.n_top; ++j) rank += before(sh.more.z[sh.group[j]], sh.more.v[sh.group[j]], z, v);
             ids[rank] = v;
             lps[rank] = lp_of(z);
         }
+        return;
     }
-    for (int r = n + tid; r < a.n_top; r += kThreads) {
-        ids[r] = -1;
-        lps[r] = -INFINITY;
+    // More equal ones than there are places: the largest below the one before, one by one.
+    float z0 = INFINITY;
+    int v0 = -1;
+    for (int r = 0; r < a.n_top; ++r) {
+        float bz = -INFINITY;
+        int bv = a.vocab;
+        each([&](int v, float z) {
+            if (before(z0, v0, z, v) && before(z, v, bz, bv)) {
+                bz = z;
+                bv = v;
+            }
+        });
+#pragma unroll
+        for (int d = 16; d; d /= 2) {
+            const float oz = __shfl_xor_sync(0xffffffffu, bz, d);
+            const int ov = __shfl_xor_sync(0xffffffffu, bv, d);
+            if (before(oz, ov, bz, bv)) {
+                bz = oz;
+                bv = ov;
+            }
+        }
+        if (lane == 0) {
+            sh.best[warp] = bz;
+            sh.id[warp] = bv;
+        }
+        __syncthreads();
+        z0 = sh.best[0];
+        v0 = sh.id[0];
+        for (int i = 1; i < kWarps; ++i)
+            if (before(sh.best[i], sh.id[i], z0, v0)) {
+                z0 = sh.best[i];
+                v0 = sh.id[i];
+            }
+        if (tid == 0) {
+            ids[r] = v0;
+            lps[r] = lp_of(z0);
+        }
+        __syncthreads();
     }
 }
 
@@ -449,7 +497,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 3)
     pdl_wait();
     pdl_launch_dependents();
     const T* src = static_cast<const T*>(a.logits) + row * a.ld;
-    uint4* const mine = sh.ring[warp][0] + lane;
+    uint4* const mine = sh.ring + warp * (kStages * kSpans * 32) + lane;
     const T* ps = src + static_cast<size_t>(q) * kPiece<T> + lane * kPer;
     auto ask = [&] {  // for the next whole step (a group of copies in any case, to count)
         if (asked < qw) {
