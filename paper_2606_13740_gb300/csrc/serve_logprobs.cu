@@ -203,32 +203,39 @@ __device__ __forceinline__ uint32_t key_of(float x) {
     return x > -INFINITY ? (b >> 31 ? ~b : b | 0x80000000u) : 0u;
 }
 
-// A warp chooses groups whose maxima reach a value that k of them, at least, reach (all where there are less), in order of their
-// numbers.  The k-th largest of the lanes' two largest is such a value.  Where it lets more than 2 k through (many equal
-// ones), the k-th largest of all is found bit by bit, and of those equal to it the first are taken.
-__device__ __forceinline__ void choose(Shared& sh, int groups, int k) {
+// A value that k of n, at least, reach, as a key: the k-th largest of the lanes' two largest each (0: they are less).  By one
+// warp; both: 64 words of shared memory, 16-byte aligned.
+__device__ __forceinline__ uint32_t bound_of(const float* x, int n, int k, uint32_t* both) {
     const int lane = threadIdx.x & 31;
     uint32_t top = 0, next = 0;
-    for (int g = lane; g < groups; g += 32) {
-        const uint32_t x = key_of(sh.top[g]);
-        next = max(next, min(x, top));
-        top = max(top, x);
+    for (int i = lane; i < n; i += 32) {
+        const uint32_t v = key_of(x[i]);
+        next = max(next, min(v, top));
+        top = max(top, v);
     }
-    // how many of all lanes' are no less than the lane's own two (by way of shared memory, the ids' places)
-    uint32_t* both = reinterpret_cast<uint32_t*>(sh.z);
     both[lane] = top;
     both[32 + lane] = next;
     __syncwarp();
-    int reach1 = 0, reach2 = 0;
+    int reach = 0, reach2 = 0;  // how many are no less
 #pragma unroll
     for (int i = 0; i < 64; i += 4) {
         const uint4 o = *reinterpret_cast<const uint4*>(both + i);
-        reach1 += (o.x >= top) + (o.y >= top) + (o.z >= top) + (o.w >= top);
+        reach += (o.x >= top) + (o.y >= top) + (o.z >= top) + (o.w >= top);
         reach2 += (o.x >= next) + (o.y >= next) + (o.z >= next) + (o.w >= next);
     }
-    const uint32_t nth = __reduce_max_sync(0xffffffffu, reach1 >= k ? top : reach2 >= k ? next : 0u);
-    uint32_t least = nth;
-    if (least == 0) least = 1;
+    return __reduce_max_sync(0xffffffffu, reach >= k ? top : reach2 >= k ? next : 0u);
+}
+// The number of a key (of none: the lowest).
+__device__ __forceinline__ float number_of(uint32_t key) {
+    return key > 1 ? __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key) : kLowest;
+}
+
+// A warp chooses groups whose maxima reach a value that k of them, at least, reach (all where there are less), in order of their
+// numbers.  Where it lets more than 2 k through (many equal ones), the k-th largest of all is found bit by bit, and of those
+// equal to it the first are taken.
+__device__ __forceinline__ void choose(Shared& sh, int groups, int k) {
+    const int lane = threadIdx.x & 31;
+    uint32_t least = max(bound_of(sh.top, groups, k, reinterpret_cast<uint32_t*>(sh.z)), 1u);
     auto reach = [&](uint32_t from) {  // how many are no less
         int n = 0;
         for (int g = lane; g < groups; g += 32) n += key_of(sh.top[g]) >= from;
@@ -253,7 +260,7 @@ __device__ __forceinline__ void choose(Shared& sh, int groups, int k) {
     }
     if (lane == 0) {
         sh.n_groups = n;
-        sh.least = least > 1 ? __uint_as_float(least >> 31 ? least & 0x7fffffffu : ~least) : kLowest;
+        sh.least = number_of(least);
     }
 }
 
@@ -297,7 +304,7 @@ __device__ __forceinline__ void finish(const dllm_serve_logprobs_args& a, int ro
     __syncthreads();
     // ------------------------------------------------ the chosen groups, their first loads asked for
     const int n_groups = k ? sh.n_groups : 0;
-    const float least = k && k == a.n_top ? sh.least : kLowest;
+    float least = k && k == a.n_top ? sh.least : kLowest;
     const int total = n_groups * group_pieces * kLoads;
     static_assert(kThreads % kLoads == 0, "a load's place in its step is the thread's own");
     auto id_of = [&](int i) {
@@ -338,10 +345,16 @@ __device__ __forceinline__ void finish(const dllm_serve_logprobs_args& a, int ro
             const int v = id_of(i);
             if (VEC && v + kPer <= a.vocab) Raw<T>::floats(sh.ring[i - i0], z);
             else load_some(src, v, a.vocab, z);
+            if (static_cast<unsigned>(a.mask_id - v) < kPer) {
+#pragma unroll
+                for (int c = 0; c < kPer; ++c)
+                    if (v + c == a.mask_id) z[c] = -INFINITY;
+            }
             return v;
         };
         const int mine = (min(total - i0, kRing) - tid + kThreads - 1) / kThreads;
         uint32_t hits = 0;
+        float most = -INFINITY;
 #pragma unroll 4
         for (int u = 0; u < mine; ++u) {
             float z[kPer];
@@ -350,6 +363,17 @@ __device__ __forceinline__ void finish(const dllm_serve_logprobs_args& a, int ro
 #pragma unroll
             for (int c = 1; c < kPer; ++c) mx = fmaxf(mx, z[c]);
             hits |= static_cast<uint32_t>(mx >= least) << u;
+            most = fmaxf(most, mx);
+        }
+        if (a.n_top > 1 && groups < 4 * a.n_top && i0 == 0) {  // few groups for the ids wanted: what so many threads reach is a better limit
+            sh.top[tid] = most;
+            __syncthreads();
+            if (warp == 0) {
+                const uint32_t key = bound_of(sh.top, kThreads, a.n_top, reinterpret_cast<uint32_t*>(sh.z));
+                if (lane == 0) sh.least = number_of(key);
+            }
+            __syncthreads();
+            least = fmaxf(least, sh.least);
         }
         for (; hits; hits &= hits - 1) {
             float z[kPer];
