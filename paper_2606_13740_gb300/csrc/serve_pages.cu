@@ -183,9 +183,9 @@ __global__ void __launch_bounds__(kMoveThreads, 2)
 }
 
 // ---------------------------------------------------------------------------------------------- fork
-constexpr int kForkThreads = 1024;
-constexpr int kForkWarps = kForkThreads / 32;
 constexpr int kForkCtas = 8;  // a cluster
+template <bool SMALL>
+constexpr int kForkThreads = SMALL ? 512 : 1024;
 // One CTA with all of it in shared memory, for so many requests, pages of the pool, and of the rows.
 constexpr int kSmallBatch = 1024, kSmallPages = 12288, kSmallStage = 16384;
 size_t fork_smem(const ServeShape& s, bool small) {
@@ -236,36 +236,37 @@ __device__ __forceinline__ int cluster_size() {
     return static_cast<int>(r);
 }
 // Sum over the block of the values before this thread's; total in sum.
+template <int WARPS>
 __device__ __forceinline__ int block_before(int v, int* buf, int* sum) {
+    static_assert(WARPS <= 32, "a lane for each warp's sum");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int upto = v;
+    auto scan = [&](int x) {
 #pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-        const int o = __shfl_up_sync(0xffffffffu, upto, d);
-        if (lane >= d) upto += o;
-    }
+        for (int d = 1; d < 32; d *= 2) {
+            const int o = __shfl_up_sync(0xffffffffu, x, d);
+            if (lane >= d) x += o;
+        }
+        return x;
+    };
+    const int upto = scan(v);
     __syncthreads();
     if (lane == 31) buf[warp] = upto;
     __syncthreads();
-    int before = 0, all = 0;
-    for (int w = 0; w < kForkWarps; ++w) {
-        const int x = buf[w];
-        if (w < warp) before += x;
-        all += x;
-    }
-    *sum = all;
-    return before + upto - v;
+    const int warps = scan(lane < WARPS ? buf[lane] : 0);
+    *sum = __shfl_sync(0xffffffffu, warps, 31);
+    const int before = __shfl_sync(0xffffffffu, warps, (warp + 31) & 31);
+    return (warp ? before : 0) + upto - v;
 }
-
 // The tables.  One cluster: every CTA looks at all requests, the rows and the pages are shared out, marks go through L2
 // between cluster barriers; or (SMALL) one CTA, marks in shared memory.  Nothing that others read is changed before it is
 // known that the fork can be carried out.
 template <bool SMALL>
-__global__ void __launch_bounds__(kForkThreads, 1) k_serve_fork(const __grid_constant__ ServeShape s,
+__global__ void __launch_bounds__(kForkThreads<SMALL>, 1) k_serve_fork(const __grid_constant__ ServeShape s,
                                                              const __grid_constant__ dllm_serve_tables t, const int* src,
                                                              const int* len, int batch, int row_lanes) {
     extern __shared__ int smem[];
-    __shared__ int s_scan[kForkWarps];
+    constexpr int kThreads = kForkThreads<SMALL>, kWarps = kThreads / 32;
+    __shared__ int s_scan[kWarps];
     const int B = s.max_batch, M = s.max_pages, lg = s.page_log2, page = s.page, tid = threadIdx.x;
     // of the requests: the one continued, its length, pages held before; the last page, if partly filled; pages shared
     int *s_src = smem, *s_len = s_src + B, *s_held = s_len + B, *s_last = s_held + B, *s_shared = s_last + B;
@@ -284,7 +285,7 @@ __global__ void __launch_bounds__(kForkThreads, 1) k_serve_fork(const __grid_con
     const int p0 = static_cast<int>(static_cast<long long>(s.n_pages) * rank / ctas);
     const int p1 = static_cast<int>(static_cast<long long>(s.n_pages) * (rank + 1) / ctas);
     if (SMALL) {
-        for (int p = tid; p < s.n_pages; p += kForkThreads) mark[p] = writer[p] = 0;
+        for (int p = tid; p < s.n_pages; p += kThreads) mark[p] = writer[p] = 0;
     }
     pdl_wait();
     pdl_launch_dependents();
@@ -292,7 +293,7 @@ __global__ void __launch_bounds__(kForkThreads, 1) k_serve_fork(const __grid_con
     // ------------------------------------------------ what is asked for
     const int head0 = t.ring_pos[0], free0 = t.ring_pos[1];
     int bits = 0;
-    for (int b = tid; b < B; b += kForkThreads) {
+    for (int b = tid; b < B; b += kThreads) {
         const int held = t.held[b], from = b < batch ? src[b] : b, n = b < batch ? len[b] : 0;
         const bool bad = from < 0 || from >= B || n < 0;
         if (held < 0 || held > M) bits |= DLLM_SERVE_STATE;
@@ -308,13 +309,13 @@ __global__ void __launch_bounds__(kForkThreads, 1) k_serve_fork(const __grid_con
     auto free_page = [&](int k) { return t.ring[(head + k) % static_cast<unsigned>(s.n_pages)]; };
     const int ring0 = tid < min(batch, free_n) ? free_page(tid) : 0;  // (asked for ahead of its use)
     if (!SMALL) {
-        for (int p = p0 + tid; p < p1; p += kForkThreads) mark[p] = writer[p] = 0;
+        for (int p = p0 + tid; p < p1; p += kThreads) mark[p] = writer[p] = 0;
     }
     if (rank == 0 && tid < 2) f.head[tid] = 0;
     barrier();
 
     // ------------------------------------------------ who holds what; row_lanes threads a row
-    for (int b = tid; b < batch; b += kForkThreads) {
+    for (int b = tid; b < batch; b += kThreads) {
         const int n = s_len[b], from = s_src[b];
         int last = -1;
         if ((static_cast<long long>(n) + page - 1) >> lg > s_held[from]) {
@@ -326,8 +327,8 @@ __global__ void __launch_bounds__(kForkThreads, 1) k_serve_fork(const __grid_con
         }
         s_last[b] = last;
     }
-    const int sub = tid % row_lanes, row0 = rank * (kForkThreads / row_lanes) + tid / row_lanes;
-    const int rows = ctas * (kForkThreads / row_lanes);
+    const int sub = tid % row_lanes, row0 = rank * (kThreads / row_lanes) + tid / row_lanes;
+    const int rows = ctas * (kThreads / row_lanes);
     bool out = false;
     for (int r = row0; r < B; r += rows) {
         const int held = s_held[r], full = min(s_len[r] >> lg, s_held[s_src[r]]);
@@ -351,7 +352,7 @@ __global__ void __launch_bounds__(kForkThreads, 1) k_serve_fork(const __grid_con
         }
     }
     if (tid < min(batch, free_n) && (ring0 < 0 || ring0 >= s.n_pages)) out = true;
-    for (int k = kForkThreads + tid; k < min(batch, free_n); k += kForkThreads) out |= free_page(k) < 0 || free_page(k) >= s.n_pages;
+    for (int k = kThreads + tid; k < min(batch, free_n); k += kThreads) out |= free_page(k) < 0 || free_page(k) >= s.n_pages;
     if (out) bits |= DLLM_SERVE_STATE;
     bool wrong = __syncthreads_or(bits) != 0;
     if (!SMALL) {
@@ -369,7 +370,7 @@ __global__ void __launch_bounds__(kForkThreads, 1) k_serve_fork(const __grid_con
     if (wrong) return refuse(bits);
 
     // ------------------------------------------------ the last pages: kept, or copied
-    const int per = (batch + kForkThreads - 1) / kForkThreads;
+    const int per = (batch + kThreads - 1) / kThreads;
     const int b0 = min(batch, tid * per), b1 = min(batch, b0 + per);
     auto copied = [&](int b) {
         const int p = s_last[b];
@@ -377,7 +378,7 @@ __global__ void __launch_bounds__(kForkThreads, 1) k_serve_fork(const __grid_con
     };
     int mine = 0, taken;
     for (int b = b0; b < b1; ++b) mine += copied(b);
-    int nth = block_before(mine, s_scan, &taken);
+    int nth = block_before<kWarps>(mine, s_scan, &taken);
     if (taken > free_n) return refuse(rank == 0 && tid == 0 ? DLLM_SERVE_PAGES : 0);
     for (int b = b0; b < b1; ++b) {
         const int p = s_last[b];
@@ -417,9 +418,9 @@ __global__ void __launch_bounds__(kForkThreads, 1) k_serve_fork(const __grid_con
 
     // ------------------------------------------------ the ring
     int n_back = 0;
-    for (int p = p0 + tid; p < p1; p += kForkThreads) n_back += (mark[p] & (kCount | kKept | kOld)) == kOld;
+    for (int p = p0 + tid; p < p1; p += kThreads) n_back += (mark[p] & (kCount | kKept | kOld)) == kOld;
     int given, all = 0, at = free_n;
-    block_before(n_back, s_scan, &given);
+    block_before<kWarps>(n_back, s_scan, &given);
     for (int r = row0; r < B; r += rows)
         if (sub == 0) w.shared[r] = s_shared[r];
     if (SMALL) {
@@ -432,11 +433,11 @@ __global__ void __launch_bounds__(kForkThreads, 1) k_serve_fork(const __grid_con
             all += f.head[2 + c];
         }
     }
-    for (int q = p0; q < p1 && given; q += kForkThreads) {
+    for (int q = p0; q < p1 && given; q += kThreads) {
         const int p = q + tid;
         const bool back = p < p1 && (mark[p] & (kCount | kKept | kOld)) == kOld;
         int here;
-        const int before = block_before(back, s_scan, &here);
+        const int before = block_before<kWarps>(back, s_scan, &here);
         if (back) t.ring[(head + at + before) % static_cast<unsigned>(s.n_pages)] = p;
         at += here;
     }
@@ -512,7 +513,7 @@ cudaError_t launch_serve_fork(const ServeShape& s, const dllm_serve_tables& t, c
     while (row_lanes < 32 && row_lanes < s.max_pages) row_lanes *= 2;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(small ? 1 : kForkCtas);
-    cfg.blockDim = dim3(kForkThreads);
+    cfg.blockDim = dim3(small ? kForkThreads<true> : kForkThreads<false>);
     cfg.dynamicSmemBytes = fork_smem(s, small);
     cfg.stream = st;
     cudaLaunchAttribute at[2];
