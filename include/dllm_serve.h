@@ -12,6 +12,8 @@
  *   dllm_serve_attention     attention over the prefix and the own pages
  *   and at its end
  *   dllm_serve_logits        penalties, biases, grammar, and the decision.
+ * dllm_serve_drafts.h adds trees of drafted tokens, requests that continue
+ * others, and log probabilities.
  *
  * Conventions: those of dllm.h for return codes, error messages
  * (dllm_last_error(NULL)) and pointers, with these differences.  Every call is
@@ -87,6 +89,7 @@ enum {
     DLLM_SERVE_STATE = 64     /* table, held or ring_pos are not what a plan leaves (request refused, or its keys read
                                * as zeros), or an attention after another config's plan (zeros, as after a reset and
                                * no plan, which sets no bit) */
+    /* 128 and 256: dllm_serve_drafts.h */
 };
 
 /* Bytes of the buffers for cfg (bytes nullable) and, with mem (16-byte aligned
@@ -105,7 +108,8 @@ int dllm_serve_reset(const dllm_serve_config* cfg, const dllm_serve_tables* t, v
  * next plan at the earliest.  len = q_len = 0 ends a request.  A request whose
  * lengths are wrong, or that needs pages when the needs of the requests up to
  * it pass what was free, is refused: it keeps what it held, its rows get slot
- * -1 and position 0 and its n_keys is 0.
+ * -1 and position 0 and its n_keys is 0.  So is one that would give back, or
+ * write to, pages that dllm_serve_fork has made those of several requests.
  * New tokens are packed, request after request: row_start[b] .. row_start[b + 1].
  * rows (<= max_rows): the rows of the step's arrays; rows past the last new
  * token are padding (slot -1, position 0, request -1).  Token t of request b has
