@@ -45,7 +45,8 @@ enum {
  * sees token j.  The tables' pos of a row becomes the request's first position
  * plus the number of tokens that this one follows.  A request whose tree is
  * wrong, or has more than 32 * words tokens, keeps the plan's positions; its
- * bits, and those of padding, are 0.  words 1 to 2^16. */
+ * bits, and those of padding, are 0.  words 1 to 1024 (a token walks to its
+ * root: a chain of 32768 takes 0.2 s). */
 int dllm_serve_tree(const dllm_serve_config* cfg, const dllm_serve_tables* t, const int32_t* parent, uint32_t* mask, int words,
                     int rows, void* stream);
 
@@ -53,7 +54,8 @@ int dllm_serve_tree(const dllm_serve_config* cfg, const dllm_serve_tables* t, co
  * request that were cached before the plan, and of the request's new tokens
  * those whose bit of mask[row] (dev uint32 [rows][words]) is set; tokens past
  * the row's bits it does not see, and bits past the request's tokens say
- * nothing.  After a causal plan it sees of these only those up to itself. */
+ * nothing.  After a causal plan it sees of these only those up to itself.
+ * words 1 to 2^16. */
 int dllm_serve_tree_attention(const dllm_serve_config* cfg, const dllm_serve_tables* t, const void* q, int64_t ldq,
                               const void* kc, const void* vc, const int32_t* prefix_pages, int n_prefix, float scale,
                               const uint32_t* mask, int words, void* out, float* lse, int rows, void* stream);

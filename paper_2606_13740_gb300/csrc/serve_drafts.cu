@@ -35,7 +35,7 @@ int dllm_serve_tree(const dllm_serve_config* cfg, const dllm_serve_tables* t, co
     if (!whole(t) || (rows > 0 && (!parent || !mask)) || !words(parent, mask))
         return fail(DLLM_EINVAL, "serve tree: null or misaligned buffer");
     if (rows < 0 || rows > s.max_rows) return fail(DLLM_EINVAL, "serve tree: rows must be 0 to max_rows");
-    if (words_ < 1 || words_ > 1 << 16) return fail(DLLM_EINVAL, "serve tree: words must be 1 to 2^16");
+    if (words_ < 1 || words_ > 1024) return fail(DLLM_EINVAL, "serve tree: words must be 1 to 1024");
     if (rows == 0) return DLLM_OK;
     const int sms = sm_count();
     if (sms <= 0) return fail(DLLM_ECUDA, "no CUDA device");

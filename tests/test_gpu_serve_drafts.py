@@ -451,6 +451,51 @@ def test_fork_matches_its_definition(dev, B, batch, page, hd, most, spare, steps
         ref.same(x.s)
 
 
+def test_pages_past_32_bits(dev):
+    """Pages 2^28 elements apart, 3 GB from the first: compaction and fork."""
+    x = Caches([70, 33], 16, layers=1, Hkv=1, hd=128, stride=1 << 28, seed=9, spare=3)
+    table = x.s.table.cpu().tolist()
+
+    def dense():
+        return [c[:].clone(memory_format=torch.contiguous_format) for c in x.k + x.v]
+
+    want = _compacted(x, dense(), table, [0, 1], [list(range(1, 70, 3)), [4, 8]])
+    x.s.dllm_serve_compact(x.layers, _i32([0, 1]), _i32([list(range(1, 70, 3)), [4, 8] + [0] * 21]), _i32([23, 2]))
+    x.s.dllm_serve_check()
+    x.same(want)
+    ref = Forks(x.s, 16)
+    copies = ref.fork([0, 0], [70, 69])
+    for a, b, n in copies:
+        for c in want:
+            c[b, :, :n] = c[a, :, :n]
+    x.s.dllm_serve_fork(x.layers, _i32([0, 0]), _i32([70, 69]))
+    x.s.dllm_serve_check()
+    x.same(want)
+    ref.same(x.s)
+
+
+@pytest.mark.parametrize("B,most,spare", [(4096, 20, 3000), (5, 50000, 4000)])
+def test_fork_of_the_largest(dev, B, most, spare):
+    """As many requests as there may be; rows of thousands of pages in a large pool."""
+    r = random.Random(B)
+    x = Caches([r.randint(0, most) for _ in range(B)], 16, layers=1, Hkv=1, spare=spare, seed=B)
+    ref = Forks(x.s, 16)
+    for step in range(3):
+        have = [len(row) * 16 for row in ref.rows]
+        src = [r.choice([b, r.randrange(B)]) for b in range(B)]
+        length = [r.choice([have[c], r.randint(have[c] // 2, have[c])]) for c in src]
+        want = x.copy()
+        copies = ref.fork(src, length)
+        assert copies is not None
+        for a, b, n in copies:
+            for c in want:
+                c[b, :, :n] = c[a, :, :n]
+        x.s.dllm_serve_fork(x.layers, _i32(src), _i32(length))
+        x.s.dllm_serve_check()
+        x.same(want)
+        ref.same(x.s)
+
+
 def test_plan_keeps_shared_pages(dev):
     """After a fork: a plan that would write to a shared page, or give it back, is refused and reported, others are not;
     the last pages are written to; a fork that ends the others frees the pages for plans again."""

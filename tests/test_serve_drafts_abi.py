@@ -51,7 +51,7 @@ def test_calls_refuse_bad_arguments(L):
     def tree(parent=P, mask=P, words=1, rows=4, tables=tp):
         return L.dllm_serve_tree(cp, tables, parent, mask, words, rows, None)
 
-    for bad in (dict(parent=None), dict(mask=None), dict(parent=P + 2), dict(mask=P + 1), dict(words=0), dict(words=(1 << 16) + 1),
+    for bad in (dict(parent=None), dict(mask=None), dict(parent=P + 2), dict(mask=P + 1), dict(words=0), dict(words=1025),
                 dict(rows=-1), dict(rows=65), dict(tables=empty), dict(tables=None)):
         assert tree(**bad) == -1, bad
     assert tree(rows=0, parent=None, mask=None) == 0
