@@ -1,7 +1,7 @@
 // Log probabilities from logits (include/dllm_serve_drafts.h, dllm_serve_logprobs): the normaliser, the entropy, given
 // tokens and the largest ones, from one read of the logits.
 //
-// A cluster takes a row, its warps stretches of it that they copy ahead into shared memory (cp.async, each lane what it
+// A cluster takes a row, its warps steps of it that they copy ahead into shared memory (cp.async, each lane what it
 // reads itself, so that nobody waits for another).  A warp keeps the largest logit m it has met and, of all the others, sums
 //   s = sum 2^y,  t = sum 2^y y,  y = z log2(e) - c
 // against a reference c that moves only when a value exceeds it by more than 8.  The largest is never among the sums,
@@ -11,8 +11,8 @@
 // leaves its maximum; where n_top groups, at least, reach a value, the n_top largest ids are no less and lie in groups that
 // reach it (of many that just reach it the first do).  These are read again, and what is no less is ranked.
 // Bound: memory, and at the end of a row the latency of that.  Measured in a graph: 512 rows of 126464 32-bit ids 44 us (259 MB: 5.9
-// TB/s), with 20 alternatives 55; 1501 rows of 152064 bf16 ids 82 (456 MB: 5.6 TB/s; issue slots 70 % busy); one row of 126464 with
-// 5 alternatives 6.7.  (Loads a step ahead in registers instead: 62 and 94.  Clamping only where -inf was met: more code than the
+// TB/s, what reading alone gives on this card), with 20 alternatives 56; 1501 rows of 152064 bf16 ids 80 (456 MB: 5.7 TB/s); one row of
+// 126464 with 5 alternatives 7.0.  (Loads a step ahead in registers instead: 62 and 94.  Clamping only where -inf was met: more code than the
 // instruction cache holds, 120 for the bf16 rows.  Every largest value met kept out one by one: 93 and 110.)
 #include "serve.cuh"
 
@@ -506,7 +506,8 @@ __device__ __forceinline__ void finish(const dllm_serve_logprobs_args& a, int ro
     }
 }
 
-// A cluster takes a row, each warp of it some groups that lie side by side; its first CTA ends it.
+// A cluster takes a row.  Its warps take turns at the groups, so that it reads in order (1501 rows of 152064 bf16 ids 82.5 ->
+// 80.5 us); its first CTA ends it.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 3)
     k_logprobs(const __grid_constant__ dllm_serve_logprobs_args a, int group_pieces, int groups) {
@@ -516,15 +517,16 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 3)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int row = blockIdx.y, share = blockIdx.x * kWarps + warp, shares = gridDim.x * kWarps;
     if (gridDim.x > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;");  // (the first CTA is there)
-    const int g0 = static_cast<int>(static_cast<long long>(groups) * share / shares);
-    const int g1 = static_cast<int>(static_cast<long long>(groups) * (share + 1) / shares);
-    const int q1 = min(g1 * group_pieces, (a.vocab + kPiece<T> - 1) / kPiece<T>), qw = VEC ? min(q1, a.vocab / kPiece<T>) : 0;
-    int q = g0 * group_pieces, asked = q, stage = 0, to = 0;
+    // steps of the row, whole ones; the warp's: those of groups share, share + shares, ...
+    const int q1 = (a.vocab + kPiece<T> - 1) / kPiece<T>, qw = VEC ? a.vocab / kPiece<T> : 0;
+    const int skip = (shares - 1) * group_pieces;
+    int q = share * group_pieces, asked = q, stage = 0, to = 0;
     pdl_wait();
     pdl_launch_dependents();
     const T* src = static_cast<const T*>(a.logits) + row * a.ld;
     uint4* const mine = sh.ring + warp * (kStages * kSpans * 32) + lane;
     const T* ps = src + static_cast<size_t>(q) * kPiece<T> + lane * kPer;
+    int asked_left = group_pieces;  // of the group
     auto ask = [&] {  // for the next whole step (a group of copies in any case, to count)
         if (asked < qw) {
 #pragma unroll
@@ -533,6 +535,11 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 3)
         cp_async_commit();
         ++asked;
         ps += kPiece<T>;
+        if (--asked_left == 0) {
+            asked_left = group_pieces;
+            asked += skip;
+            ps += static_cast<size_t>(skip) * kPiece<T>;
+        }
         to = to + 1 == kStages ? 0 : to + 1;
     };
 #pragma unroll
@@ -550,7 +557,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 3)
     Sums wide;                              // else
     const int mask_piece = a.mask_id >= 0 ? a.mask_id / kPiece<T> : -1;
     int left = group_pieces;  // steps of the group
-    for (int g = g0; q < q1; ++q) {
+    for (int g = share; q < q1;) {
         uint4* at = mine + stage * (kSpans * 32);
         cp_async_wait<kStages - 1>();
         if (q >= qw) {  // one by one
@@ -634,11 +641,13 @@ __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 3)
         stage = stage + 1 == kStages ? 0 : stage + 1;
         ask();
         best = fmaxf(best, wm);
-        if (--left == 0 || q + 1 == q1) {
+        ++q;
+        if (--left == 0 || q == q1) {
             if (lane == 0 && a.n_top) first->top[g] = best;
             best = -INFINITY;
             left = group_pieces;
-            ++g;
+            q += skip;
+            g += shares;
         }
     }
     cp_async_wait<0>();

@@ -761,6 +761,38 @@ def test_a_step_in_a_graph_on_another_stream(dev):
         b["s"].dllm_serve_check()
 
 
+def test_host_threads_on_streams_of_their_own(dev):
+    """Four threads, each with a handle, caches and logits of its own on a stream of its own: what one alone gives."""
+    import threading
+
+    def work(seed, out):
+        r = random.Random(seed)
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            x = Caches([r.randint(20, 200) for _ in range(6)], 16, hd=128 if seed % 2 else 64, spare=40, seed=seed)
+            z = torch.randn(30 + 400 * (seed % 2), 9000, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed))
+            for step in range(15):
+                keep = [sorted(r.sample(range(n), n * 2 // 3)) for n in x.L]
+                most = max(map(len, keep))
+                x.s.dllm_serve_compact(x.layers, _i32([0] * 6), _i32([k + [0] * (most - len(k)) for k in keep]), _i32([len(k) for k in keep]))
+                have = [n // 2 + 1 for n in x.L]
+                x.s.dllm_serve_fork(x.layers, _i32([b // 2 for b in range(6)]), _i32([have[b // 2] for b in range(6)]))
+                x.L = [have[b // 2] for b in range(6)]
+                lp = _logprobs(z, None, step, 1 + step)
+            out.append([c.cpu() for c in x.k + x.v] + [x.s.table.cpu(), x.s.ring_pos.cpu()] + [v.cpu() for v in lp if v is not None])
+
+    alone, together = [[] for _ in range(4)], [[] for _ in range(4)]
+    for seed in range(4):
+        work(seed, alone[seed])
+    threads = [threading.Thread(target=work, args=(seed, together[seed])) for seed in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for a, b in zip(alone, together):
+        assert len(a) == len(b) == 1 and all(torch.equal(p, q) for p, q in zip(a[0], b[0]))
+
+
 def test_results_repeat(dev):
     x = Tree([500, 0, 77], [1, 64, 32], 3000 + 8, 64, 32, 32, 128, seed=14)
     first = x.call()
