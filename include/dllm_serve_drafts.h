@@ -109,8 +109,8 @@ int dllm_serve_fork(const dllm_serve_config* cfg, const dllm_serve_tables* t, vo
  *             vocabulary and for mask_id
  *   top_ids, top_lp: the n_top largest logits in descending order (ties: lowest
  *             id), without NaN and -inf; past them id -1, -inf
- * so that peaked rows keep their digits.  A row of nothing but -inf: lse -inf,
- * entropy 0, lp -inf.  A NaN (not mask_id's) makes the row's lse, lp and
+ * so that peaked rows keep their digits (exponentials below 2^-126 are 0).  A
+ * row of nothing but -inf: lse -inf, entropy 0, lp -inf.  A NaN (not mask_id's) makes the row's lse, lp and
  * entropy NaN; logits of +inf make lse +inf, entropy NaN, lp NaN for those ids
  * and -inf for the others. */
 typedef struct {
