@@ -87,8 +87,8 @@ enum {
     DLLM_SERVE_PREFIX = 16,   /* fewer prefix pages than the plan's prefix_len needs, or one outside the pool */
     DLLM_SERVE_SLOT = 32,     /* a slot outside the pool: its row was not stored */
     DLLM_SERVE_STATE = 64     /* table, held or ring_pos are not what a plan leaves (request refused, or its keys read
-                               * as zeros), or an attention after another config's plan (zeros, as after a reset and
-                               * no plan, which sets no bit) */
+                               * as zeros), or a plan of more keys than it takes (all requests refused), or an attention
+                               * after another config's plan (zeros, as after a reset and no plan, which sets no bit) */
     /* 128 and 256: dllm_serve_drafts.h */
 };
 
@@ -110,6 +110,8 @@ int dllm_serve_reset(const dllm_serve_config* cfg, const dllm_serve_tables* t, v
  * it pass what was free, is refused: it keeps what it held, its rows get slot
  * -1 and position 0 and its n_keys is 0.  So is one that would give back, or
  * write to, pages that dllm_serve_fork has made those of several requests.
+ * A plan takes all keys that the pool has places for; requests that share pages
+ * may have up to 2^28 in all, each counted in blocks of 64, where that is more.
  * New tokens are packed, request after request: row_start[b] .. row_start[b + 1].
  * rows (<= max_rows): the rows of the step's arrays; rows past the last new
  * token are padding (slot -1, position 0, request -1).  Token t of request b has

@@ -14,6 +14,7 @@ namespace dllm {
 constexpr int kServeMaxBatch = 4096;
 constexpr int kServeBlock = 64;    // keys of a block of the work list
 constexpr int kServeRows = 128;    // query rows of an attention tile (UMMA M)
+constexpr int kServeSharedBlocks = 1 << 22;  // of a plan whose requests share pages (2^28 keys, 128 MB of the work list)
 constexpr int kServeCtas = 320;    // CTAs that the attention's work is cut for, at most: two on each of 160 SMs
 
 // A config with its defaults filled in.

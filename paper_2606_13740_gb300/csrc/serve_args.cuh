@@ -72,8 +72,13 @@ inline const char* shape_of(const dllm_serve_config* c, ServeShape* s) {
     s->dtype = c->dtype;
     s->page_stride = c->page_stride ? c->page_stride : dense;
     s->max_tiles = (c->max_rows + s->tile_tokens - 1) / s->tile_tokens;
-    // a request's last block may be one key
-    s->max_blocks = static_cast<int>((static_cast<long long>(c->n_pages) * c->page + kServeBlock - 1) / kServeBlock + c->max_batch);
+    // Blocks of a plan.  No page in two rows of the table: as many as the pool has, and a request's last one may be one key.
+    // After a fork each request may see as much as the pool has; of these up to kServeSharedBlocks.
+    auto blocks = [&](int pages) { return (static_cast<long long>(pages) * c->page + kServeBlock - 1) / kServeBlock; };
+    const long long apart = blocks(c->n_pages) + c->max_batch;
+    const long long together = c->max_batch * blocks(c->max_pages < c->n_pages ? c->max_pages : c->n_pages);
+    const long long shared = together < kServeSharedBlocks ? together : kServeSharedBlocks;
+    s->max_blocks = static_cast<int>(apart > shared ? apart : shared);
     return nullptr;
 }
 

@@ -1,0 +1,118 @@
+"""Requests that share pages after a fork, on the GPU: plans and attention over keys that are more, all requests together,
+than the pool has places."""
+import random
+
+import pytest
+
+torch = pytest.importorskip("torch")
+from test_gpu_serve import DT, Paged, _i32, _serve, dev  # noqa: E402,F401
+from test_gpu_serve_drafts import Tree, _seen, _tree_of, _words  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ plans after a fork
+class Forked(Tree):
+    """Requests that continue the first one's own positions, each up to a place of its own, with new tokens behind."""
+
+    def __init__(self, base, cuts, Q, P, page, H, Hkv, hd, causal=False, dtype="bf16", seed=0):
+        self.L, self.Q, self.P, self.page, self.H, self.Hkv, self.hd, self.causal = cuts, Q, P, page, H, Hkv, hd, causal
+        self.dtype = DT[dtype]
+        B, N, r = len(cuts), sum(Q), random.Random(seed)
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        held, npre = -(-base // page), -(-P // page)
+        n_pages = npre + held + sum(1 + -(-q // page) for q in Q)
+        self.s = s = _serve(max_batch=B, max_rows=N, page=page, n_pages=n_pages, max_pages=held + 1 + -(-max(Q) // page), n_heads=H,
+                            n_kv_heads=Hkv, head_dim=hd, dtype=dtype)
+        order = torch.randperm(n_pages, device="cuda", generator=g, dtype=torch.int32)
+        s.ring.copy_(order)
+        self.prefix = order[:npre].clone()
+        s.ring_pos.copy_(_i32([npre, n_pages - npre]))
+        self.kc, self.vc = (torch.full((n_pages, Hkv, page, hd), float("nan"), device="cuda", dtype=self.dtype) for _ in range(2))
+
+        def fresh(n):
+            return [torch.randn(n, Hkv, hd, device="cuda", generator=g).to(self.dtype) for _ in range(2)]
+
+        def put(pages, first, kv):
+            at = torch.arange(first, first + len(kv[0]), device="cuda")
+            for c, x in zip((self.kc, self.vc), kv):
+                c[pages[at // page].long(), :, at % page] = x
+
+        shared, prefix = fresh(base), fresh(P)
+        s.dllm_serve_plan(_i32([base] + [0] * (B - 1)), _i32([0] * B), 0)
+        put(s.table[0], 0, shared), put(self.prefix, 0, prefix)
+        s.dllm_serve_fork(s.layers([self.kc], [self.vc]), _i32([0] * B), _i32(cuts))
+        s.dllm_serve_check()
+        s.dllm_serve_plan(_i32(cuts), _i32(Q), N, prefix_len=P, causal=causal)
+        self.k, self.v = [prefix[0]], [prefix[1]]
+        for b, (cut, q) in enumerate(zip(cuts, Q)):
+            new = fresh(q)
+            put(s.table[b], cut, new)
+            self.k.append(torch.cat([shared[0][:cut], new[0]])), self.v.append(torch.cat([shared[1][:cut], new[1]]))
+        self.q = torch.randn(N, H, hd, device="cuda", generator=g).to(self.dtype)
+        self.words = -(-max(Q) // 32)
+        self.bits = [b for q in Q for b in _seen(_tree_of(r, q))]
+        self.mask = _i32([_words(b, self.words) for b in self.bits])
+
+    def check_plain(self):
+        """dllm_serve_attention, whose rows see all new tokens (causal: those up to themselves)."""
+        out, lse = self.s.dllm_serve_attention(self.q, self.kc, self.vc, self.prefix, lse=True)
+        self.s.dllm_serve_check()
+        want, size, wlse = Paged.want(self)
+        u = 2.0 ** -8 if self.dtype == torch.bfloat16 else 2.0 ** -11
+        # a rounding of the output, one of each probability (which in f16 lose what is below 2^-25 too), fp32 sums
+        tol = u * want.abs() + (u + 2e-5) * size + ((self.P + max(map(len, self.k))) * 2.0 ** -25 if u < 2.0 ** -10 else 0.0)
+        assert bool(((out.double() - want).abs() <= tol).all())
+        assert bool(((lse.double() - wlse).abs() <= 1e-5 * (1 + wlse.abs())).all())
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("base,n,q,P,page,H,Hkv,hd,dtype", [
+    (1900, 12, 1, 0, 64, 8, 8, 64, "bf16"), (1920, 8, 5, 100, 64, 28, 4, 128, "f16"), (500, 40, 3, 0, 16, 16, 4, 64, "bf16"),
+    (3000, 9, 70, 300, 256, 4, 2, 128, "bf16"),
+])
+def test_requests_that_share_more_keys_than_the_pool_has_places(dev, base, n, q, P, page, H, Hkv, hd, dtype, causal):
+    """Beams of a long prompt: by bits and without, against 64 bits; nothing is refused or reported."""
+    r = random.Random(base)
+    cuts = [base - r.choice([0, 0, r.randint(0, 40)]) for _ in range(n)]
+    x = Forked(base, cuts, [q] * n, P, page, H, Hkv, hd, causal=causal, dtype=dtype, seed=n)
+    assert x.s.status.cpu().tolist()[:2] == [0, 0]
+    assert sum(-(-(c + q) // 64) for c in cuts) > x.s.cfg.n_pages * page // 64 + n
+    x.check()
+    x.check_plain()
+
+
+def test_as_many_shared_keys_as_a_plan_takes(dev):
+    """4000 requests that share 65600 keys are attended to; with 4090 of them there are more than 2^22 blocks of 64 keys:
+    the plan refuses all, takes no page, and a plan of fewer goes on."""
+    from paper_2606_13740_gb300 import DllmError
+    base, most, hd = 65600, 4090, 64
+    held = base // 16
+    s = _serve(max_batch=most, max_rows=most, page=16, n_pages=held + most, max_pages=held + 1, n_heads=1, n_kv_heads=1, head_dim=hd)
+    kc, vc = (torch.randn(held + most, 1, 16, hd, device="cuda").to(torch.bfloat16) for _ in range(2))
+    s.dllm_serve_plan(_i32([base]), _i32([0]), 0)
+    s.dllm_serve_fork(s.layers([kc], [vc]), _i32([0] * most), _i32([base] * most))
+    s.dllm_serve_check()
+    table, ring = s.table.clone(), s.ring_pos.clone()
+    q = torch.randn(most, 1, hd, device="cuda").to(torch.bfloat16)
+    s.dllm_serve_plan(_i32([base] * most), _i32([1] * most), most)
+    out = s.dllm_serve_attention(q, kc, vc)
+    assert s.status.cpu().tolist()[1:] == [most, 0, 0]
+    with pytest.raises(DllmError, match="status bits 64"):
+        s.dllm_serve_check()
+    assert bool((out == 0).all()) and bool((s.slot == -1).all()) and bool((s.n_keys == 0).all())
+    assert torch.equal(s.table, table) and torch.equal(s.ring_pos, ring) and bool((s.held == held).all())
+    n = 4000
+    s.dllm_serve_plan(_i32([base] * n), _i32([1] * n), n)
+    out = s.dllm_serve_attention(q[:n], kc, vc)
+    s.dllm_serve_check()
+    assert s.status.cpu().tolist()[1:] == [0, n, 0]
+    k, v = (c[table[0, :held].long()].reshape(base, hd).double() for c in (kc, vc))
+    last = s.table[:n, held].long()
+    for i in range(0, n, 500):
+        z = torch.cat([q[i:i + 500, 0].double() @ k.T, (q[i:i + 500, 0].double() * kc[last[i:i + 500], 0, 0].double()).sum(1, True)], 1)
+        p = torch.softmax(z * hd ** -0.5, 1)
+        own = vc[last[i:i + 500], 0, 0].double()
+        want, size = p[:, :-1] @ v + p[:, -1:] * own, p[:, :-1] @ v.abs() + p[:, -1:] * own.abs()
+        # as of the attention elsewhere: the output's rounding, the probabilities', and sums of 65601 terms in 32 bits
+        assert bool(((out[i:i + 500].double() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2e-5) * size).all())
