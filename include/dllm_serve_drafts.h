@@ -65,8 +65,11 @@ int dllm_serve_tree_attention(const dllm_serve_config* cfg, const dllm_serve_tab
  * each of them as decided.  The path begins at token 0 and goes on to the first
  * later token that follows its last one and whose id is the last one's x0, up to
  * max_len tokens.  keep[b][0 .. n[b]) (dev int32 [batch][max_len]): the path's
- * tokens, then -1; next[b]: x0 of its last token (-1: the request has no new
- * tokens, n = 0).  batch: the plan's; rows past it have none. */
+ * tokens, then -1; next[b]: x0 of its last token.  A request without new
+ * tokens, one that the plan has refused, and one whose tree dllm_serve_tree has
+ * found wrong since the plan have no path: n = 0, next -1 (so that the lengths
+ * that follow count no position that was not written).  batch: the plan's; rows
+ * past it have none. */
 int dllm_serve_accept(const dllm_serve_config* cfg, const dllm_serve_tables* t, const int32_t* parent, const int32_t* ids,
                       const int32_t* x0, int batch, int rows, int max_len, int32_t* keep, int32_t* n, int32_t* next,
                       void* stream);

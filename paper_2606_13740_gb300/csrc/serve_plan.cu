@@ -291,6 +291,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
     if (blockIdx.x == 0) {
         // -------------------------------------------- row starts, the CTAs' runs
         for (int b = threadIdx.x; b <= B; b += kThreads) t.row_start[b] = u.row[b];
+        for (int b = threadIdx.x; b < B; b += kThreads) w.left_out[b] = 0;
         // The cost of a unit: its start, its prefix steps, its own steps; of all units of the tiles before tile i.
         // (Measured at heads of 128, in prefix steps of 0.78 us: an own step 1.17, a unit's start and end 1.5 to 2.7.  Cut by steps
         // alone, the CTAs of 16 windows of 32 under 4096 shared keys ended between 34 and 47 us.)

@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_tree(const __grid_constant__
         mask[i] = 0;
     for (int b = blockIdx.x; b < batch; b += gridDim.x) {
         const int2 r = rows_of(t, b, there);
-        const int n = r.y - r.x;
+        const int n = r.y - r.x, was = w.left_out[b];
         if (n == 0) continue;
         const int* par = parent + r.x;
         bool bad = n > 32ll * words;
@@ -47,7 +47,9 @@ __global__ void __launch_bounds__(kThreads) k_serve_tree(const __grid_constant__
             if (i < kStaged) staged[i] = p;
         }
         // (a request whose rows the plan has left out in part is of no use)
-        if (__syncthreads_or(bad)) {
+        const bool wrong = __syncthreads_or(bad);
+        if (threadIdx.x == 0 && was != wrong) w.left_out[b] = wrong;
+        if (wrong) {
             if (threadIdx.x == 0) atomicOr(t.status, DLLM_SERVE_TREE);
             for (long long i = threadIdx.x; i < static_cast<long long>(n) * words; i += kThreads)
                 mask[static_cast<long long>(r.x) * words + i] = 0;
@@ -76,7 +78,8 @@ __global__ void __launch_bounds__(kThreads) k_serve_tree(const __grid_constant__
     }
 }
 
-// A warp takes a request and goes down the path, 32 tokens looked at side by side.  Bound: latency, two trips to L2 a
+// A warp takes a request and goes down the path, 32 tokens looked at side by side.  A request that the plan has refused, or
+// whose tree was wrong, has no path: its rows have attended to nothing that a decision could come from.  Bound: latency, two trips to L2 a
 // token of the path (the decision, then the children's parents and ids).  32 trees of up to 61, 4 us of the 9.9 that it takes
 // with the compaction behind it.
 __global__ void __launch_bounds__(kThreads) k_serve_accept(const __grid_constant__ ServeShape s,
@@ -90,10 +93,12 @@ __global__ void __launch_bounds__(kThreads) k_serve_accept(const __grid_constant
     if (b >= a.batch) return;
     const bool same = serve_same_shape(s, *w.head);
     if (!same && w.head->ctas && b == 0 && lane == 0) atomicOr(t.status, DLLM_SERVE_STATE);
+    const int left_out = w.left_out[b];
     int2 r = make_int2(0, 0);
     if (same && b < w.head->batch) r = rows_of(t, b, min(a.rows, w.head->rows));
     const int n = r.y - r.x;
     int* keep = a.keep + static_cast<long long>(b) * a.max_len;
+    const int slot = n > 0 ? t.slot[r.x] : -1;  // (looked at behind the walk, which does not wait for it)
     int node = n > 0 ? 0 : -1, len = 0, next = -1;
     while (node >= 0) {
         if (lane == 0) keep[len] = node;
@@ -112,6 +117,11 @@ __global__ void __launch_bounds__(kThreads) k_serve_accept(const __grid_constant
         }
         node = child;
     }
+    if (slot < 0 || left_out) {
+        len = 0;
+        next = -1;
+    }
+    __syncwarp();
     for (int i = len + lane; i < a.max_len; i += 32) keep[i] = -1;
     if (lane == 0) {
         a.n[b] = len;

@@ -116,3 +116,74 @@ def test_as_many_shared_keys_as_a_plan_takes(dev):
         want, size = p[:, :-1] @ v + p[:, -1:] * own, p[:, :-1] @ v.abs() + p[:, -1:] * own.abs()
         # as of the attention elsewhere: the output's rounding, the probabilities', and sums of 65601 terms in 32 bits
         assert bool(((out[i:i + 500].double() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2e-5) * size).all())
+
+
+# ------------------------------------------------------------------ paths of requests that were left out
+def test_accept_gives_no_path_to_requests_that_are_left_out(dev):
+    """Refused by the plan (pages, lengths), or with a wrong tree: no path, no next token, nothing moved; the others as
+    without them.  A right tree after a wrong one, and the next plan, are judged for themselves."""
+    from paper_2606_13740_gb300 import DllmError
+    q = [5, 40, 6, 3, 4]
+    s = _serve(max_batch=5, max_rows=60, page=16, n_pages=5, max_pages=4, n_heads=2, n_kv_heads=2, head_dim=64)
+    kc, vc = (torch.randn(5, 2, 16, 64, device="cuda").to(torch.bfloat16) for _ in range(2))
+    layers, x0 = s.layers([kc], [vc]), _i32([1] * 58)
+
+    def flat(trees):
+        return _i32([p for t in trees for p in t])
+
+    def chain(n):
+        return list(range(-1, n - 1))
+
+    def paths(trees):
+        keep, n, nxt = s.dllm_serve_accept(flat(trees), x0, x0, 5, 8)
+        at = [c.clone() for c in (kc, vc)]
+        s.dllm_serve_compact(layers, _i32(first), keep, n)
+        assert torch.equal(at[0], kc) and torch.equal(at[1], vc)  # (paths from token 0 on stay where they are)
+        for row, k in zip(keep.cpu().tolist(), n.cpu().tolist()):
+            assert row == list(range(k)) + [-1] * (8 - k)
+        return n.cpu().tolist(), nxt.cpu().tolist()
+
+    right = [chain(n) for n in q]
+    first = [0, 0, 4, 0, 3]
+    s.dllm_serve_plan(_i32(first), _i32([0] * 5), 0)
+    s.dllm_serve_plan(_i32([0, 0, 4, -1, 3]), _i32(q), 58)  # three pages for the second when two are left; a length of -1
+    with pytest.raises(DllmError, match="status bits 6"):
+        s.dllm_serve_check()
+    refused = [i for i, b in enumerate((0, 5, 45, 51, 54)) if int(s.slot[b]) < 0]
+    assert refused == [1, 3]
+    want = [0 if b in refused else min(n, 8) for b, n in enumerate(q)]
+    assert paths(right) == (want, [1 if n else -1 for n in want])
+    for wrong in (0, 5, -2, 1 << 30):  # of the first request, whose tree is otherwise a chain
+        trees = [[-1, 0, 1, wrong if wrong else 3, 3]] + right[1:]
+        s.dllm_serve_tree(flat(trees), 64)
+        with pytest.raises(DllmError, match="status bits 128"):
+            s.dllm_serve_check()
+        less = [0] + want[1:]
+        assert paths(trees) == (less, [1 if n else -1 for n in less])
+    s.dllm_serve_tree(flat(right), 64)
+    assert paths(right) == (want, [1 if n else -1 for n in want])
+    s.dllm_serve_tree(flat(right), 32)  # the second has more tokens than bits (it is refused all the same)
+    with pytest.raises(DllmError, match="status bits 128"):
+        s.dllm_serve_check()
+    assert paths(right)[0] == want
+
+    s.dllm_serve_reset()
+    first = [0] * 5
+    q = [33, 2, 1, 1, 1]
+    right = [chain(n) for n in q]
+    for wide, n in ((32, [0, 2, 1, 0, 0]), (64, [8, 2, 1, 0, 0])):
+        s.dllm_serve_plan(_i32([0] * 5), _i32(q), 38)
+        x0 = _i32([1] * 38)
+        if wide == 32:  # without a tree, a path is judged by the plan alone
+            assert paths(right)[0] == [8, 2, 1, 0, 0]
+        with pytest.raises(DllmError, match="status bits 4"):
+            s.dllm_serve_check()
+        s.dllm_serve_tree(flat(right), wide)
+        if wide == 32:
+            with pytest.raises(DllmError, match="status bits 128"):
+                s.dllm_serve_check()
+        assert paths(right)[0] == n
+    s.dllm_serve_check()
+    s.dllm_serve_tree(flat(right), 32)
+    s.dllm_serve_plan(_i32([0] * 5), _i32(q), 38)
+    assert paths(right)[0] == [8, 2, 1, 0, 0]
