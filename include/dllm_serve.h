@@ -59,14 +59,18 @@ typedef struct {
 } dllm_serve_config;
 
 /* Device buffers, carved by dllm_serve_layout from one piece of memory.  The
- * first four are the state of the pool, kept from step to step; a program may
- * read all of them, and write the state between steps (a page belongs to one
- * request's row of table, to the ring, or to the program). */
+ * first five are the state of the pool, kept from step to step; a program may
+ * read all of them, and write the state between steps, all five: an earlier
+ * state of this handle, that of another one (with more pages or requests), or
+ * one of its own.  A page belongs to one request's row of table, to the ring,
+ * or to the program; after dllm_serve_fork it may be in several rows, at the
+ * same place in each, which shared says. */
 typedef struct {
     int32_t* table;      /* [max_batch][max_pages]: pages of a request in order; past held: -1 */
     int32_t* held;       /* [max_batch]: pages that a request holds */
     int32_t* ring;       /* [n_pages]: free pages, oldest first, from ring_pos[0] on (cyclic) */
     int32_t* ring_pos;   /* [2]: place of the oldest free page, number of free pages */
+    int32_t* shared;     /* [max_batch]: leading pages of a request's row up to the last that another row holds too */
     int32_t* row_start;  /* [max_batch + 1]: first row of a request in the step's packed rows */
     int32_t* n_keys;     /* [max_batch]: own keys after the step (0: refused) */
     int32_t* slot;       /* [max_rows]: where a row's key and value go (-1: nowhere) */

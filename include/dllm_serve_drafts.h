@@ -97,9 +97,11 @@ int dllm_serve_compact(const dllm_serve_config* cfg, const dllm_serve_tables* t,
  * call is carried out whole or not at all: where a src or a len is wrong
  * (DLLM_SERVE_LENGTHS), or the copies are more than the free pages
  * (DLLM_SERVE_PAGES), tables and caches stay as they were and status[1] is batch.
- * What requests share is known from the last fork on.  While it is shared, a
- * plan refuses (DLLM_SERVE_SHARED) to give it back or to write to it: requests
- * that share pages are ended, or cut by more than their last page, by a fork. */
+ * What requests share is in the tables' shared, which each fork makes anew from
+ * all rows (one of requests onto themselves, at their own lengths, serves to do
+ * that alone).  While a page is shared, a plan refuses (DLLM_SERVE_SHARED) to
+ * give it back or to write to it: requests that share pages are ended, or cut by
+ * more than their last page, by a fork. */
 int dllm_serve_fork(const dllm_serve_config* cfg, const dllm_serve_tables* t, void* const* kc, void* const* vc, int n_layers,
                     const int32_t* src, const int32_t* len, int batch, void* stream);
 

@@ -21,6 +21,7 @@ int dllm_serve_layout(const dllm_serve_config* cfg, void* mem, dllm_serve_tables
     t.held = reinterpret_cast<int32_t*>(take(B * 4));
     t.ring = reinterpret_cast<int32_t*>(take(static_cast<size_t>(s.n_pages) * 4));
     t.ring_pos = reinterpret_cast<int32_t*>(take(8));
+    t.shared = reinterpret_cast<int32_t*>(take(B * 4));
     t.row_start = reinterpret_cast<int32_t*>(take((B + 1) * 4));
     t.n_keys = reinterpret_cast<int32_t*>(take(B * 4));
     t.slot = reinterpret_cast<int32_t*>(take(R * 4));

@@ -67,7 +67,6 @@ __device__ inline bool serve_same_shape(const ServeShape& s, const ServeWork& w)
 
 struct ServeArrays {
     ServeWork* head;
-    int* shared;          // [kServeMaxBatch]: leading pages of a request that others hold too, of the last fork
     int* left_out;        // [kServeMaxBatch]: whether dllm_serve_tree has found a request's tree wrong since the plan
     int4* join;           // [joins]: the unit's tile and K/V head, the first and the last CTA that holds a part of it
     int4* cta;            // [kServeCtas][2]: tile, K/V head, step within the unit, number of steps; the tile's entry
@@ -85,8 +84,6 @@ __host__ __device__ inline size_t serve_arrays(const ServeShape& s, void* base, 
     ServeArrays r;
     r.head = reinterpret_cast<ServeWork*>(b + at);
     at += serve_round(sizeof(ServeWork));
-    r.shared = reinterpret_cast<int*>(b + at);
-    at += serve_round(sizeof(int) * kServeMaxBatch);
     r.left_out = reinterpret_cast<int*>(b + at);
     at += serve_round(sizeof(int) * kServeMaxBatch);
     r.join = reinterpret_cast<int4*>(b + at);

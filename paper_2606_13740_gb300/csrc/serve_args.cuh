@@ -83,9 +83,9 @@ inline const char* shape_of(const dllm_serve_config* c, ServeShape* s) {
 }
 
 inline bool whole(const dllm_serve_tables* t) {
-    return t && t->table && t->held && t->ring && t->ring_pos && t->row_start && t->n_keys && t->slot && t->pos && t->req &&
+    return t && t->table && t->held && t->ring && t->ring_pos && t->shared && t->row_start && t->n_keys && t->slot && t->pos && t->req &&
            t->status && t->work && t->partials &&
-           words(t->table, t->held, t->ring, t->ring_pos, t->row_start, t->n_keys, t->slot, t->pos, t->req, t->status) &&
+           words(t->table, t->held, t->ring, t->ring_pos, t->shared, t->row_start, t->n_keys, t->slot, t->pos, t->req, t->status) &&
            aligned(t->work, 16) && aligned(t->partials, 16);
 }
 

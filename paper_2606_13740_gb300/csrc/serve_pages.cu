@@ -26,13 +26,13 @@ struct Column {
 // What request b asks for.  Threads: a warp's or a CTA's (THREADS of them, me one of them).  False: nothing to move.
 template <int HD, int THREADS>
 __device__ __forceinline__ bool column_of(const ServeShape& s, const dllm_serve_tables& t, const ServeCaches& c,
-                                          const ServeCompactArgs& a, const int* shared_pages, int b, int col, int me, int* s_stay,
+                                          const ServeCompactArgs& a, int b, int col, int me, int* s_stay,
                                           Column* out) {
     constexpr int kLanes = HD / 8;
     constexpr bool kWarp = THREADS == 32;
     auto any = [&](bool v) { return kWarp ? __any_sync(0xffffffffu, v) != 0 : __syncthreads_or(v) != 0; };
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int n = a.n[b], first = a.first[b], held = t.held[b], shared = shared_pages[b];
+    const int n = a.n[b], first = a.first[b], held = t.held[b], shared = t.shared[b];
     if (n == 0) return false;
     const int* keep = a.keep + static_cast<long long>(b) * a.keep_ld;
     const int* table = t.table + static_cast<size_t>(b) * s.max_pages;
@@ -90,8 +90,6 @@ __global__ void __launch_bounds__(kMoveThreads, 3)
                     const __grid_constant__ ServeCaches c, const __grid_constant__ ServeCompactArgs a) {
     constexpr int kLanes = HD / 8, kAtOnce = 32 / kLanes;  // lanes of a row of 16-byte pieces, rows of a warp's load
     constexpr int kLoads = 8, kStep = kLoads * kAtOnce;
-    ServeArrays w;
-    serve_arrays(s, t.work, &w);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nth = lane / kLanes;
     const int columns = 2 * c.n * s.Hkv;
     const long long units = static_cast<long long>(a.batch) * columns;
@@ -100,7 +98,7 @@ __global__ void __launch_bounds__(kMoveThreads, 3)
     for (long long unit = static_cast<long long>(blockIdx.x) * kMoveWarps + warp; unit < units;
          unit += static_cast<long long>(gridDim.x) * kMoveWarps) {
         Column u;
-        if (!column_of<HD, 32>(s, t, c, a, w.shared, static_cast<int>(unit / columns), static_cast<int>(unit % columns), lane, nullptr, &u))
+        if (!column_of<HD, 32>(s, t, c, a, static_cast<int>(unit / columns), static_cast<int>(unit % columns), lane, nullptr, &u))
             continue;
         for (int i0 = u.from; i0 < u.n; i0 += kStep) {
             long long src = 0, dst = 0;
@@ -136,8 +134,6 @@ __global__ void __launch_bounds__(kMoveThreads, 2)
     constexpr int kRows = kMoveLoads * kAtOnce, kStep = kRows * kMoveWarps;  // of a warp, of a CTA
     extern __shared__ __align__(16) uint4 ring[];
     __shared__ int s_stay[kMoveWarps];
-    ServeArrays w;
-    serve_arrays(s, t.work, &w);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nth = lane / kLanes;
     const int columns = 2 * c.n * s.Hkv;
     const long long units = static_cast<long long>(a.batch) * columns;
@@ -146,7 +142,7 @@ __global__ void __launch_bounds__(kMoveThreads, 2)
     pdl_launch_dependents();
     for (long long unit = blockIdx.x; unit < units; unit += gridDim.x) {
         Column u;
-        if (column_of<HD, kMoveThreads>(s, t, c, a, w.shared, static_cast<int>(unit / columns), static_cast<int>(unit % columns),
+        if (column_of<HD, kMoveThreads>(s, t, c, a, static_cast<int>(unit / columns), static_cast<int>(unit % columns),
                                         threadIdx.x, s_stay, &u)) {
             const int begin = u.from + warp * kRows;
             long long src = 0;
@@ -277,8 +273,6 @@ __global__ void __launch_bounds__(kForkThreads<SMALL>, 1) k_serve_fork(const __g
     // of the requests: the one continued, its length, pages held before; the last page, if partly filled; pages shared
     int *s_src = smem, *s_len = s_src + B, *s_held = s_len + B, *s_last = s_held + B, *s_shared = s_last + B;
     const int rank = SMALL ? 0 : cluster_rank(), ctas = SMALL ? 1 : cluster_size();
-    ServeArrays w;
-    serve_arrays(s, t.work, &w);
     ForkArrays f;
     fork_arrays(s, t.partials, &f);
     int* const mark = SMALL ? smem + 5 * B : f.mark;
@@ -428,7 +422,7 @@ __global__ void __launch_bounds__(kForkThreads<SMALL>, 1) k_serve_fork(const __g
     int given, all = 0, at = free_n;
     block_before<kWarps>(n_back, s_scan, &given);
     for (int r = row0; r < B; r += rows)
-        if (sub == 0) w.shared[r] = s_shared[r];
+        if (sub == 0) t.shared[r] = s_shared[r];
     if (SMALL) {
         all = given;
     } else {

@@ -84,8 +84,8 @@ struct Wants {
     bool bad, state;       // its lengths make no sense, or its held does not
     bool shared;           // pages that others hold too would be given back or written to
 };
-__device__ __forceinline__ Wants wants(const PlanArgs& a, const int* shared, int b) {
-    const int L = load_in(a.len + b), q = load_in(a.q_len + b), held = a.t.held[b], others = shared[b];
+__device__ __forceinline__ Wants wants(const PlanArgs& a, int b) {
+    const int L = load_in(a.len + b), q = load_in(a.q_len + b), held = a.t.held[b], others = a.t.shared[b];
     Wants w;
     w.rows = max(q, 0);
     w.state = held < 0 || held > a.s.max_pages;
@@ -187,7 +187,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
     if (free0 != free_n || head0 != head) bits |= DLLM_SERVE_STATE;
     long long run[3] = {0, 0, 0}, all[3];
     for (int b = b0; b < b1; ++b) {
-        const Wants x = wants(a, w.shared, b);
+        const Wants x = wants(a, b);
         run[0] += x.rows;
         run[1] += max(x.need - x.held, 0);
         run[2] += max(x.held - x.need, 0);
@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
     };
     long long more[2] = {0, 0}, all_more[2];
     for (int b = b0; b < b1; ++b) {
-        const Wants x = wants(a, w.shared, b);
+        const Wants x = wants(a, b);
         const int grow = max(x.need - x.held, 0), L = load_in(a.len + b);
         u.row[b] = clip(run[0]);
         u.grow[b] = clip(run[1]);
@@ -437,7 +437,7 @@ __global__ void __launch_bounds__(kThreads) k_serve_plan(const __grid_constant__
 __global__ void k_serve_reset(ServeShape s, dllm_serve_tables t) {
     const size_t i0 = blockIdx.x * static_cast<size_t>(blockDim.x) + threadIdx.x, n = static_cast<size_t>(gridDim.x) * blockDim.x;
     for (size_t i = i0; i < static_cast<size_t>(s.max_batch) * s.max_pages; i += n) t.table[i] = -1;
-    for (size_t i = i0; i < s.max_batch; i += n) t.held[i] = t.n_keys[i] = 0;
+    for (size_t i = i0; i < s.max_batch; i += n) t.held[i] = t.shared[i] = t.n_keys[i] = 0;
     for (size_t i = i0; i <= s.max_batch; i += n) t.row_start[i] = 0;
     for (size_t i = i0; i < s.n_pages; i += n) t.ring[i] = static_cast<int>(i);
     for (size_t i = i0; i < s.max_rows; i += n) {
@@ -446,9 +446,6 @@ __global__ void k_serve_reset(ServeShape s, dllm_serve_tables t) {
     }
     if (i0 < 4) t.status[i0] = 0;
     if (i0 < 2) t.ring_pos[i0] = i0 ? s.n_pages : 0;
-    ServeArrays w;
-    serve_arrays(s, t.work, &w);
-    for (size_t i = i0; i < kServeMaxBatch; i += n) w.shared[i] = 0;
     if (i0 < sizeof(ServeWork) / 4) t.work[i0] = 0;
 }
 

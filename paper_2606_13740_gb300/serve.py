@@ -27,7 +27,7 @@ class dllm_serve_config(C.Structure):
 
 
 class dllm_serve_tables(C.Structure):
-    _fields_ = [(n, _P) for n in ("table", "held", "ring", "ring_pos", "row_start", "n_keys", "slot", "pos", "req",
+    _fields_ = [(n, _P) for n in ("table", "held", "ring", "ring_pos", "shared", "row_start", "n_keys", "slot", "pos", "req",
                                   "status", "work", "partials")]
 
 
@@ -150,8 +150,8 @@ class Layers:
 
 class Serve:
     """The buffers of one serving batch (a torch tensor), and the calls on them with the ABI's names.  The
-    attributes table, held, ring, ring_pos, row_start, n_keys, slot, pos, req and status are int32 views of
-    them.  One stream at a time."""
+    attributes table, held, ring, ring_pos, shared (these five are the pool's state), row_start, n_keys, slot, pos, req and
+    status are int32 views of them.  One stream at a time."""
 
     def __init__(self, cfg: ServeConfig, device=None):
         import torch
@@ -187,7 +187,7 @@ class Serve:
             return self.buffer.view(torch.int32)[at:at + count].view(*shape)
 
         self.table = view("table", cfg.max_batch, cfg.max_pages)
-        self.held, self.n_keys = view("held", cfg.max_batch), view("n_keys", cfg.max_batch)
+        self.held, self.shared, self.n_keys = (view(n, cfg.max_batch) for n in ("held", "shared", "n_keys"))
         self.ring, self.ring_pos = view("ring", cfg.n_pages), view("ring_pos", 2)
         self.row_start, self.status = view("row_start", cfg.max_batch + 1), view("status", 4)
         self.slot, self.pos, self.req = (view(n, cfg.max_rows) for n in ("slot", "pos", "req"))

@@ -6,7 +6,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 from test_gpu_serve import DT, Paged, _i32, _serve, dev  # noqa: E402,F401
-from test_gpu_serve_drafts import Tree, _seen, _tree_of, _words  # noqa: E402
+from test_gpu_serve_drafts import Caches, Tree, _compacted, _seen, _tree_of, _words  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -187,3 +187,77 @@ def test_accept_gives_no_path_to_requests_that_are_left_out(dev):
     s.dllm_serve_tree(flat(right), 32)
     s.dllm_serve_plan(_i32([0] * 5), _i32(q), 38)
     assert paths(right)[0] == [8, 2, 1, 0, 0]
+
+
+# ------------------------------------------------------------------ the pool's state, written by the program
+STATE = ("table", "held", "ring", "ring_pos", "shared")
+
+
+def _beams(**kw):
+    """Three requests that continue the first one's 40 positions, in pages of 16, and a fourth of 20."""
+    x = Caches([40, 0, 0, 20], 16, spare=12, **kw)
+    before = {n: getattr(x.s, n).clone() for n in STATE}
+    x.s.dllm_serve_fork(x.layers, _i32([0, 0, 0]), _i32([40, 40, 33]))
+    x.s.dllm_serve_check()
+    assert x.s.shared.cpu().tolist() == [2, 2, 2, 0] and not bool(before["shared"].any())
+    return x, before
+
+
+def test_a_state_from_before_a_fork_is_written_back(dev):
+    """Nothing is shared then: plans give pages back and write to them, and compactions move."""
+    x, before = _beams(seed=3)
+    s = x.s
+    for n, v in before.items():
+        getattr(s, n).copy_(v)
+    want = _compacted(x, x.copy(), s.table.cpu().tolist(), [1], [[2, 30]])
+    s.dllm_serve_compact(x.layers, _i32([1]), _i32([[2, 30]]), _i32([2]))
+    x.same(want)
+    s.dllm_serve_plan(_i32([3, 0, 0, 0]), _i32([2, 1, 0, 0]), 3)
+    s.dllm_serve_check()
+    assert s.status.cpu().tolist()[1:] == [0, 1, 4] and s.held.cpu().tolist() == [1, 1, 0, 0]
+
+
+def test_a_forked_state_moves_to_a_larger_handle(dev):
+    """With what is shared: a plan there that would give back or write to a shared page is refused, others are not, and a
+    fork there ends the sharing.  A fork of requests onto themselves finds it where a program does not know it."""
+    from paper_2606_13740_gb300 import DllmError
+    x, _ = _beams(seed=5)
+    a, n = x.s, x.s.cfg.n_pages
+    b = _serve(max_batch=9, max_rows=50, page=16, n_pages=n + 7, max_pages=20, n_heads=3, n_kv_heads=3, head_dim=64)
+    kc, vc = ([torch.cat([c, torch.zeros_like(c[:7])]) for c in cs] for cs in (x.k, x.v))
+    layers = b.layers(kc, vc)
+    wide = a.cfg.max_pages
+    b.table[:4, :wide].copy_(a.table), b.held[:4].copy_(a.held), b.shared[:4].copy_(a.shared)
+    head, free = a.ring_pos.cpu().tolist()
+    ring = a.ring.cpu().tolist()
+    left = [ring[(head + i) % n] for i in range(free)] + list(range(n, n + 7))
+    b.ring[:len(left)].copy_(_i32(left)), b.ring_pos.copy_(_i32([0, len(left)]))
+
+    def refused():
+        for length, q in ((0, 0), (16, 0), (31, 2)):
+            b.dllm_serve_plan(_i32([40, length, 33, 20]), _i32([1, q, 1, 1]), 3 + q)
+            with pytest.raises(DllmError, match="status bits 256"):
+                b.dllm_serve_check()
+            assert b.n_keys.cpu().tolist()[:4] == [41, 0, 34, 21] and b.held.cpu().tolist()[:4] == [3, 3, 3, 2]
+
+    refused()
+    b.shared.zero_()  # as by a program that does not know
+    for src in ([0, 1, 2, 3], [0, 1]):  # (all of them, or some: the rows of the others count too)
+        b.dllm_serve_fork(layers, _i32(src), _i32([40, 40, 33, 20][:len(src)]))
+        b.dllm_serve_check()
+        assert b.shared.cpu().tolist() == [2, 2, 2] + [0] * 6 and b.status.cpu().tolist()[1:] == [0, 0, 0]
+        refused()
+        b.shared.zero_()
+    b.dllm_serve_fork(layers, _i32([0, 1, 2]), _i32([40, 0, 0]))
+    b.dllm_serve_plan(_i32([5, 0, 0, 20]), _i32([1, 0, 0, 1]), 2)
+    b.dllm_serve_check()
+    assert b.shared.cpu().tolist() == [0] * 9 and b.held.cpu().tolist() == [1, 0, 0, 2] + [0] * 5
+    assert b.ring_pos.cpu().tolist()[1] == n + 7 - 3
+
+
+def test_reset_forgets_what_is_shared(dev):
+    x, _ = _beams(seed=6)
+    x.s.dllm_serve_reset()
+    assert not bool(x.s.shared.any())
+    x.s.dllm_serve_plan(_i32([3, 3, 0, 0]), _i32([4, 4, 1, 1]), 10)
+    x.s.dllm_serve_check()
