@@ -141,10 +141,10 @@ def _logits_bytes(rows, vocab):
 
 
 class Layers:
-    """The caches of a model's layers, as Serve.layers looks them over."""
+    """The caches of a model's layers, as Serve.layers looks them over; of: what they were looked over for."""
 
-    def __init__(self, kc, vc, pointers):
-        self.kc, self.vc, self.n = kc, vc, len(kc)
+    def __init__(self, kc, vc, pointers, of):
+        self.kc, self.vc, self.n, self.of = kc, vc, len(kc), of
         self.k, self.v = ((_P * self.n)(*p) for p in pointers)
 
 
@@ -345,12 +345,24 @@ class Serve:
         kc, vc = list(kc), list(vc)
         if len(kc) != len(vc):
             raise ValueError(f"{len(kc)} caches of keys, {len(vc)} of values")
-        return Layers(kc, vc, [[self._cache(name, x) for x in xs] for name, xs in (("kc", kc), ("vc", vc))])
+        return Layers(kc, vc, [[self._cache(name, x) for x in xs] for name, xs in (("kc", kc), ("vc", vc))], self._caches())
+
+    def _caches(self):
+        """What the caches of this handle's layers are like."""
+        return self._dt, self._index, self._cache_shape, self._cache_strides
+
+    def _own(self, layers):
+        """layers, if they fit this handle."""
+        if layers.of != self._caches():
+            raise ValueError("layers must be caches of %s on cuda:%s, of shape %s and strides %s, not of %s on cuda:%s, %s, %s"
+                             % (self._caches() + layers.of))
+        return layers
 
     def dllm_serve_compact(self, layers, first, keep, n):
         """Own position first[b] + keep[b][i] goes to first[b] + i, for i < n[b], in all layers (of Serve.layers); keep
         int32 [batch][any] ascends."""
         batch, ld = keep.shape
+        layers = self._own(layers)
         rc = self._L.dllm_serve_compact(self._cp, self._tp, layers.k, layers.v, layers.n, self._words("first", first, (batch,)),
                                         self._words("keep", keep, (batch, ld)), ld, self._words("n", n, (batch,)), batch,
                                         self._stream())
@@ -362,6 +374,7 @@ class Serve:
         last one is copied in all layers (of Serve.layers) unless nobody else holds it.  length 0 ends a request."""
         if len(src.shape) != 1:
             raise ValueError("src must be [batch]")
+        layers = self._own(layers)
         rc = self._L.dllm_serve_fork(self._cp, self._tp, layers.k, layers.v, layers.n, self._words("src", src, src.shape),
                                      self._words("length", length, src.shape), src.numel(), self._stream())
         if rc:
