@@ -153,6 +153,8 @@ class Serve:
     attributes table, held, ring, ring_pos, shared (these five are the pool's state), row_start, n_keys, slot, pos, req and
     status are int32 views of them.  One stream at a time."""
 
+    batch = 0  # requests of the last plan
+
     def __init__(self, cfg: ServeConfig, device=None):
         import torch
 
@@ -327,8 +329,10 @@ class Serve:
     def dllm_serve_accept(self, parent, ids, x0, batch, max_len):
         """parent, ids (the tokens) and x0 (what follows each of them, as decided) int32 of the plan's rows -> (keep, n,
         next): the path of each request's tree that the decisions bear out, int32 [batch][max_len] (-1 behind it), its
-        length, and the decision at its end."""
+        length, and the decision at its end.  batch: that of the plan, or more."""
         rows = self.rows
+        if batch < self.batch:
+            raise ValueError(f"batch is {batch}, the plan has {self.batch} requests")
         at = [self._words(name, x, (rows,)) for name, x in (("parent", parent), ("ids", ids), ("x0", x0))]
         keep = self._empty((batch, max_len), dtype=self._i32, device=self.device)
         n = self._empty((batch,), dtype=self._i32, device=self.device)

@@ -30,3 +30,16 @@ def test_layers_of_another_handle_are_refused(serve):
         for call in calls(layers(**bad)):
             with pytest.raises(ValueError, match="layers"):
                 call()
+
+
+def test_accept_takes_no_fewer_requests_than_the_plan_has(serve):
+    """The paths of those past batch would be lost without a word."""
+    s = _handle(serve, 0)
+    s.batch = 2
+    ids = [_i32(0, 4)] * 3
+    for batch in (0, 1, -1):
+        with pytest.raises(ValueError, match="plan has 2"):
+            s.dllm_serve_accept(*ids, batch, 3)
+    for batch in (2, 3):
+        with pytest.raises(AssertionError, match="launched"):
+            s.dllm_serve_accept(*ids, batch, 3)
