@@ -6,7 +6,8 @@ import pytest
 
 torch = pytest.importorskip("torch")
 from test_gpu_serve import DT, Paged, _i32, _serve, dev  # noqa: E402,F401
-from test_gpu_serve_drafts import Caches, Tree, _compacted, _seen, _tree_of, _words  # noqa: E402
+from test_gpu_serve_drafts import Caches, Forks, Tree, _compacted, _seen, _tree_of, _words  # noqa: E402
+from test_gpu_serve_drafts_example import _alone, ex  # noqa: E402,F401
 
 pytestmark = pytest.mark.gpu
 
@@ -261,3 +262,163 @@ def test_reset_forgets_what_is_shared(dev):
     assert not bool(x.s.shared.any())
     x.s.dllm_serve_plan(_i32([3, 3, 0, 0]), _i32([4, 4, 1, 1]), 10)
     x.s.dllm_serve_check()
+
+
+# ------------------------------------------------------------------ plans and forks in turn
+class Pages(Forks):
+    """Forks with the plan's definition beside the fork's."""
+
+    def __init__(self, s, page):
+        super().__init__(s, page)
+        self.most, self.shared = s.cfg.max_pages, [0] * len(self.rows)
+
+    def fork(self, src, length):
+        copies = super().fork(src, length)
+        if copies is not None:
+            count = {}
+            for p in (p for row in self.rows for p in row):
+                count[p] = count.get(p, 0) + 1
+            self.shared = [max([i + 1 for i, p in enumerate(row) if count[p] > 1] + [0]) for row in self.rows]
+        return copies
+
+    def plan(self, L, Q):
+        """(n_keys, bits, pages taken, pages given back)."""
+        budget, asked, bits, taken, back, keys = len(self.free), 0, 0, 0, [], []
+        for b, (l, q) in enumerate(zip(L, Q)):
+            row, need = self.rows[b], -(-(l + q) // self.page)
+            others = need < self.shared[b] or (q > 0 and l // self.page < self.shared[b])
+            bad = l < 0 or q < 0 or need > self.most
+            grow = 0 if bad or others else max(0, need - len(row))
+            asked += grow
+            no = 2 if bad else 256 if others else 4 if grow and asked > budget else 0
+            bits |= no
+            keys.append(0 if no else l + q)
+            if no:
+                continue
+            for _ in range(grow):
+                row.append(self.free.pop(0))
+            taken += grow
+            back += row[need:]
+            del row[need:]
+        self.free += back
+        return keys, bits, taken, len(back)
+
+
+@pytest.mark.parametrize("B,page,base,spare,steps", [(2, 16, 50, 6, 25), (7, 64, 300, 14, 25), (40, 16, 90, 100, 12),
+                                                      (1100, 16, 40, 3000, 6)])
+def test_plans_and_forks_in_turn(dev, B, page, base, spare, steps):
+    """Requests grow by plans, shrink, end, and continue one another by forks, step after step; some plans and forks cannot be
+    carried out.  Tables, ring, key counts, what is shared, and the caches."""
+    r = random.Random(B)
+    x = Caches([r.randint(0, base) for _ in range(B)], page, layers=1, Hkv=1, spare=spare, seed=B)
+    s, ref = x.s, Pages(x.s, page)
+    own = list(x.L)
+    seen = 0
+    for step in range(steps):
+        L, Q = [], []
+        for b in range(B):
+            low = ref.shared[b] * page
+            kind = r.random()
+            L.append(own[b] if kind < 0.7 else r.randint(min(low, own[b]), own[b]) if kind < 0.9 else r.randint(0, own[b]))
+            Q.append(0 if r.random() < 0.2 else r.randint(1, 20))
+        rows = min(sum(Q), s.cfg.max_rows)
+        keys, bits, taken, given = ref.plan(L, Q)
+        s.dllm_serve_plan(_i32(L), _i32(Q), rows)
+        assert s.status.cpu().tolist() == [bits | (8 if sum(Q) > rows else 0), keys.count(0) - sum(l + q == 0 for l, q in zip(L, Q)),
+                                           taken, given]
+        s.status.zero_()
+        seen |= bits
+        assert s.n_keys.cpu().tolist() == keys
+        ref.same(s)
+        own = [k or min(o, len(row) * page) for k, o, row in zip(keys, own, ref.rows)]
+        own = [0 if l + q == 0 else o for l, q, o in zip(L, Q, own)]
+        src = [r.choice([b, b, r.randrange(B)]) for b in range(B)]
+        length = [r.choice([own[c], own[c], r.randint(0, own[c]), 0]) for c in src]
+        if step % 5 == 4:
+            length[r.randrange(B)] = -1
+        want, copies = x.copy(), ref.fork(src, length)
+        s.dllm_serve_fork(x.layers, _i32(src), _i32(length))
+        status = s.status.cpu().tolist()
+        s.status.zero_()
+        if copies is None:
+            assert status[0] in (2, 4) and status[1:] == [B, 0, 0]
+        else:
+            assert status[:3] == [0, 0, len(copies)]
+            own = length
+            for a, b, n in copies:
+                for c in want:
+                    c[b, :, :n] = c[a, :, :n]
+        x.same(want)
+        ref.same(s)
+        assert s.shared.cpu().tolist() == ref.shared
+    assert B == 2 or seen & 256  # (two requests happen not to run into it)
+
+
+def test_forks_of_many_requests_that_cannot_be_carried_out(dev):
+    """Past the one-CTA form: a wrong request, a broken row or place of the ring, wherever it lies, or too few pages: all CTAs
+    leave everything as it was, and the next fork goes on."""
+    B = 1500
+    r = random.Random(8)
+    x = Caches([r.randint(17, 60) for _ in range(B)], 16, layers=1, Hkv=1, spare=900, seed=8)
+    s, names = x.s, STATE + ("n_keys",)
+    want, state = x.copy(), {n: getattr(x.s, n).clone() for n in names}
+    same, half = list(range(B)), [n // 2 for n in x.L]
+
+    def fork(src, length, bits):
+        s.dllm_serve_fork(x.layers, _i32(src), _i32(length))
+        assert s.status.cpu().tolist() == [bits, B, 0, 0]
+        s.status.zero_()
+        x.same(want)
+
+    for b in (0, 255, 256, 511, 700, 1023, 1024, B - 1):
+        for src, n in ((-1, 5), (B, 5), (1 << 30, 0), (b, -1), (b, len(x.L) * 16), (b, (1 << 31) - 1), (b, -(1 << 31))):
+            fork(same[:b] + [src] + same[b + 1:], half[:b] + [n] + half[b + 1:], 2)
+        for break_it in (lambda: s.held[b].fill_(99), lambda: s.held[b].fill_(-1), lambda: s.table[b, 0].fill_(-5),
+                         lambda: s.table[b, 1].fill_(1 << 28)):
+            break_it()
+            now = {n: getattr(s, n).clone() for n in names}
+            s.dllm_serve_fork(x.layers, _i32(same), _i32(half))
+            assert s.status.cpu().tolist()[0] & 64 and s.status.cpu().tolist()[1:] == [B, 0, 0]
+            s.status.zero_()
+            x.same(want)
+            assert all(torch.equal(getattr(s, n), v) for n, v in now.items())
+            for n, v in state.items():
+                getattr(s, n).copy_(v)
+    head = s.ring_pos.cpu().tolist()[0]
+    for k in (0, 5, 899):
+        kept = s.ring[(head + k) % s.cfg.n_pages].clone()
+        s.ring[(head + k) % s.cfg.n_pages] = -3
+        fork(same, half, 64)
+        s.ring[(head + k) % s.cfg.n_pages] = kept
+    few = [n - n % 16 + 1 if n % 16 != 1 else n - 1 for n in x.L]
+    fork([0] * B, [min(few[0], 17)] * B, 4)  # 1499 copies, 900 pages
+    assert all(torch.equal(getattr(s, n), v) for n, v in state.items())
+    ref = Pages(s, 16)
+    assert ref.fork(same, half) == []
+    s.dllm_serve_fork(x.layers, _i32(same), _i32(half))
+    s.dllm_serve_check()
+    x.same(want)
+    ref.same(s)
+
+
+# ------------------------------------------------------------------ together
+def test_tree_attention_of_pages_far_apart(dev):
+    """Pages farther apart than dense, and 2^28 elements apart: 5 GB from the first."""
+    for hd, stride in ((64, 2 * 32 * 64 * 4), (128, 4 * 32 * 128 + 8), (128, 1 << 28)):
+        for form in ("tree", "any"):
+            Tree([50, 100], [30, 65], 64, 32, 28, 4, hd, form=form, seed=13, stride=stride).check()
+
+
+def test_beams_of_a_long_prompt(ex):
+    """Beams whose prompt is longer, all beams together, than the pool: scores are those of their sequences."""
+    rng = random.Random(6)
+    prompt = [rng.randrange(ex.VOCAB) for _ in range(700)]
+    b = ex.Beams(prompt, 4, 8, seed=5)
+    assert 4 * 700 > b.serve.cfg.n_pages * 16
+    for _ in range(7):
+        b.step()
+    for score, t in zip(b.score.tolist(), b.tokens.tolist()):
+        z = torch.log_softmax(_alone(ex, prompt + t, seed=5).double(), 1)
+        want = sum(float(z[699 + i, v]) for i, v in enumerate(t))
+        # logits 1e-2 off relative to their size (about 1.5 rms): 0.015 a log probability, rms, 8 of them
+        assert abs(score - want) <= 8 * 0.03
