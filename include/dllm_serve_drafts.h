@@ -78,9 +78,10 @@ int dllm_serve_accept(const dllm_serve_config* cfg, const dllm_serve_tables* t, 
  * b < batch goes to first[b] + i, for i < n[b] (keep dev int32 [batch][keep_ld];
  * first, n dev int32 [batch]), in the n_layers caches kc[i], vc[i] (host arrays
  * of device pointers, n_layers 1 to 128, all different).  keep ascends, so that
- * places only move down; a first of n[b] or more keeps, of places that the
- * request does not hold, or of pages that others share, leaves its caches as
- * they were.  Lengths and pages stay: the next plan's len says what is left. */
+ * places only move down; a list that does not, that names places which the
+ * request does not hold, or that would write to pages which others share, leaves
+ * its caches as they were.  Lengths and pages stay: the next plan's len says what is left.
+ * (Paths belong into rows of up to 128: wider ones are taken for long lists.) */
 int dllm_serve_compact(const dllm_serve_config* cfg, const dllm_serve_tables* t, void* const* kc, void* const* vc, int n_layers,
                        const int32_t* first, const int32_t* keep, int keep_ld, const int32_t* n, int batch, void* stream);
 

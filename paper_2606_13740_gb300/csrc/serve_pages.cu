@@ -487,7 +487,11 @@ __global__ void __launch_bounds__(kMoveThreads) k_serve_copy(const __grid_consta
 
 cudaError_t launch_serve_compact(const ServeShape& s, const dllm_serve_tables& t, const ServeCaches& c,
                                  const ServeCompactArgs& a, int sms, cudaStream_t st) {
-    const bool small = a.keep_ld <= 64;
+    // By the width of the list's rows, as their lengths are on the device.  Measured in a graph, heads of 128, a warp against a
+    // CTA a column: 32 requests of 4 heads and 28 layers 41 and 77 us at 64 places, 76 and 102 at 128, 152 and 154 at 256, 584
+    // and 549 at 1024; 4 requests 6.5 and 10.0, 10.3 and 12.1, 23.8 and 17.9, 120 and 77; 32 of 32 heads and layers 321 and 652,
+    // 629 and 871, 1245 and 1357, 4953 and 4930.  (Of a wide row little of which is used, 3 places: 6.6 and 57, 3.1 and 9.0.)
+    const bool small = a.keep_ld <= 128;
     const long long units = 2ll * c.n * s.Hkv * a.batch, ctas = small ? (units + kMoveWarps - 1) / kMoveWarps : units;
     const dim3 grid(static_cast<unsigned>(ctas < 64ll * sms ? ctas : 64ll * sms));
     if (small)

@@ -422,3 +422,18 @@ def test_beams_of_a_long_prompt(ex):
         want = sum(float(z[699 + i, v]) for i, v in enumerate(t))
         # logits 1e-2 off relative to their size (about 1.5 rms): 0.015 a log probability, rms, 8 of them
         assert abs(score - want) <= 8 * 0.03
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_compact_where_one_form_gives_way_to_the_other(dev, hd):
+    """Rows of 127 to 130 places, full, short and in between."""
+    r = random.Random(hd)
+    L = [r.randint(100, 300) for _ in range(9)] + [130, 128]
+    x = Caches(L, 16, hd=hd, layers=2, Hkv=2, seed=4)
+    table = x.s.table.cpu().tolist()
+    for most in (65, 127, 128, 129, 130):
+        keep = [sorted(r.sample(range(n), min(n, r.choice([most, most, 3, r.randint(0, most)])))) for n in L]
+        want = _compacted(x, x.copy(), table, [0] * 11, keep)
+        x.s.dllm_serve_compact(x.layers, _i32([0] * 11), _i32([k + [-1] * (most - len(k)) for k in keep]), _i32([len(k) for k in keep]))
+        x.s.dllm_serve_check()
+        x.same(want)
