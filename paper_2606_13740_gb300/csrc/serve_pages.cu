@@ -185,8 +185,10 @@ __global__ void __launch_bounds__(kMoveThreads, 2)
 constexpr int kForkCtas = 8;  // a cluster
 template <bool SMALL>
 constexpr int kForkThreads = SMALL ? 512 : 1024;
-// One CTA with all of it in shared memory, for so many requests, pages of the pool, and of the rows.
-constexpr int kSmallBatch = 1024, kSmallPages = 12288, kSmallStage = 16384;
+// One CTA with all of it in shared memory, for so many requests, and places of the rows with half the pool's pages (the
+// launch has the measurements).
+constexpr int kSmallBatch = 256, kSmallWork = 6144;
+constexpr int kSmallPages = 2 * kSmallWork, kSmallStage = kSmallWork;
 size_t fork_smem(const ServeShape& s, bool small) {
     return sizeof(int) * (5 * static_cast<size_t>(s.max_batch) + (small ? 2 * static_cast<size_t>(s.n_pages) + kSmallStage : 0));
 }
@@ -507,14 +509,19 @@ size_t serve_fork_bytes(const ServeShape& s) { return fork_arrays(s, nullptr, nu
 
 cudaError_t launch_serve_fork(const ServeShape& s, const dllm_serve_tables& t, const ServeCaches& c, const int* src,
                               const int* len, int batch, int sms, cudaStream_t st) {
-    const bool small = s.max_batch <= kSmallBatch && s.n_pages <= kSmallPages && static_cast<long long>(batch) * s.max_pages <= kSmallStage;
+    int row_lanes = 1;  // threads a row: as many as it may hold pages, up to a warp
+    while (row_lanes < 32 && row_lanes < s.max_pages) row_lanes *= 2;
+    // One CTA goes over the rows 512 places at a time, and over the pool.  Measured in a graph, one CTA against the cluster, beams
+    // in fours: 4 requests of 4 pages 6.2 and 10.6 us; 16 of 63 6.9 and 10.6, in a pool of 10284 13.1 and 13.5; 64 of 16 9.7 and
+    // 11.8, of 63 12.0 and 13.1, in a pool of 11136 17.9 and 13.7; 128 of 16 13.1 and 12.3; 256 of 16 19.8 and 12.8, of 63
+    // 29.5 and 13.5; 1000 of 11 38.0 and 16.2.
+    const long long places = static_cast<long long>(s.max_batch) * ((s.max_pages + row_lanes - 1) / row_lanes * row_lanes);
+    const bool small = s.max_batch <= kSmallBatch && places + s.n_pages / 2 <= kSmallWork;
     const auto kernel = small ? k_serve_fork<true> : k_serve_fork<false>;
     // (always the most of any call, so that host threads do not lower it between another's asking and launch)
     cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          static_cast<int>(kForkSmem[small]));
     if (e != cudaSuccess) return e;
-    int row_lanes = 1;  // threads a row: as many as it may hold pages, up to a warp
-    while (row_lanes < 32 && row_lanes < s.max_pages) row_lanes *= 2;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(small ? 1 : kForkCtas);
     cfg.blockDim = dim3(small ? kForkThreads<true> : kForkThreads<false>);
