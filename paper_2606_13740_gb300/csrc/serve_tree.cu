@@ -53,6 +53,9 @@ __global__ void __launch_bounds__(kThreads) k_serve_tree(const __grid_constant__
             if (threadIdx.x == 0) atomicOr(t.status, DLLM_SERVE_TREE);
             for (long long i = threadIdx.x; i < static_cast<long long>(n) * words; i += kThreads)
                 mask[static_cast<long long>(r.x) * words + i] = 0;
+            if (t.slot[r.x] >= 0) {  // (an earlier tree of the same plan may have moved them)
+                for (int i = 1 + threadIdx.x; i < n; i += kThreads) t.pos[r.x + i] = t.pos[r.x] + i;
+            }
             continue;
         }
         const bool refused = t.slot[r.x] < 0;

@@ -437,3 +437,24 @@ def test_compact_where_one_form_gives_way_to_the_other(dev, hd):
         x.s.dllm_serve_compact(x.layers, _i32([0] * 11), _i32([k + [-1] * (most - len(k)) for k in keep]), _i32([len(k) for k in keep]))
         x.s.dllm_serve_check()
         x.same(want)
+
+
+def test_a_wrong_tree_after_a_right_one_has_the_plan_s_positions(dev):
+    from paper_2606_13740_gb300 import DllmError
+    q = [4, 300, 3]
+    s = _serve(max_batch=3, max_rows=310, page=16, n_pages=24, max_pages=20, n_heads=2, n_kv_heads=2, head_dim=64)
+    s.dllm_serve_plan(_i32([7, 2, -1]), _i32(q), 307, prefix_len=5)
+    plain = s.pos.cpu().tolist()
+    assert plain[:6] == [12, 13, 14, 15, 7, 8] and plain[304:307] == [0, 0, 0]
+    with pytest.raises(DllmError, match="status bits 2"):
+        s.dllm_serve_check()
+    right = [-1, 0, 0, 0] + [-1] + [0] * 299 + [-1, 0, 0]
+    s.dllm_serve_tree(_i32(right), 320)
+    assert s.pos.cpu().tolist()[:304] == [12] + [13] * 3 + [7] + [8] * 299
+    s.dllm_serve_check()
+    for wrong in ([-1, 0, 2, 0] + [-1] + [0] * 298 + [300] + [-1, 0, 3], right):
+        s.dllm_serve_tree(_i32(wrong), 320 if wrong is not right else 32)
+        with pytest.raises(DllmError, match="status bits 128"):
+            s.dllm_serve_check()
+        want = plain if wrong is not right else [12, 13, 13, 13] + plain[4:]
+        assert s.pos.cpu().tolist() == want
