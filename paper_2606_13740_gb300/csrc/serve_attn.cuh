@@ -23,15 +23,16 @@
 // Keys past a request's end, and those that a row's bits or its place leave out, score -inf.  The values of keys past the
 // end, which may be anything, are set to 0 in shared memory.  In a block that rows see in part, values that are infinities or
 // NaN are set to 0 as well, as 0 times them would reach the rows that do not see them, and added at the unit's end for
-// those that do.  The warp of P V does this while the softmax is at work.  (By the softmax's warps it cost 5 causal prompts
-// under 2000 1 us more.)  Keys of a request that has rows in several tiles keep their place in L2 (64 ragged trees, 28
+// those that do.  The warp of P V does this while the softmax is at work.  (By the softmax's warps 5 causal prompts under
+// 2000 take 111.1 us for 109.6, side by side.)  Keys of a request that has rows in several tiles keep their place in L2 (64 ragged trees, 28
 // heads over 4: 79 -> 71 us; for all requests, 16 windows under 4096 shared keys lose 2.6), others leave it first.
 // Bound: 0.78 us a step, in which S, softmax and P V of a tile wait for one another, the SM's two CTAs side by side.
-// Measured in a graph, join included: 16 windows of 32 under 4096 shared keys, 32 heads of 128, 56.2 us (189 MB at
-// least: 3.4 TB/s); 96 tokens under 8001, 28 heads over 4, 40.6 us (151 MB, 3.7 TB/s); 5 causal prompts under
-// 2000, 108.2 us (127 GFLOP: 1.17 PFLOP/s); one token under 300 keys 9.5 us.  By bits: trees of 48 of 16 requests under 2048
-// shared and up to 1000 own keys, 32 heads, 53.6 us (164 MB at least: 3.1 TB/s); 64 ragged trees of up to 61 over up to 2500 own
-// keys, 28 heads over 4, f16, 67.2 us (176 MB, 2.6 TB/s; own keys are read for 2.7 tiles a request, so that L2 gives 434 MB).
+// (Of the 128 registers that two CTAs leave a thread, 3 words are spilled in every form.)  Measured in a graph, passes in a
+// row, join included: 16 windows of 32 under 4096 shared keys, 32 heads of 128, 55.9 us (189 MB at least: 3.4 TB/s); 96 tokens
+// under 8001, 28 heads over 4, 39.5 us (151 MB, 3.8 TB/s); 5 causal prompts under 2000, 110.4 us (127 GFLOP: 1.15 PFLOP/s); one
+// token under 300 keys 9.1 us.  By bits: trees of 48 of 16 requests under 2048 shared and up to 1000 own keys, 32 heads, 53.6 us
+// (164 MB at least: 3.1 TB/s); 64 ragged trees of up to 61 over up to 2500 own keys, 28 heads over 4, f16, 66.6 us (176 MB, 2.6
+// TB/s; own keys are read for 2.7 tiles a request, so that L2 gives 434 MB).
 #pragma once
 
 #include "serve.cuh"

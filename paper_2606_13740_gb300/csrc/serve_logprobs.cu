@@ -10,9 +10,10 @@
 // itself.  Parts meet in the same way.  The largest ids: each group of ids (a step, or more where that makes over 1024 groups)
 // leaves its maximum; where n_top groups, at least, reach a value, the n_top largest ids are no less and lie in groups that
 // reach it (of many that just reach it the first do).  These are read again, and what is no less is ranked.
-// Bound: memory, and at the end of a row the latency of that.  Measured in a graph: 512 rows of 126464 32-bit ids 44 us (259 MB: 5.9
-// TB/s, what reading alone gives on this card), with 20 alternatives 56; 1501 rows of 152064 bf16 ids 80 (456 MB: 5.7 TB/s); one row of
-// 126464 with 5 alternatives 7.0.  (Loads a step ahead in registers instead: 62 and 94.  Clamping only where -inf was met: more code than the
+// Bound: memory, and at the end of a row the latency of that.  Measured in a graph, passes in a row: 512 rows of 126464 32-bit ids
+// 45.9 us (259 MB: 5.6 TB/s; a kernel that does nothing but read them 39.6), with 20 alternatives 52.5; 1501 rows of 152064 bf16 ids
+// 79.9 (456 MB: 5.7 TB/s; 67 to read them); one row of 126464 with 5 alternatives 7.0.  Rows that do not begin at 16 bytes go id by
+// id, without copies ahead: 1500 rows of 50257 bf16 ids 105 us, of 50264 36.  (Loads a step ahead in registers instead: 62 and 94.  Clamping only where -inf was met: more code than the
 // instruction cache holds, 120 for the bf16 rows.  Every largest value met kept out one by one: 93 and 110.)
 #include "serve.cuh"
 

@@ -14,8 +14,8 @@ constexpr int kMoveWarps = kMoveThreads / 32;
 // time, all of a step loaded before the first is stored.  A place moves down or stays, so what is stored lies below all that
 // is yet to be loaded, and loads may run ahead.  A list that ascends from 0 begins with the places that stay.
 // Bound: memory, for long lists.  Measured in a graph, 28 layers of 4 heads of 128: 6 requests of 500 to 2000 keep two
-// thirds 82 us (484 MB: 5.9 TB/s; a warp a column 165, a CTA a column without steps ahead 100); paths of up to 16 of
-// 32 requests, with their finding, 9.9 (a column's chain: lengths, list, pages, values).
+// thirds 79.6 us (484 MB: 6.1 TB/s; a warp a column took 2 times that, a CTA a column without steps ahead 1.2 times); paths of
+// up to 16 of 32 requests, with their finding, 9.6 (a column's chain: lengths, list, pages, values).
 struct Column {
     const int* keep;
     const int* table;
@@ -83,7 +83,7 @@ __device__ __forceinline__ long long row_of(const ServeShape& s, const Column& u
     return static_cast<long long>(u.table[place >> s.page_log2]) * (s.page_stride / 8) + (place & (s.page - 1)) * (HD / 8);
 }
 
-// Short lists (an accepted path): a warp a column.
+// Short lists (an accepted path): a warp a column.  (80 registers, so that three CTAs fit an SM: 4 words are spilled.)
 template <int HD>
 __global__ void __launch_bounds__(kMoveThreads, 3)
     k_serve_compact(const __grid_constant__ ServeShape s, const __grid_constant__ dllm_serve_tables t,
@@ -262,8 +262,10 @@ __device__ __forceinline__ int block_before(int v, int* buf, int* sum) {
 // between cluster barriers; or (SMALL) one CTA, marks in shared memory.  Nothing that others read is changed before it is
 // known that the fork can be carried out.
 // Bound: latency of its phases: two trips to memory, the marks, a scan.  Measured in a graph with the copies: four beams of a
-// small request 6.0 us (the cluster for all sizes 12.3), 16 groups of 6 beams of a 28-layer cache 33.6 (163 MB copied in 22.5).
-// Threads of the one CTA: 128 5.8 and 45, 256 5.9 and 38.5, 512 6.0 and 36.3, 1024 6.4 and 36.0.
+// small request 5.6 us by one CTA (10.4 by the cluster), 16 groups of 6 beams of a 28-layer cache 32.3 by the cluster (33.1 by one
+// CTA; 163 MB copied in 22.5); by the cluster, with one layer of 4 heads, 1500 requests of 11 pages 50, 4096 of 5 84, 16 of 6250
+// 160.  Threads of the one CTA, four beams and, by it too, the groups, each pass with a graph's launch: 128 5.8 and 45, 256 5.9
+// and 38.5, 512 6.0 and 36.3, 1024 6.4 and 36.0.
 template <bool SMALL>
 __global__ void __launch_bounds__(kForkThreads<SMALL>, 1) k_serve_fork(const __grid_constant__ ServeShape s,
                                                              const __grid_constant__ dllm_serve_tables t, const int* src,

@@ -9,7 +9,7 @@
 // the tiles took 30 us for 19500 of them.)  The state that all CTAs read (held, ring_pos) is replaced by the
 // CTA that has read it last.  Pages come from the ring's front and go to its end, so that what a plan takes and what
 // it gives back never meet: the free pages and those given back fit into the ring together.
-// Bound: latency of that chain.  Measured in a graph: 16 requests of 32 tokens 8.1 us, 1000 ragged prompts 15.0; the CTA that cuts the
+// Bound: latency of that chain.  Measured in a graph: 16 requests of 32 tokens 8.2 us, 1000 ragged prompts 15.2; the CTA that cuts the
 // runs ends last, so that fewer or more items a thread for the others change nothing.
 #include "serve.cuh"
 

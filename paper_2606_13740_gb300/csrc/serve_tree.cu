@@ -18,7 +18,7 @@ __device__ __forceinline__ int2 rows_of(const dllm_serve_tables& t, int b, int r
 
 // A CTA takes a request, a thread its tokens: from each it walks to the root, which numbers the bits downwards, so that
 // a row's words are made one by one and written once.  Bound: latency, of the plan's row starts, the parents and
-// the walk (a load from shared memory a step).  Measured in a graph: a tree of 26 2.6 us, 800 trees of up to 64 4.7.
+// the walk (a load from shared memory a step).  Measured in a graph: a tree of 26 2.5 us, 800 trees of up to 64 4.8.
 __global__ void __launch_bounds__(kThreads) k_serve_tree(const __grid_constant__ ServeShape s,
                                                          const __grid_constant__ dllm_serve_tables t, const int* parent,
                                                          uint32_t* mask, int words, int rows) {
@@ -82,9 +82,9 @@ __global__ void __launch_bounds__(kThreads) k_serve_tree(const __grid_constant__
 }
 
 // A warp takes a request and goes down the path, 32 tokens looked at side by side.  A request that the plan has refused, or
-// whose tree was wrong, has no path: its rows have attended to nothing that a decision could come from.  Bound: latency, two trips to L2 a
-// token of the path (the decision, then the children's parents and ids).  32 trees of up to 61, 4 us of the 9.9 that it takes
-// with the compaction behind it.
+// whose tree was wrong, has no path: its rows have attended to nothing that a decision could come from.  Bound: latency, two
+// trips to L2 a token of the path (the decision, then the children's parents and ids).  32 trees of up to 61, 4 us of the 9.6
+// that it takes with the compaction behind it.
 __global__ void __launch_bounds__(kThreads) k_serve_accept(const __grid_constant__ ServeShape s,
                                                            const __grid_constant__ dllm_serve_tables t,
                                                            const __grid_constant__ ServeAcceptArgs a) {
