@@ -6,7 +6,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 from test_gpu_serve import DT, Paged, _i32, _serve, dev  # noqa: E402,F401
-from test_gpu_serve_drafts import Caches, Forks, Tree, _compacted, _seen, _tree_of, _words  # noqa: E402
+from test_gpu_serve_drafts import Caches, Forks, Tree, _compacted, _path, _seen, _tree_of, _words  # noqa: E402
 from test_gpu_serve_drafts_example import _alone, ex  # noqa: E402,F401
 
 pytestmark = pytest.mark.gpu
@@ -458,3 +458,83 @@ def test_a_wrong_tree_after_a_right_one_has_the_plan_s_positions(dev):
             s.dllm_serve_check()
         want = plain if wrong is not right else [12, 13, 13, 13] + plain[4:]
         assert s.pos.cpu().tolist() == want
+
+
+@pytest.mark.parametrize("B,page,H,Hkv,hd,most,spare,steps,cuts", [
+    (3, 16, 4, 2, 64, 6, 4, 12, 4), (7, 32, 28, 4, 128, 40, 9, 8, 4), (12, 64, 4, 4, 64, 9, 14, 10, 4), (5, 16, 4, 2, 64, 12, 6, 40, 60),
+    (9, 16, 28, 4, 128, 20, 1, 30, 80),
+])
+def test_drafting_beams_step_after_step(dev, B, page, H, Hkv, hd, most, spare, steps, cuts):
+    """Plan, keys stored at their slots, tree, attention, accepted path, compaction and fork, over and over, some requests refused
+    for lack of pages: the attention of every row against 64 bits, and every key and value that a request holds, where it should be."""
+    r = random.Random(B * hd)
+    g = torch.Generator(device="cuda").manual_seed(B)
+    n_pages = B * 2 + spare
+    s = _serve(max_batch=B, max_rows=B * most, page=page, n_pages=n_pages, max_pages=n_pages, n_heads=H, n_kv_heads=Hkv, head_dim=hd)
+    cache = torch.full((2, n_pages, Hkv, page, hd), float("nan"), device="cuda", dtype=torch.bfloat16)
+    layers = s.layers([cache[0]], [cache[1]])
+    own = [torch.zeros(2, 0, Hkv, hd, device="cuda", dtype=torch.bfloat16) for _ in range(B)]
+    refusals = shared = 0
+    for step in range(steps):
+        L, Q = [x.shape[1] for x in own], [r.choice([0, 1, r.randint(1, most), most]) for _ in range(B)]
+        N = max(1, sum(Q))
+        s.dllm_serve_plan(_i32(L), _i32(Q), N)
+        status = s.status.cpu().tolist()[0]
+        s.status.zero_()
+        assert status in (0, 4)
+        refused = [L[b] + Q[b] > 0 and k == 0 for b, k in enumerate(s.n_keys.cpu().tolist())]
+        refusals += sum(refused)
+        trees = [_tree_of(r, n) for n in Q]
+        parent = _i32(([p for t in trees for p in t] + [-1])[:N])
+        mask = s.dllm_serve_tree(parent, max(Q + [1]))
+        new = torch.randn(2, N, Hkv, hd, device="cuda", generator=g).to(torch.bfloat16)
+        slot = s.slot[:N].long()
+        there = (slot >= 0).nonzero()[:, 0]
+        cache[:, slot[there] // page, :, slot[there] % page] = new[:, there].transpose(0, 1)
+        q = torch.randn(N, H, hd, device="cuda", generator=g).to(torch.bfloat16)
+        out = s.dllm_serve_tree_attention(q, cache[0], cache[1], mask).view(N, H, hd)
+        ids = [[r.randrange(3) for _ in t] for t in trees]
+        x0 = [[r.randrange(3) for _ in t] for t in trees]
+        flat = [_i32(([x for t in v for x in t] + [0])[:N]) for v in (ids, x0)]
+        keep, n, nxt = s.dllm_serve_accept(parent, *flat, B, most)
+        s.dllm_serve_compact(layers, _i32(L), keep, n)
+        s.dllm_serve_check()
+        at = 0
+        for b in range(B):
+            bits = _seen(trees[b])
+            for t in range(Q[b]):
+                if refused[b]:
+                    assert bool((out[at + t] == 0).all())
+                    continue
+                sees = [j for j in range(Q[b]) if bits[t] >> j & 1]
+                k, v = (torch.cat([own[b][c], new[c, [at + j for j in sees]]]).double().repeat_interleave(H // Hkv, 1) for c in (0, 1))
+                p = torch.softmax(torch.einsum("hd,khd->hk", q[at + t].double(), k) * hd ** -0.5, 1)
+                want, size = torch.einsum("hk,khd->hd", p, v), torch.einsum("hk,khd->hd", p, v.abs())
+                # as of the attention elsewhere: the output's rounding and the probabilities'
+                assert bool(((out[at + t].double() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2e-5) * size).all())
+            path, last = _path(trees[b], ids[b], x0[b], most) if Q[b] and not refused[b] else ([], -1)
+            assert keep[b].cpu().tolist() == path + [-1] * (most - len(path)) and int(n[b]) == len(path) and int(nxt[b]) == last
+            own[b] = torch.cat([own[b], new[:, [at + j for j in path]]], 1)
+            at += Q[b]
+
+        def same():
+            table = s.table.cpu().tolist()
+            for b, x in enumerate(own):
+                if x.shape[1]:
+                    i = torch.arange(x.shape[1], device="cuda")
+                    pages = torch.tensor(table[b], device="cuda")[i // page]
+                    assert bool((pages >= 0).all()) and torch.equal(cache[:, pages, :, i % page].transpose(0, 1), x), (step, b)
+
+        same()
+        src = [r.choice([b, b, r.randrange(B)]) for b in range(B)]
+        length = [r.choice([own[c].shape[1]] * (cuts - 1) + [r.randint(0, own[c].shape[1])]) for c in src]
+        s.dllm_serve_fork(layers, _i32(src), _i32(length))
+        status = s.status.cpu().tolist()
+        s.status.zero_()
+        assert status[0] in (0, 4) and status[1] == (B if status[0] else 0)
+        if status[0] == 0:
+            own = [own[c][:, :m] for c, m in zip(src, length)]
+        same()
+        shared += int((s.shared > 0).sum())
+    assert cuts == 4 or shared > 0  # (where a request is cut at every fourth fork, hardly one fills a page)
+    assert cuts < 80 or refusals > 0
